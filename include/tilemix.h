@@ -356,6 +356,116 @@ tilemix_status tilemix_decode_varlen(const tilemix_params* params, const int32_t
                                      const uint64_t* route_bits, void* O, void* workspace,
                                      size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------------ paged key/value cache
+ * A key/value cache that grows while a server runs.  A pool holds P pages of `page_size` token
+ * slots; a sequence owns the pages that its row of the page table names, and token t of it lies
+ * in slot t % page_size of page page_table[b][t / page_size].  Sequences may share pages (a
+ * common prefix) as long as no call writes the shared slots.
+ *   K, V   [P, H_k, page_size, d] in the pool's format, each page dense, pages stride_k /
+ *          stride_v elements apart (so K and V may be interleaved in one tensor)
+ *   dK, dV FP32 [P, H_k, page_size], INT8 and E4M3 only: one scale per row (a token's d channels
+ *          of one head), pages stride_dk / stride_dv elements apart
+ * A row x with a = max |x| is held as codes c and the scale a / top, top = 127 (INT8) or 448
+ * (E4M3): c = top x / a rounded once, from the exact quotient, half to even, to a whole number
+ * or to an E4M3 number; it stands for c * scale.  A row of zeros has codes and scale 0.  A row
+ * that holds an infinity or a NaN has codes 0 and scale NaN: all of it reads as NaN.  (The scale
+ * of a row never changes, so a cache can be written one token at a time; the blocks of 64 keys of
+ * tilemix_quantize_kv would have to be made anew whenever a token raises their maximum.)
+ * The library reads seqlens_k, page_table and cu_seqlens on the device only.  A page id outside
+ * [0, P) names no page: nothing is written there, it reads as zeros, and its keys are not
+ * attended to (so the pages that a sliding window has left behind may be given back).
+ */
+typedef enum tilemix_format {
+  TILEMIX_FP16 = 0,
+  TILEMIX_BF16 = 1,
+  TILEMIX_INT8 = 2,
+  TILEMIX_E4M3 = 3   /* 1-4-3 bits, largest value 448, no infinities */
+} tilemix_format;
+
+/* A pool and the sequences of one call. */
+typedef struct tilemix_paged_cache {
+  int32_t format;             /* tilemix_format of K and V */
+  int32_t pages;              /* P >= 1 */
+  int32_t page_size;          /* 16, 32, 64, 128 or 256 */
+  int32_t heads_kv;           /* H_k >= 1 */
+  int32_t head_dim;           /* d: 64 or 128 */
+  int32_t batch;              /* B: 1 .. 65535 sequences */
+  int32_t max_pages;          /* page-table entries per sequence, >= 1; max_pages * page_size <= 2^30 */
+  int64_t stride_k, stride_v; /* elements between pages: >= H_k * page_size * d, multiples of 16 */
+  int64_t stride_dk, stride_dv; /* >= H_k * page_size, multiples of 4; ignored for FP16 and BF16 */
+  int64_t stride_table;       /* entries between rows of page_table, >= max_pages */
+  void* K;                    /* device, 16-byte aligned */
+  void* V;
+  float* dK;                  /* device, 16-byte aligned; ignored for FP16 and BF16 */
+  float* dV;
+  const int32_t* page_table;  /* device int32 [B, max_pages], 4-byte aligned */
+  const int32_t* seqlens_k;   /* device int32 [B], 4-byte aligned: tokens of each sequence */
+} tilemix_paged_cache;
+
+/*
+ * tilemix_paged_append -- write new rows into the cache, quantising them for an 8-bit pool.  The
+ * new rows of a sequence are its last ones: seqlens_k counts them already, and row r of n new
+ * ones becomes token seqlens_k[b] - n + r (the bottom-right alignment of tilemix_prefill).
+ *   type         TILEMIX_FP16 or TILEMIX_BF16: of K_new and V_new; that of a 16-bit pool
+ *   cu_seqlens   device int32 [B + 1] as for tilemix_prefill_varlen: sequence b brings rows
+ *                cu_seqlens[b] .. cu_seqlens[b + 1] - 1 of the packed K_new, V_new [total, H_k, d];
+ *                or NULL: each brings len rows, K_new, V_new [B, len, H_k, d]
+ *   len          the most new rows of a sequence, 1 .. 2^23 (1: one decode step); rows past it
+ *                are not written
+ *   total        rows of K_new and V_new, >= 0; B * len without cu_seqlens
+ *   K_new, V_new device, 16-byte aligned, read only; rows of H_k * d elements, k_stride / v_stride
+ *                elements apart (>= 0, multiples of 8: a slice of a fused projection needs no copy)
+ * Rows whose token number is negative or past max_pages * page_size are not written, nor are
+ * packed rows that no sequence owns read.  Two rows for one slot (pages shared by sequences that
+ * both write them) leave either.  Out-of-range cu_seqlens are clamped as in
+ * tilemix_prefill_varlen.
+ */
+tilemix_status tilemix_paged_append(const tilemix_paged_cache* cache, int32_t type,
+                                    const int32_t* cu_seqlens, int32_t len, int32_t total,
+                                    const void* K_new, int64_t k_stride, const void* V_new,
+                                    int64_t v_stride, void* stream);
+
+/*
+ * tilemix_paged_gather -- the inverse: the last rows of every sequence's cache as dense K and V, the
+ * operands of tilemix_prefill_varlen (all of them, n = seqlens_k[b]: a prefill in chunks over a
+ * cached prefix).
+ *   type   of K_out and V_out: TILEMIX_FP16 or TILEMIX_BF16; that of a 16-bit pool
+ *   K_out, V_out   device [total, H_k, d] or [B, len, H_k, d], dense, 16-byte aligned, written: a value
+ *          is code * scale in FP32, rounded once.  Rows of tokens that the cache does not hold
+ *          (negative, past max_pages * page_size, no page) are zeros; packed rows that no sequence
+ *          owns, and rows past len, are left as they were
+ * Other arguments as for tilemix_paged_append.
+ */
+tilemix_status tilemix_paged_gather(const tilemix_paged_cache* cache, int32_t type,
+                                    const int32_t* cu_seqlens, int32_t len, int32_t total,
+                                    void* K_out, void* V_out, void* stream);
+
+/* Bytes of device workspace tilemix_paged_decode uses for heads_q query heads (0: none). */
+tilemix_status tilemix_paged_decode_workspace_size(const tilemix_paged_cache* cache, int32_t heads_q,
+                                                   size_t* bytes);
+
+/*
+ * tilemix_paged_decode -- one decode step: each sequence's query token attends to its cached tokens.
+ *   type      of Q and O: TILEMIX_FP16 or TILEMIX_BF16; that of a 16-bit pool
+ *   heads_q   H_q, a multiple of H_k; query head h_q reads KV head h_q / (H_q / H_k)
+ *   scale     softmax scale; finite, > 0
+ *   window    0: all tokens; w >= 1: the last w of each sequence
+ *   Q         device [B, H_q, d], 16-byte aligned; sequences q_stride elements apart (>= 0, a
+ *             multiple of 8)
+ *   O         device [B, H_q, d], dense, 16-byte aligned, written
+ *   lse       device FP32 [B, H_q] or NULL: ln sum_j exp(s_j) of the scores, written (results over
+ *             parts of a cache can be joined by it)
+ *   workspace >= tilemix_paged_decode_workspace_size() bytes, 256-byte aligned; overwritten; must not
+ *             be shared with a concurrently running call; may be NULL if that size is 0
+ * O = sum_j p_j v_j with p = softmax(scale q . k_j) over the tokens attended to.  Lengths are clamped
+ * to [0, max_pages * page_size]; a sequence without any such token gets O = 0 and lse = -inf.
+ * Scores, softmax and sums are FP32; the query is not quantised.
+ */
+tilemix_status tilemix_paged_decode(const tilemix_paged_cache* cache, int32_t type, int32_t heads_q,
+                                    float scale, int32_t window, const void* Q, int64_t q_stride,
+                                    void* O, float* lse, void* workspace, size_t workspace_bytes,
+                                    void* stream);
+
 /* ------------------------------------------------------------------ routing templates
  * Host-side routing policies of Appendix B ("Policy Construction and Sharing", "Coverage
  * Accounting" and the layouts One, Zero, Band, Global, Row-Random, Aligned Sparse, BigBird,

@@ -45,6 +45,11 @@ __all__ = [
     "tilemix_decode_workspace_size",
     "tilemix_decode",
     "tilemix_decode_varlen",
+    "PagedCache",
+    "tilemix_paged_append",
+    "tilemix_paged_gather",
+    "tilemix_paged_decode_workspace_size",
+    "tilemix_paged_decode",
     "EXPORTED_SYMBOLS",
 ]
 
@@ -73,6 +78,10 @@ EXPORTED_SYMBOLS = (
     "tilemix_decode_workspace_size",
     "tilemix_decode",
     "tilemix_decode_varlen",
+    "tilemix_paged_append",
+    "tilemix_paged_gather",
+    "tilemix_paged_decode_workspace_size",
+    "tilemix_paged_decode",
     "tilemix_status_string",
     "tilemix_last_error",
 )
@@ -195,6 +204,29 @@ class _CDebugExport(ctypes.Structure):
                 ("kinds", ctypes.c_void_p)]
 
 
+class _CPagedCache(ctypes.Structure):
+    _fields_ = [
+        ("format", ctypes.c_int32),
+        ("pages", ctypes.c_int32),
+        ("page_size", ctypes.c_int32),
+        ("heads_kv", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("batch", ctypes.c_int32),
+        ("max_pages", ctypes.c_int32),
+        ("stride_k", ctypes.c_int64),
+        ("stride_v", ctypes.c_int64),
+        ("stride_dk", ctypes.c_int64),
+        ("stride_dv", ctypes.c_int64),
+        ("stride_table", ctypes.c_int64),
+        ("K", ctypes.c_void_p),
+        ("V", ctypes.c_void_p),
+        ("dK", ctypes.c_void_p),
+        ("dV", ctypes.c_void_p),
+        ("page_table", ctypes.c_void_p),
+        ("seqlens_k", ctypes.c_void_p),
+    ]
+
+
 _LIB = None
 
 
@@ -268,6 +300,17 @@ def load_library() -> ctypes.CDLL:
     lib.tilemix_decode.restype = ctypes.c_int
     lib.tilemix_decode_varlen.argtypes = [P, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
     lib.tilemix_decode_varlen.restype = ctypes.c_int
+    CP = ctypes.POINTER(_CPagedCache)
+    rows_args = [CP, ctypes.c_int32, vp, ctypes.c_int32, ctypes.c_int32, vp]
+    lib.tilemix_paged_append.argtypes = rows_args + [ctypes.c_int64, vp, ctypes.c_int64, vp]
+    lib.tilemix_paged_append.restype = ctypes.c_int
+    lib.tilemix_paged_gather.argtypes = rows_args + [vp, vp]
+    lib.tilemix_paged_gather.restype = ctypes.c_int
+    lib.tilemix_paged_decode_workspace_size.argtypes = [CP, ctypes.c_int32, ctypes.POINTER(ctypes.c_size_t)]
+    lib.tilemix_paged_decode_workspace_size.restype = ctypes.c_int
+    lib.tilemix_paged_decode.argtypes = [CP, ctypes.c_int32, ctypes.c_int32, ctypes.c_float, ctypes.c_int32, vp,
+                                         ctypes.c_int64, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.tilemix_paged_decode.restype = ctypes.c_int
     lib.tilemix_route_coverage.argtypes = [P, vp, ctypes.POINTER(ctypes.c_double),
                                            ctypes.POINTER(ctypes.c_double)]
     lib.tilemix_route_coverage.restype = ctypes.c_int
@@ -749,3 +792,247 @@ def tilemix_decode(Q, K, K8, dK, V8, dV, route_bits, group_size: int, scale: flo
     else:
         _check_call(load_library().tilemix_decode(ctypes.byref(cp), *rest))
     return O
+
+
+# -------------------------------------------------------------------- paged key/value cache
+
+@dataclass(frozen=True)
+class PagedCache:
+    """A pool of pages for ``tilemix_paged_append``, ``_gather`` and ``_decode``: K, V [P, Hk, page, d] CUDA
+    tensors in float16, bfloat16, int8 or float8_e4m3fn, and for the last two dK, dV float32
+    [P, Hk, page], one scale per row.  Each page is dense; pages may lie further apart (a slice of a
+    larger tensor).  A page holds 16, 32, 64, 128 or 256 tokens, d is 64 or 128."""
+    K: object
+    V: object
+    dK: object = None
+    dV: object = None
+
+    @staticmethod
+    def empty(pages: int, page_size: int, heads_kv: int, head_dim: int, dtype=None, device="cuda") -> "PagedCache":
+        """An uninitialised pool (int8 when no dtype is given)."""
+        import torch
+        dtype = torch.int8 if dtype is None else dtype
+        shape = (pages, heads_kv, page_size, head_dim)
+        K, V = (torch.empty(shape, dtype=dtype, device=device) for _ in range(2))
+        if dtype.itemsize == 2:
+            return PagedCache(K, V)
+        dK, dV = (torch.empty(shape[:3], dtype=torch.float32, device=device) for _ in range(2))
+        return PagedCache(K, V, dK, dV)
+
+
+_FORMATS: dict = {}
+
+
+def _format(dtype) -> int:
+    """tilemix_format of a torch dtype, or -1."""
+    if not _FORMATS:
+        import torch
+        _FORMATS.update({torch.float16: 0, torch.bfloat16: 1, torch.int8: 2, torch.float8_e4m3fn: 3})
+    return _FORMATS.get(dtype, -1)
+
+
+def _outer_stride(t, dims: int, name: str) -> int:
+    """Elements between the entries of t's first dimension; its last ``dims`` dimensions must be dense (the
+    stride of a dimension of size 1 means nothing)."""
+    inner = 1
+    for i in range(1, dims + 1):
+        if t.shape[-i] != 1 and t.stride(-i) != inner:
+            raise ValueError(f"{name}: the last {dims} dimensions must be dense")
+        inner *= t.shape[-i]
+    return inner if t.shape[0] == 1 else t.stride(0)
+
+
+def _require_like(t, dtype, shape, device, name):
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.get_device() != device:
+        raise ValueError(f"{name} must be on the pool's device")
+
+
+def _paged_c(cache: PagedCache, page_table, seqlens_k) -> _CPagedCache:
+    import torch
+    K, V = cache.K, cache.V
+    if not isinstance(K, torch.Tensor) or not K.is_cuda:
+        raise TypeError("the pool's K must be a CUDA (HIP) tensor")
+    fmt = _format(K.dtype)
+    if fmt < 0:
+        raise TypeError(f"the pool must be float16, bfloat16, int8 or float8_e4m3fn, got {K.dtype}")
+    if K.dim() != 4:
+        raise ValueError(f"the pool's K must be [pages, Hk, page, d], got {tuple(K.shape)}")
+    dev = K.get_device()
+    P, Hk, page, d = K.shape
+    _require_like(V, K.dtype, K.shape, dev, "the pool's V")
+    c = _CPagedCache(fmt, P, page, Hk, d)
+    c.stride_k, c.stride_v = _outer_stride(K, 3, "the pool's K"), _outer_stride(V, 3, "the pool's V")
+    c.K, c.V = K.data_ptr(), V.data_ptr()
+    if fmt >= 2:
+        _require_like(cache.dK, torch.float32, K.shape[:3], dev, "the pool's dK")
+        _require_like(cache.dV, torch.float32, K.shape[:3], dev, "the pool's dV")
+        c.stride_dk, c.stride_dv = _outer_stride(cache.dK, 2, "the pool's dK"), _outer_stride(cache.dV, 2, "the pool's dV")
+        c.dK, c.dV = cache.dK.data_ptr(), cache.dV.data_ptr()
+    if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2:
+        raise ValueError("page_table must be a tensor [B, max_pages]")
+    _require_like(page_table, torch.int32, page_table.shape, dev, "page_table")
+    c.batch, c.max_pages = page_table.shape
+    c.stride_table = _outer_stride(page_table, 1, "page_table")
+    c.page_table = page_table.data_ptr()
+    _require_like(seqlens_k, torch.int32, page_table.shape[:1], dev, "seqlens_k")
+    if not seqlens_k.is_contiguous():
+        raise ValueError("seqlens_k must be contiguous")
+    c.seqlens_k = seqlens_k.data_ptr()
+    return c
+
+
+def _paged_rows(c: _CPagedCache, cu_seqlens, max_len, total, device):
+    """(cu_seqlens pointer, len, total, shape of the rows) of an append or gather."""
+    if cu_seqlens is None:
+        return None, max_len, c.batch * max_len, (c.batch, max_len, c.heads_kv, c.head_dim)
+    import torch
+    _require_like(cu_seqlens, torch.int32, (c.batch + 1,), device, "cu_seqlens")
+    if not cu_seqlens.is_contiguous():
+        raise ValueError("cu_seqlens must be contiguous")
+    return cu_seqlens.data_ptr(), max_len, total, (total, c.heads_kv, c.head_dim)
+
+
+def _row_stride(t, c: _CPagedCache, name: str) -> int:
+    """Elements between the token rows of t, [total, Hk, d] or [B, len, Hk, d]."""
+    if t.dim() == 3:
+        return _outer_stride(t, 2, name)
+    B, L = t.shape[:2]
+    if B * L == 0:
+        return c.heads_kv * c.head_dim
+    row = _outer_stride(t[:, 0] if L == 1 else t[0], 2, name)
+    if B > 1 and L > 1 and t.stride(0) != L * row:
+        raise ValueError(f"{name}: the rows of all sequences must be equally far apart")
+    return row
+
+
+def _on_device(device: int):
+    """The library launches on the current device: make it the tensors' one."""
+    import contextlib
+    import torch
+    return contextlib.nullcontext() if torch.cuda.current_device() == device else torch.cuda.device(device)
+
+
+def _stream_on(stream, device: int) -> int:
+    if stream is not None and stream.device_index != device:
+        raise ValueError("stream must be on the pool's device")
+    return _stream(stream)
+
+
+def tilemix_paged_append(cache: PagedCache, K, V, page_table, seqlens_k, cu_seqlens=None,
+                         max_len: int | None = None, *, stream=None) -> None:
+    """Write new rows into a paged cache; they are the last rows of their sequences, which
+    ``seqlens_k`` (int32 CUDA [B]) counts already.  K, V: float16 or bfloat16 CUDA [total, Hk, d] with
+    ``cu_seqlens`` (int32 CUDA [B + 1]) and ``max_len`` >= the most rows of a sequence, or
+    [B, L, Hk, d], L rows for each sequence (1: a decode step).  Tokens may lie any multiple of 8 elements
+    apart.  page_table: int32 CUDA [B, max_pages]; ids outside the pool name no page."""
+    c = _paged_c(cache, page_table, seqlens_k)
+    dev = cache.K.get_device()
+    packed = cu_seqlens is not None
+    if getattr(K, "ndim", None) != (3 if packed else 4):
+        raise ValueError("K and V must be [total, Hk, d] with cu_seqlens, and [B, L, Hk, d] without")
+    if packed and max_len is None:
+        raise ValueError("max_len is needed with cu_seqlens")
+    if not packed and max_len not in (None, K.shape[1]):
+        raise ValueError("max_len is the rows of K without cu_seqlens")
+    cu, length, total, shape = _paged_rows(c, cu_seqlens, max_len if packed else K.shape[1], K.shape[0], dev)
+    dtype = K.dtype
+    if _format(dtype) not in (0, 1):
+        raise TypeError(f"K must be float16 or bfloat16, got {dtype}")
+    _require_like(K, dtype, shape, dev, "K")
+    _require_like(V, dtype, shape, dev, "V")
+    ks, vs = _row_stride(K, c, "K"), _row_stride(V, c, "V")
+    with _on_device(dev):
+        _check(load_library().tilemix_paged_append(ctypes.byref(c), _format(dtype), cu, length, total, K.data_ptr(), ks,
+                                                   V.data_ptr(), vs, _stream_on(stream, dev)))
+
+
+def tilemix_paged_gather(cache: PagedCache, page_table, seqlens_k, max_len: int, cu_seqlens=None,
+                         total: int | None = None, *, dtype=None, K=None, V=None, stream=None):
+    """Read the last rows of every sequence back: with ``cu_seqlens`` (int32 CUDA [B + 1]) sequence b's last
+    cu_seqlens[b + 1] - cu_seqlens[b] rows, packed [total, Hk, d], none with more than ``max_len``; else
+    its last max_len rows, [B, max_len, Hk, d].  Returns (K, V) in ``dtype`` (that of a 16-bit pool;
+    float16 by default for an 8-bit one), written into ``K`` and ``V`` if given: the K and V of
+    tilemix_prefill_varlen.  Tokens that the cache does not hold are zeros; packed rows that no sequence
+    owns are not written."""
+    import torch
+    c = _paged_c(cache, page_table, seqlens_k)
+    dev = cache.K.get_device()
+    if dtype is None:
+        dtype = K.dtype if K is not None else cache.K.dtype if c.format < 2 else torch.float16
+    if _format(dtype) not in (0, 1):
+        raise TypeError(f"dtype must be float16 or bfloat16, got {dtype}")
+    if cu_seqlens is not None and total is None:
+        if K is None:
+            raise ValueError("total is needed with cu_seqlens")
+        total = K.shape[0]
+    if cu_seqlens is None and total not in (None, c.batch * max_len):
+        raise ValueError("total is B * max_len without cu_seqlens")
+    cu, length, total, shape = _paged_rows(c, cu_seqlens, max_len, total, dev)
+    with _on_device(dev):
+        out = [_alloc(stream, shape, dtype=dtype, device=cache.K.device) if t is None else t for t in (K, V)]
+        for t, name in zip(out, ("K", "V")):
+            _require_like(t, dtype, shape, dev, name)
+            if not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous")
+        _check(load_library().tilemix_paged_gather(ctypes.byref(c), _format(dtype), cu, length, total,
+                                                   out[0].data_ptr(), out[1].data_ptr(), _stream_on(stream, dev)))
+    return out[0], out[1]
+
+
+def tilemix_paged_decode_workspace_size(cache: PagedCache, page_table, seqlens_k, heads_q: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load_library().tilemix_paged_decode_workspace_size(ctypes.byref(_paged_c(cache, page_table, seqlens_k)),
+                                                              heads_q, ctypes.byref(n)))
+    return n.value
+
+
+def tilemix_paged_decode(cache: PagedCache, Q, page_table, seqlens_k, scale: float | None = None, *, window: int = 0,
+                         O=None, lse=None, return_lse: bool = False, workspace=None, stream=None):
+    """One decode step over a paged cache: Q [B, 1, Hq, d] (float16 or bfloat16, that of a 16-bit pool; sequences
+    may lie any multiple of 8 elements apart) attends to each sequence's ``seqlens_k`` tokens, or its
+    last ``window`` >= 1.  Returns O, like Q, and with ``return_lse`` (O, lse): float32 [B, Hq], the log of
+    the sum of e^score.  A sequence without a token gets O = 0 and lse = -inf.  ``O``, ``lse`` and ``workspace``
+    (uint8, >= tilemix_paged_decode_workspace_size) are allocated when not given."""
+    import torch
+    c = _paged_c(cache, page_table, seqlens_k)
+    dev = cache.K.get_device()
+    if getattr(Q, "ndim", None) != 4:
+        raise ValueError("Q must be [B, 1, Hq, d]")
+    dtype = Q.dtype
+    if _format(dtype) not in (0, 1):
+        raise TypeError(f"Q must be float16 or bfloat16, got {dtype}")
+    shape = (c.batch, 1, Q.shape[2], c.head_dim)
+    _require_like(Q, dtype, shape, dev, "Q")
+    heads = shape[2]
+    q_stride = _outer_stride(Q[:, 0], 2, "Q")
+    with _on_device(dev):
+        if O is None:
+            O = _alloc(stream, shape, dtype=dtype, device=Q.device)
+        else:
+            _require_like(O, dtype, shape, dev, "O")
+            if not O.is_contiguous():
+                raise ValueError("O must be contiguous")
+        if lse is not None:
+            _require_like(lse, torch.float32, (c.batch, heads), dev, "lse")
+            if not lse.is_contiguous():
+                raise ValueError("lse must be contiguous")
+        elif return_lse:
+            lse = _alloc(stream, (c.batch, heads), dtype=torch.float32, device=Q.device)
+        if workspace is None:
+            n = ctypes.c_size_t(0)
+            _check(load_library().tilemix_paged_decode_workspace_size(ctypes.byref(c), heads, ctypes.byref(n)))
+            nbytes = n.value
+            workspace = _alloc(stream, nbytes, dtype=torch.uint8, device=Q.device) if nbytes else None
+        else:
+            nbytes = workspace.numel() * workspace.element_size()
+        _check_call(load_library().tilemix_paged_decode(
+            ctypes.byref(c), _format(dtype), heads, scale if scale is not None else 1.0 / math.sqrt(c.head_dim), window,
+            Q.data_ptr(), q_stride, O.data_ptr(), _ptr(lse), _ptr(workspace), nbytes, _stream_on(stream, dev)))
+    return (O, lse) if return_lse else O

@@ -165,4 +165,42 @@ struct DecodePlan {
 DecodePlan plan_decode(const tilemix_params& p, DecodeCut cut);
 hipError_t launch_debug_tiles(const DebugTileArgs& args, int d, int block_m, hipStream_t stream);
 
+// A paged cache as the kernels see it.
+struct PagedPool {
+  void* K;                 // [P, Hk, page, d], pages stride_k elements apart
+  void* V;
+  float* dK;               // [P, Hk, page], 8-bit formats
+  float* dV;
+  const int* table;        // [B, max_pages], rows stride_table entries apart
+  const int* seqlens;      // [B]
+  long long stride_k, stride_v, stride_dk, stride_dv, stride_table;
+  int pages, page_shift;   // page_shift: log2 of the slots of a page
+  int Hk, B, max_pages;
+};
+
+// Arguments of the kernels that write the cache (append) and read it back (gather).
+struct PagedRowsArgs {
+  PagedPool pool;
+  const int* cu;           // [B + 1], or nullptr: len rows per sequence
+  int len, total;
+  void* K;                 // packed rows: read by append, written by gather
+  void* V;
+  long long k_stride, v_stride;   // elements between rows
+  int tile_shift;          // filled in by the launch: log2 of the tokens of a workgroup
+};
+hipError_t launch_paged_append(PagedRowsArgs args, int d, int type, int format, hipStream_t stream);
+hipError_t launch_paged_gather(PagedRowsArgs args, int d, int type, int format, hipStream_t stream);
+
+// Arguments of the decode step over a paged cache.
+struct PagedDecodeArgs {
+  PagedPool pool;
+  const void* Q;           // [B, Hq, d], sequences q_stride elements apart
+  void* O;                 // [B, Hq, d]
+  float* lse;              // [B, Hq] or nullptr
+  long long q_stride;
+  int Hq, window;
+  float scale_log2e;
+};
+hipError_t launch_paged_decode(const PagedDecodeArgs& args, int d, int type, int format, hipStream_t stream);
+
 }  // namespace tilemix

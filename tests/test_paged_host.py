@@ -1,0 +1,118 @@
+"""Host-side checks of the paged cache calls (no kernel is launched, the pointers are fake)."""
+
+import ctypes
+import os
+
+import pytest
+import torch
+
+import paper_2608_17336_amd as tm
+
+pytestmark = pytest.mark.skipif(not os.path.exists(tm.library_path()),
+                                reason="libtilemix.so not built (run __graft_entry__.build())")
+
+OK = 0x100000
+NULL, SHAPE, UNSUPPORTED, ALIGN, WORKSPACE = 1, 2, 3, 4, 5
+
+
+def _cache(**kw):
+    base = dict(format=2, pages=10, page_size=64, heads_kv=8, head_dim=128, batch=3, max_pages=5,
+                stride_k=8 * 64 * 128, stride_v=8 * 64 * 128, stride_dk=512, stride_dv=512, stride_table=5,
+                K=OK, V=OK, dK=OK, dV=OK, page_table=OK, seqlens_k=OK)
+    base.update(kw)
+    return tm._CPagedCache(**base)
+
+
+def _append(cache, type=0, cu=OK, length=7, total=20, K=OK, ks=1024, V=OK, vs=1024):
+    return tm.load_library().tilemix_paged_append(ctypes.byref(cache) if cache else None, type, cu, length, total, K, ks,
+                                                  V, vs, None)
+
+
+def _gather(cache, type=0, cu=OK, length=7, total=20, K=OK, V=OK):
+    return tm.load_library().tilemix_paged_gather(ctypes.byref(cache) if cache else None, type, cu, length, total, K, V,
+                                                  None)
+
+
+def _decode(cache, type=0, heads=32, scale=0.1, window=0, Q=OK, qs=4096, O=OK, lse=None, ws=OK, nbytes=1 << 40):
+    return tm.load_library().tilemix_paged_decode(ctypes.byref(cache) if cache else None, type, heads, scale, window, Q,
+                                                  qs, O, lse, ws, nbytes, None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(format=4), UNSUPPORTED), (dict(format=-1), UNSUPPORTED),
+    (dict(head_dim=96), UNSUPPORTED), (dict(page_size=8), UNSUPPORTED), (dict(page_size=512), UNSUPPORTED),
+    (dict(page_size=48), UNSUPPORTED),
+    (dict(pages=0), SHAPE), (dict(heads_kv=0), SHAPE), (dict(batch=0), SHAPE), (dict(max_pages=0), SHAPE),
+    (dict(batch=65536), SHAPE), (dict(heads_kv=65536), SHAPE),
+    (dict(max_pages=(1 << 24) + 1, stride_table=1 << 25), SHAPE),
+    (dict(stride_table=4), SHAPE),
+    (dict(stride_k=8 * 64 * 128 - 16), SHAPE), (dict(stride_v=8 * 64 * 128 + 8), SHAPE),
+    (dict(stride_dk=511), SHAPE), (dict(stride_dv=514), SHAPE),
+    (dict(K=None), NULL), (dict(V=None), NULL), (dict(dK=None), NULL), (dict(dV=None), NULL),
+    (dict(page_table=None), NULL), (dict(seqlens_k=None), NULL),
+    (dict(K=OK + 8), ALIGN), (dict(V=OK + 1), ALIGN), (dict(dK=OK + 4), ALIGN), (dict(dV=OK + 8), ALIGN),
+    (dict(page_table=OK + 2), ALIGN), (dict(seqlens_k=OK + 1), ALIGN),
+])
+def test_cache_refusals(kw, status):
+    for call in (_append, _gather, _decode):
+        assert call(_cache(**kw)) == status, call
+        assert tm.load_library().tilemix_last_error()
+
+
+def test_null_cache_and_types():
+    for call in (_append, _gather, _decode):
+        assert call(None) == NULL
+        assert call(_cache(), type=2) == UNSUPPORTED
+        assert call(_cache(format=1), type=0) == UNSUPPORTED     # a 16-bit pool and rows of another type
+        assert call(_cache(format=0), type=1) == UNSUPPORTED
+    assert tm.load_library().tilemix_paged_decode_workspace_size(None, 32, None) == NULL
+    assert tm.load_library().tilemix_paged_decode_workspace_size(ctypes.byref(_cache()), 32, None) == NULL
+
+
+def test_16bit_pools_need_no_scales():
+    none = dict(dK=None, dV=None, stride_dk=0, stride_dv=0)
+    assert _append(_cache(format=0, **none), total=0) == 0
+    assert _decode(_cache(format=1, **none), type=1, Q=None) == NULL   # passed the cache's checks
+
+
+def test_rows_refusals():
+    for call in (_append, _gather):
+        assert call(_cache(), length=0) == SHAPE
+        assert call(_cache(), length=(1 << 23) + 1) == SHAPE
+        assert call(_cache(), total=-1) == SHAPE
+        assert call(_cache(), cu=None, length=7, total=20) == SHAPE    # not batch * len
+        assert call(_cache(), cu=OK + 2) == ALIGN
+        assert call(_cache(), K=None) == NULL
+        assert call(_cache(), V=None) == NULL
+        assert call(_cache(), K=OK + 8) == ALIGN
+        assert call(_cache(), V=OK + 2) == ALIGN
+        assert call(_cache(), total=0, K=None, V=None) == 0            # nothing to do
+    assert _append(_cache(), ks=-8) == SHAPE
+    assert _append(_cache(), vs=1028) == SHAPE
+
+
+def test_decode_refusals():
+    assert _decode(_cache(), heads=0) == SHAPE
+    assert _decode(_cache(), heads=30) == SHAPE
+    assert _decode(_cache(), heads=65536) == SHAPE
+    for scale in (0.0, -1.0, float("nan"), float("inf")):
+        assert _decode(_cache(), scale=scale) == SHAPE
+    assert _decode(_cache(), window=-1) == SHAPE
+    assert _decode(_cache(), qs=-8) == SHAPE
+    assert _decode(_cache(), qs=4100) == SHAPE
+    assert _decode(_cache(), Q=None) == NULL
+    assert _decode(_cache(), O=None) == NULL
+    assert _decode(_cache(), Q=OK + 8) == ALIGN
+    assert _decode(_cache(), O=OK + 2) == ALIGN
+    assert _decode(_cache(), lse=OK + 2) == ALIGN
+
+
+def test_binding_refuses_host_tensors():
+    pool = tm.PagedCache.empty(4, 16, 2, 64, device="cpu")
+    table, lens = torch.zeros(1, 2, dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
+    x = torch.zeros(1, 1, 2, 64, dtype=torch.float16)
+    for call in (lambda: tm.tilemix_paged_append(pool, x, x, table, lens),
+                 lambda: tm.tilemix_paged_gather(pool, table, lens, 1),
+                 lambda: tm.tilemix_paged_decode(pool, x, table, lens)):
+        with pytest.raises(TypeError, match="CUDA"):
+            call()
