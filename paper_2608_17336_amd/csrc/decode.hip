@@ -60,25 +60,6 @@ constexpr int kDecRaggedWaves = 3072;
 constexpr int kDecOneRoundTiles = 14;               // most key tiles per wave of a short chunk
 constexpr int kCombineThreads = 256;
 
-// Eight int8 codes (one per byte of v) widened to FP16, exactly: with the sign bit flipped a
-// byte b reads as 1024 + 128 + b in the FP16 pattern 0x64xx, and 1152 is then subtracted.
-__device__ __forceinline__ half8 i8x8_to_half8(uint32_t w0, uint32_t w1) {
-  const half2v bias = {(_Float16)-1152.0f, (_Float16)-1152.0f};
-  half8 out;
-  const uint32_t w[2] = {w0 ^ 0x80808080u, w1 ^ 0x80808080u};
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    // bytes 0,1 -> halves 0x64b0, 0x64b1; bytes 2,3 -> 0x64b2, 0x64b3
-    const uint32_t p01 = __builtin_amdgcn_perm(0x64646464u, w[i], 0x07010700u);
-    const uint32_t p23 = __builtin_amdgcn_perm(0x64646464u, w[i], 0x07030702u);
-    const half2v h01 = __builtin_bit_cast(half2v, p01) + bias;
-    const half2v h23 = __builtin_bit_cast(half2v, p23) + bias;
-    out[4 * i + 0] = h01[0]; out[4 * i + 1] = h01[1];
-    out[4 * i + 2] = h23[0]; out[4 * i + 3] = h23[1];
-  }
-  return out;
-}
-
 // Key tiles of sequence b of a ragged batch.
 __device__ __forceinline__ int ragged_keys(const DecodeArgs& a, int b) {
   return min(max(a.seqlens[b], 0), a.Lk);
@@ -237,13 +218,6 @@ __global__ __launch_bounds__(kCutThreads) void ragged_cut_kernel(DecodeArgs a) {
     a.cut[1] = base;
     first[a.B] = base;
   }
-}
-
-// Maximum over the four lanes l, l ^ 16, l ^ 32, l ^ 48.
-__device__ __forceinline__ float quad_rows_max(float x) {
-  const int v = __builtin_bit_cast(int, x);
-  const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
-  return pair_max(fmaxf(__builtin_bit_cast(float, (int)r[0]), __builtin_bit_cast(float, (int)r[1])));
 }
 
 // Workgroup = (chunk of chunk_tiles key tiles, KV head, sequence), or with `balanced` a slot and KV

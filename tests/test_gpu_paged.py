@@ -283,18 +283,23 @@ def _poison(pool, fmt, used):
             pool[op + 2].masked_fill_(~used[:, None, :], float("nan"))
 
 
-def _check_decode(name, O, lse, want, dtype, n):
+def _check_decode(name, O, lse, want, dtype, n, v_max=0.0):
     """O: half a step of its type, and FP32 arithmetic: a score is off by at most (d + 8) 2^-24 reach (products and
     sums of d terms, the scale, log2 e) and 2^-22 |s| (the exponent's argument), a weight by twice the largest of these
     relative to the others, the weights' 16-bit pieces by 2^-15 (two pieces of 8 bits) and a sum of n terms by
-    n 2^-24; these act on sum p |v|.  lse: the same without the pieces."""
+    n 2^-24; these act on sum p |v|.  lse: the same without the pieces.
+    v_max: the largest |v|, where weights are held in pieces of FP16 (all caches but BF16).  A weight
+    w = 2^15 p dV / 2^e <= 2^15, with 2^e <= 2 max dV and z >= 1, is split into hi = RN16(w) and
+    lo = RN16(w - hi) (the difference is exact): off by at most 2^-22 w (within 2^-15 above) or half
+    the step of FP16's subnormals, 2^-25.  The n terms of the latter add n 2^-25 2^-15 2^e max |code| <=
+    n 2^-39 v_max to O, whatever the weights: it shows where the heavy tokens' codes are 0."""
     wO, wl, mass, reach = want
     d = wO.shape[-1]
     f = torch.finfo(FORMATS[dtype])
     O, lse = O.double().cpu().numpy().reshape(wO.shape), lse.double().cpu().numpy()
     ds = (d + 8) * 2.0 ** -24 * reach + 2.0 ** -22 * np.maximum(np.where(np.isfinite(wl), np.abs(wl), 0), reach)
     rel = np.exp(2 * ds) - 1 + 2.0 ** -15 + n * 2.0 ** -24
-    tol = f.eps / 2 * np.abs(wO) + f.smallest_normal * f.eps + rel[..., None] * mass * (1 + f.eps)
+    tol = f.eps / 2 * np.abs(wO) + f.smallest_normal * f.eps + (rel[..., None] * mass + n * 2.0 ** -39 * v_max) * (1 + f.eps)
     err = np.abs(O - wO)
     seen = np.isfinite(wl)
     l_tol = ds + n * 2.0 ** -24 + 2.0 ** -22 * (1 + np.abs(np.where(seen, wl, 0)))
@@ -307,6 +312,10 @@ def _check_decode(name, O, lse, want, dtype, n):
     if norm:
         kappa = np.linalg.norm(mass) / norm
         assert np.linalg.norm(O - wO) <= norm * (f.eps / 2 + 2.0 ** -15 * kappa) + np.sqrt(wO.size) * f.smallest_normal * f.eps, name
+
+
+def _v_max(V, fmt):
+    return 0.0 if fmt == "bf16" else float(np.abs(V).max())
 
 
 def _decode_case(fmt, dtype, Hq, Hk, d, page, lens, window=0, seed=0, holes=(), gain=1.0, q_gain=1.0, scale=None, per=None):
@@ -337,7 +346,7 @@ def _decode_case(fmt, dtype, Hq, Hk, d, page, lens, window=0, seed=0, holes=(), 
     torch.cuda.synchronize()
     K, V = (np.where(used.numpy()[:, None, :, None], _values(pool, op, fmt), 0.0) for op in (0, 1))
     want = paged_decode(Q.double().numpy()[:, 0], K, V, lens, table.numpy(), scale, window)
-    _check_decode(name, O, lse, want, dtype, max(lens))
+    _check_decode(name, O, lse, want, dtype, max(lens), _v_max(V, fmt))
     again = tm.tilemix_paged_decode(cache, Q.cuda(), *args, scale, window=window)
     torch.cuda.synchronize()
     assert torch.equal(_bits(again), _bits(O)), "the same call twice"
@@ -413,7 +422,7 @@ def test_decode_values_of_many_magnitudes(fmt, dtype):
         host = [None if t is None else t.cpu() for t in (cache.K, cache.V, cache.dK, cache.dV)]
         want = paged_decode(Q.double().numpy()[:, 0], _values(host, 0, fmt), _values(host, 1, fmt), [L], table.cpu().numpy(),
                             d ** -0.5)
-        _check_decode(f"sink at {sink} {fmt}/{dtype}", O, lse, want, dtype, L)
+        _check_decode(f"sink at {sink} {fmt}/{dtype}", O, lse, want, dtype, L, _v_max(_values(host, 1, fmt), fmt))
 
 
 @pytest.mark.parametrize("fmt", ["int8", "e4m3"])
@@ -435,7 +444,7 @@ def test_decode_bf16_range(fmt):
         host = [t.cpu() for t in (cache.K, cache.V, cache.dK, cache.dV)]
         k, v = (np.nan_to_num(_values(host, op, fmt)) for op in (0, 1))
         want = paged_decode(Q.double().numpy()[:, 0], k, v, [L], table.cpu().numpy(), d ** -0.5)
-        _check_decode(f"range {gk:g} {fmt}", O, lse, want, "bf16", L)
+        _check_decode(f"range {gk:g} {fmt}", O, lse, want, "bf16", L, _v_max(v, fmt))
 
 
 @pytest.mark.parametrize("fmt,dtype", PAIRS)
@@ -554,7 +563,7 @@ def test_prefill_append_decode_and_chunked_prefill(fmt):
     K, V = (np.nan_to_num(_values(host, op, fmt)) for op in (0, 1))
     for i, (O, lse) in enumerate(outs):
         want = paged_decode(q[:, L + i].double().cpu().numpy(), K, V, [L + i + 1], table.cpu().numpy(), d ** -0.5)
-        _check_decode(f"step {i} {fmt}", O, lse, want, "fp16", L + i + 1)
+        _check_decode(f"step {i} {fmt}", O, lse, want, "fp16", L + i + 1, _v_max(V, fmt))
     for r in (0, 1, turn - 1):   # a row of the chunk is a decode step of its prefix; that call's own bar
         want = paged_decode(q[:, L + steps + r].double().cpu().numpy(), K, V, [L + steps + r + 1], table.cpu().numpy(), d ** -0.5)[0]
         err = chunk[r].double().cpu().numpy() - want[0]
