@@ -114,22 +114,22 @@ tilemix_status check_decode(const tilemix_paged_cache* c, int32_t heads_q) {
   if (st != TILEMIX_OK) return st;
   if (heads_q < 1 || heads_q > 65535 || heads_q % c->heads_kv != 0)
     return fail(TILEMIX_ERR_SHAPE, "heads_q (%d) must be a multiple of heads_kv (%d), at most 65535", heads_q, c->heads_kv);
-  if (tilemix::plan_paged_decode(pool_of(c), heads_q, c->format).tiles > 0x7fffffffLL)
+  if (tilemix::plan_paged_decode(pool_of(c), heads_q, c->head_dim, c->format).tiles > 0x7fffffffLL)
     return fail(TILEMIX_ERR_SHAPE, "batch * heads * max_pages * page_size is too large");
   return TILEMIX_OK;
 }
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// Workspace: [segments][part_mze][part_o], each 256-byte aligned.
+// Workspace: [segments][part_rz][part_o], each 256-byte aligned.
 struct DecodeBytes {
-  size_t segments, mze, o;
-  size_t total() const { return segments + mze + o; }
+  size_t segments, rz, o;
+  size_t total() const { return segments + rz + o; }
 };
 DecodeBytes decode_bytes(const tilemix_paged_cache* c, const tilemix::PagedDecodePlan& pl) {
   if (!pl.join) return {0, 0, 0};
-  const size_t rows = (size_t)pl.workgroups * pl.part_heads;
-  return {align256((size_t)c->batch * pl.head_blocks * 2 * sizeof(int)), align256(rows * 3 * sizeof(float)),
+  const size_t rows = 2 * (size_t)pl.workgroups * pl.part_heads;
+  return {align256((size_t)c->batch * pl.head_blocks * 2 * sizeof(int)), align256(rows * 2 * sizeof(float)),
           align256(rows * c->head_dim * sizeof(float))};
 }
 
@@ -167,7 +167,7 @@ tilemix_status tilemix_paged_decode_workspace_size(const tilemix_paged_cache* ca
   const tilemix_status st = check_decode(cache, heads_q);
   if (st != TILEMIX_OK) return st;
   if (!bytes) return fail(TILEMIX_ERR_NULL, "bytes is NULL");
-  *bytes = decode_bytes(cache, tilemix::plan_paged_decode(pool_of(cache), heads_q, cache->format)).total();
+  *bytes = decode_bytes(cache, tilemix::plan_paged_decode(pool_of(cache), heads_q, cache->head_dim, cache->format)).total();
   return ok();
 }
 
@@ -186,7 +186,7 @@ tilemix_status tilemix_paged_decode(const tilemix_paged_cache* cache, int32_t ty
     return fail(TILEMIX_ERR_ALIGN, "Q and O must be 16-byte and lse 4-byte aligned");
   tilemix::PagedDecodeArgs a{};
   a.pool = pool_of(cache);
-  const tilemix::PagedDecodePlan pl = tilemix::plan_paged_decode(a.pool, heads_q, cache->format);
+  const tilemix::PagedDecodePlan pl = tilemix::plan_paged_decode(a.pool, heads_q, cache->head_dim, cache->format);
   const DecodeBytes need = decode_bytes(cache, pl);
   if (need.total()) {
     if (!workspace) return fail(TILEMIX_ERR_WORKSPACE, "workspace is NULL");
@@ -195,12 +195,11 @@ tilemix_status tilemix_paged_decode(const tilemix_paged_cache* cache, int32_t ty
       return fail(TILEMIX_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need.total());
     char* ws = static_cast<char*>(workspace);
     a.segments = reinterpret_cast<int*>(ws);
-    a.part_mze = reinterpret_cast<float*>(ws + need.segments);
-    a.part_o = reinterpret_cast<float*>(ws + need.segments + need.mze);
+    a.part_rz = reinterpret_cast<float*>(ws + need.segments);
+    a.part_o = reinterpret_cast<float*>(ws + need.segments + need.rz);
   }
   a.head_blocks = pl.head_blocks;
   a.part_heads = pl.part_heads;
-  a.chunk_workgroups = pl.chunk_workgroups;
   a.Q = Q; a.O = O; a.lse = lse; a.q_stride = q_stride;
   a.Hq = heads_q; a.window = window;
   a.scale_log2e = scale * 1.4426950408889634f;

@@ -3,11 +3,12 @@
 // For query head hq of sequence b, over the tokens j attended to (the last `window`, or all, whose page
 // exists): s_j = scale q . k_j, O = sum_j e^(s_j - m) v_j / sum_j e^(s_j - m), lse = m + ln of that sum.
 //
-//   paged_decode_kernel: workgroup (chunk of tiles, KV head and block of 16 query heads, sequence), 4 waves.
-//     Each wave streams tiles of the chunk with a running (max, normalizer, output) of its own in
-//     registers; they are joined in LDS, and the workgroup writes O, or the chunk's partial result
-//     where the sequence has several chunks.
-//   paged_join_kernel: joins the chunks of one (sequence, query head) by their log-sum-exp.
+//   paged_decode_kernel: as many workgroups of 4 waves as run at once share the tiles of the batch equally, each
+//     a run of consecutive ones, whatever sequences and heads they belong to.  In each (sequence, head block) of
+//     its run a workgroup's waves stream tiles with a running (max, normalizer, output) of their own in
+//     registers; they are joined in LDS, and the workgroup writes O, or a partial result where others
+//     have tiles of the same sequence and heads.
+//   paged_join_kernel: joins the partial results of one (sequence, query head) by their log-sum-exp.
 //
 // Bound: HBM.  Each cached row is read once per block of 16 query heads, with O(1) work per byte.
 #include "paged_device.h"
@@ -19,68 +20,64 @@ namespace tilemix {
 namespace {
 
 constexpr int kPagedWaves = 4;
+constexpr int kCUs = 256;
 constexpr int kPagedHeads = 16;                  // query heads on the columns of a matrix-core tile
-// Workgroups that share the tiles of a batch.
-constexpr int kPagedWorkgroups = 768;
-
 // 16-key slabs per tile: a tile is 16 KiB of K and V for d = 128, 8 KiB for d = 64.
 template <int FORMAT>
 constexpr int kSlabs = is_8bit(FORMAT) ? 4 : 2;
 
-int tile_keys(int format) { return 16 * (format == TILEMIX_INT8 || format == TILEMIX_E4M3 ? 4 : 2); }
+// Waves that a SIMD holds, by their registers (K and V rows of a tile, the output): workgroups per CU.
+constexpr int resident_per_cu(int d, int format) { return (d == 64 ? 4 : 3) - (is_8bit(format) ? 1 : 0); }
+
+int tile_keys(int format) { return 16 * (is_8bit(format) ? 4 : 2); }
 
 // The tokens that a sequence's query attends to, as tiles of `keys` tokens: first .. len - 1, of tiles
 // first / keys .. .
 struct Span {
   int first, len, tile0, tiles;
-  __device__ __forceinline__ Span(const PagedDecodeArgs& a, int b, int keys) {
+  __device__ __forceinline__ Span(const PagedDecodeArgs& a, int keys, int tokens) {
     const PagedPool& p = a.pool;
-    len = min(max(p.seqlens[b], 0), p.max_pages << p.page_shift);
+    len = min(max(tokens, 0), p.max_pages << p.page_shift);
     first = a.window > 0 ? max(len - a.window, 0) : 0;
     tile0 = first / keys;
     tiles = (len + keys - 1) / keys - tile0;
   }
 };
 
-// How the batch is cut: every sequence into chunks of `tiles` tiles (the last one maybe fewer; one empty
-// chunk where it has no token), the fewest tiles, the same number for every wave, with which the chunks of
-// all heads fit the workgroups.  Found by every wave for itself: a lane takes a run of sequences.
-struct Chunk {
-  int b = -1, index, count, tiles;   // b = -1: no chunk for this workgroup
-  int head_block;                    // KV head and block of query heads
-  int first_id;                      // workgroup of the sequence's and head block's chunk 0
-  __device__ __forceinline__ Chunk(const PagedDecodeArgs& a, int id, int lane, int keys) {
-    const int B = a.pool.B, per = (B + kWave - 1) / kWave, b0 = lane * per, b1 = min(b0 + per, B);
-    int sum = 0;
-    for (int s = b0; s < b1; ++s) sum += Span(a, s, keys).tiles;
-    const int total = __builtin_amdgcn_readlane(wave_scan(sum), kWave - 1);
-    const int share = a.chunk_workgroups * kPagedWaves;
-    tiles = kPagedWaves * max(1, (int)(((long long)total * a.head_blocks + share - 1) / share));
+// How the batch is cut.  A unit is kPagedWaves tiles of one sequence and head block, one per wave; a sequence has
+// one at least, so that one without tokens is written, too.  Units are numbered by sequence, then head block, then
+// token; workgroup w takes units [w quota, (w + 1) quota).  Every wave finds its place for itself: a lane
+// takes a run of sequences.
+struct Run {
+  int b = -1, head_block, unit;   // first unit: in its sequence and head block; b = -1: no unit is left
+  int quota;
+  __device__ __forceinline__ static int units(const Span& s) { return max(1, (s.tiles + kPagedWaves - 1) / kPagedWaves); }
+  __device__ __forceinline__ Run(const PagedDecodeArgs& a, int w, int lane, int keys) {
+    const int B = a.pool.B, per = (B + kWave - 1) / kWave, b0 = min(lane * per, B), b1 = min(b0 + per, B);
     int mine = 0;
-    for (int s = b0; s < b1; ++s) mine += max(1, (Span(a, s, keys).tiles + tiles - 1) / tiles);
-    const int end = wave_scan(mine), all = __builtin_amdgcn_readlane(end, kWave - 1);
-    head_block = id / all;
-    if (head_block >= a.head_blocks) return;
-    const int slot = id - head_block * all;
-    int at = end - mine, seq = 0, idx = 0, cnt = 0;
-    const bool hit = slot >= at && slot < end;
+    for (int s = b0; s < b1; ++s) mine += units(Span(a, keys, a.pool.seqlens[s]));
+    const int end = wave_scan(mine), all = __builtin_amdgcn_readlane(end, kWave - 1) * a.head_blocks;
+    quota = (all + (int)gridDim.x - 1) / (int)gridDim.x;
+    if ((long long)w * quota >= all) return;
+    const int u = w * quota;
+    int at = (end - mine) * a.head_blocks, seq = 0, hb = 0, in = 0;
+    const bool hit = u >= at && u < end * a.head_blocks;
     if (hit) {
       for (int s = b0; s < b1; ++s) {
-        const int n = max(1, (Span(a, s, keys).tiles + tiles - 1) / tiles);
-        if (slot < at + n) {
+        const int n = units(Span(a, keys, a.pool.seqlens[s])), next = at + n * a.head_blocks;
+        if (u < next) {
           seq = s;
-          idx = slot - at;
-          cnt = n;
+          hb = (u - at) / n;
+          in = (u - at) - hb * n;
           break;
         }
-        at += n;
+        at = next;
       }
     }
     const int l = __builtin_ctzll(__ballot(hit));
     b = __builtin_amdgcn_readlane(seq, l);
-    index = __builtin_amdgcn_readlane(idx, l);
-    count = __builtin_amdgcn_readlane(cnt, l);
-    first_id = id - index;
+    head_block = __builtin_amdgcn_readlane(hb, l);
+    unit = __builtin_amdgcn_readlane(in, l);
   }
 };
 
@@ -118,24 +115,28 @@ __device__ __forceinline__ float quad_rows_sum(float x) {
   return pair_sum(__builtin_bit_cast(float, (int)r[0]) + __builtin_bit_cast(float, (int)r[1]));
 }
 
-// Weights are formed as 2^(s - m + kShift) so that their FP16 pieces reach far below the largest:
-// two pieces hold a weight to 2^-22 of itself down to 2^-29 of the largest and to 2^-40 of it below.  BF16
-// pieces have FP32's range.
+// Weights p = 2^(s - r) are taken against a reference r near the running max m: r = m for a BF16 cache, m - 15 for
+// an FP16 one, and m - 15 + e for an 8-bit one, where 2^e is above every value scale dV so far.  The
+// weights of the codes, p dV (p for 16 bits), then stay below 2^15, and are handed to the matrix cores as
+// two 16-bit pieces: FP16 pieces hold them to 2^-22 of themselves, and to 2^-40 of the largest possible
+// weight where they are small; BF16 pieces to 2^-16, with FP32's range.  One piece alone (2^-12 or
+// 2^-9) would add as much error as the output's own rounding.  e >= kExpMin keeps the normalizer, a sum
+// of up to 2^30 terms p <= 2^(15 - e), finite.
+constexpr int kExpMin = -80;
 template <int FORMAT>
-constexpr float kShift = FORMAT == TILEMIX_BF16 ? 0.0f : 15.0f;
+constexpr float kHeadroom = FORMAT == TILEMIX_BF16 ? 0.0f : 15.0f;
 
-// Two 16-bit pieces of four weights.
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+// Two 16-bit pieces of two weights.
 template <int FORMAT>
-__device__ __forceinline__ void split4(const float (&w)[4], uint2& hi, uint2& lo) {
-  constexpr int kMath = FORMAT == TILEMIX_BF16 ? TILEMIX_BF16 : TILEMIX_FP16;
-  uint32_t h[4], l[4];
-#pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    h[r] = float_to_bits<kMath>(w[r]);
-    l[r] = float_to_bits<kMath>(w[r] - bits_to_float<kMath>(h[r]));
-  }
-  hi = make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
-  lo = make_uint2(l[0] | l[1] << 16, l[2] | l[3] << 16);
+__device__ __forceinline__ void split2(float w0, float w1, uint32_t& hi, uint32_t& lo) {
+  using V = std::conditional_t<FORMAT == TILEMIX_BF16, bf16x2, half2_t>;
+  const V h = __builtin_convertvector((f32x2{w0, w1}), V);
+  const V l = __builtin_convertvector((f32x2{w0 - (float)h[0], w1 - (float)h[1]}), V);
+  hi = __builtin_bit_cast(uint32_t, h);
+  lo = __builtin_bit_cast(uint32_t, l);
 }
 
 // Scores are computed transposed, S^T = K Q^T: a slab's 16 keys on the rows, the query heads on the columns
@@ -146,7 +147,7 @@ __device__ __forceinline__ void split4(const float (&w)[4], uint2& hi, uint2& lo
 // adjacent channels of a key at once and pairs the keys by byte permutes: no transposed copy of V is
 // kept, and a row can be appended to a page as it is.
 template <int D, int TYPE, int FORMAT>
-__global__ __launch_bounds__(kPagedWaves * kWave) __attribute__((amdgpu_waves_per_eu(2)))
+__global__ __launch_bounds__(kPagedWaves * kWave) __attribute__((amdgpu_waves_per_eu(resident_per_cu(D, FORMAT))))
 void paged_decode_kernel(PagedDecodeArgs a) {
   constexpr int kS = kSlabs<FORMAT>, kKeys = 16 * kS;
   constexpr int kBytes = kElemBytes<FORMAT>;
@@ -161,18 +162,23 @@ void paged_decode_kernel(PagedDecodeArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int l16 = lane & 15, lq = lane >> 4;
   const float ninf = -__builtin_huge_valf();
-  const Chunk ch(a, blockIdx.x, lane, kKeys);
-  if (ch.b < 0) return;
-  const int b = ch.b, G = a.Hq / p.Hk, blocks = a.head_blocks / p.Hk;
-  const int hk = ch.head_block / blocks, g0 = ch.head_block % blocks * kPagedHeads;
-  const int heads = min(kPagedHeads, G - g0), hq0 = hk * G + g0;
-  const Span span(a, b, kKeys);
-  const int tile0 = span.tile0 + ch.index * ch.tiles;
-  const int tile_end = min(tile0 + ch.tiles, span.tile0 + span.tiles);
-
   __shared__ float red_m[kPagedWaves][kPagedHeads], red_z[kPagedWaves][kPagedHeads];
-  __shared__ int red_e[kPagedWaves];
   __shared__ __align__(16) float osum[kPagedWaves][kPagedHeads][kOS];
+
+  const Run run(a, blockIdx.x, lane, kKeys);
+  const int quota = __builtin_amdgcn_readfirstlane(run.quota);
+  int b = __builtin_amdgcn_readfirstlane(run.b), head_block = __builtin_amdgcn_readfirstlane(run.head_block);
+  int unit = __builtin_amdgcn_readfirstlane(run.unit);
+  int left = b < 0 ? 0 : quota;   // units
+  while (left > 0 && b < p.B) {
+  const int G = a.Hq / p.Hk, blocks = a.head_blocks / p.Hk;
+  const int hk = head_block / blocks, g0 = head_block % blocks * kPagedHeads;
+  const int heads = min(kPagedHeads, G - g0), hq0 = hk * G + g0;
+  // (The load's result is the same in every lane, which only a scalar register tells the compiler.)
+  const Span span(a, kKeys, __builtin_amdgcn_readfirstlane(p.seqlens[b]));
+  const int units = Run::units(span), take = min(left, units - unit);
+  const int tile0 = span.tile0 + unit * kPagedWaves;
+  const int tile_end = span.tile0 + min(span.tiles, (unit + take) * kPagedWaves);
 
   // 1. Page ids of the wave's tiles tile0 + wave + i kPagedWaves, 64 at a time: lane (i, j) holds the j-th of
   //    the 2^per_shift pages of tile i.
@@ -181,7 +187,7 @@ void paged_decode_kernel(PagedDecodeArgs a) {
   const int* table = p.table + b * p.stride_table;
   auto load_ids = [&](int i0) {
     const int i = i0 + (lane >> per_shift), n = tile0 + wave + i * kPagedWaves;
-    const long long e = ((long long)n * kKeys >> p.page_shift) + (lane & ((1 << per_shift) - 1));
+    const int e = (n * kKeys >> p.page_shift) + (lane & ((1 << per_shift) - 1));
     int id = -1;
     if (n < tile_end && e < p.max_pages && (e << p.page_shift) < span.len) id = table[e];
     return id >= 0 && id < p.pages ? id : -1;
@@ -189,31 +195,43 @@ void paged_decode_kernel(PagedDecodeArgs a) {
   int ids = load_ids(0);
   const int id_tiles = kWave >> per_shift;
 
-  // 2. One tile in registers.
+  // 2. One tile in registers.  Behind its last tile a wave requests one all the same (see 4.), a few cache lines
+  //    of page 0: every lane's offset is 0.
   uint4 kr[kS][kKL];
   uint32_t vr[kS][4][kVW];
   f32x4 dk[kS], dv[kS];
-  int page[kS];                                    // of the tile that is requested next, per slab
+  int page[kS];                                    // per slab, of the tile that was requested last
   const char* poolK = static_cast<const char*>(p.K);
   const char* poolV = static_cast<const char*>(p.V);
-  const uint32_t k_off = (uint32_t)(l16 * D * kBytes + 16 * lq);
-  const uint32_t v_off = (uint32_t)(4 * lq * D * kBytes + l16 * kC * kBytes);
+  const uint32_t k_lane = l16 * D * kBytes + 16 * lq, v_lane = 4 * lq * D * kBytes + l16 * kC * kBytes;
   auto find_pages = [&](int i) {
     const int at = (i & (id_tiles - 1)) << per_shift;
 #pragma unroll
     for (int s = 0; s < kS; ++s) page[s] = __builtin_amdgcn_readlane(ids, at + (16 * s >> p.page_shift));
   };
-  // Rows of slab s of tile n in page `id`, or of page 0 where there is none: they are masked.
+  // Row of slab s of tile n in its page, or in page 0 where there is none: it is masked.
   auto slab_row = [&](int n, int s) { return (hk << p.page_shift) + ((n * kKeys + 16 * s) & ((1 << p.page_shift) - 1)); };
   auto load_keys = [&](int n) {
+    const uint32_t k_off = n < tile_end ? k_lane : 0u, s_off = n < tile_end ? 16u * lq : 0u;
 #pragma unroll
     for (int s = 0; s < kS; ++s) {
       const char* base = poolK + kBytes * (max(page[s], 0) * p.stride_k + (long long)slab_row(n, s) * D);
 #pragma unroll
       for (int i = 0; i < kKL; ++i) kr[s][i] = ld_global_16(base + 64 * i + k_off);
     }
+    if constexpr (k8) {
+#pragma unroll
+      for (int s = 0; s < kS; ++s)
+        dk[s] = *reinterpret_cast<const f32x4*>(reinterpret_cast<const char*>(p.dK + max(page[s], 0) * p.stride_dk + slab_row(n, s)) + s_off);
+    }
   };
   auto load_values = [&](int n) {
+    const uint32_t v_off = n < tile_end ? v_lane : 0u, s_off = n < tile_end ? 16u * lq : 0u;
+    if constexpr (k8) {
+#pragma unroll
+      for (int s = 0; s < kS; ++s)
+        dv[s] = *reinterpret_cast<const f32x4*>(reinterpret_cast<const char*>(p.dV + max(page[s], 0) * p.stride_dv + slab_row(n, s)) + s_off);
+    }
 #pragma unroll
     for (int s = 0; s < kS; ++s) {
       const char* base = poolV + kBytes * (max(page[s], 0) * p.stride_v + (long long)slab_row(n, s) * D);
@@ -232,30 +250,22 @@ void paged_decode_kernel(PagedDecodeArgs a) {
       }
     }
   };
-  auto load_scales = [&](int n) {
-    if constexpr (k8) {
-#pragma unroll
-      for (int s = 0; s < kS; ++s) {
-        const int row = slab_row(n, s) + 4 * lq;
-        dk[s] = *reinterpret_cast<const f32x4*>(p.dK + max(page[s], 0) * p.stride_dk + row);
-        dv[s] = *reinterpret_cast<const f32x4*>(p.dV + max(page[s], 0) * p.stride_dv + row);
-      }
-    }
-  };
 
   // 3. Query rows as the B operand of the score products: lane (head l16, lq) holds the channels that it
   //    reads of a key row.  BF16 queries against 8-bit codes are brought to FP16 by a power of two per
   //    head, 2^q_exp: the largest to [2^14, 2^15), so that what FP16 cannot hold lies below 2^-39 of it.
   uint4 qf[kQ];
-  int q_exp = 0;
+  float f_head = a.scale_log2e;   // score of a product, in log2 units, before the key's scale
   {
     const char* q = static_cast<const char*>(a.Q) + 2 * (b * a.q_stride + (long long)(hq0 + min(l16, heads - 1)) * D);
 #pragma unroll
     for (int i = 0; i < kQ; ++i) {
       const int c = k8 ? 64 * (i / 2) + 16 * lq + 8 * (i % 2) : 32 * i + 8 * lq;
       qf[i] = ld_global_16(q + 2 * c);
-      if (l16 >= heads) qf[i] = make_uint4(0, 0, 0, 0);
     }
+    const uint32_t some = l16 < heads ? ~0u : 0u;
+#pragma unroll
+    for (int i = 0; i < kQ; ++i) qf[i] = make_uint4(qf[i].x & some, qf[i].y & some, qf[i].z & some, qf[i].w & some);
     if constexpr (k8 && TYPE == TILEMIX_BF16) {
       float x[kQ][8], amax = 0.0f;
 #pragma unroll
@@ -267,7 +277,8 @@ void paged_decode_kernel(PagedDecodeArgs a) {
           amax = fmaxf(amax, fabsf(x[i][e]));
         }
       }
-      q_exp = 15 - __builtin_amdgcn_frexp_expf(quad_rows_max(amax));
+      const int q_exp = 15 - __builtin_amdgcn_frexp_expf(quad_rows_max(amax));
+      f_head = __builtin_amdgcn_ldexpf(f_head, -q_exp);
 #pragma unroll
       for (int i = 0; i < kQ; ++i) {
         uint32_t w[8];
@@ -278,31 +289,30 @@ void paged_decode_kernel(PagedDecodeArgs a) {
     }
   }
 
-  // 4. The wave's tiles.  m, z: running max (log2 units) and this lane's share of the normalizer; acc: output in
-  //    units of 2^e.  e follows the largest value scale so far, so that p dV, the weight of a code, fits
-  //    FP16 pieces whatever the values' size.
-  float m = ninf, z = 0.0f;
-  int e = -2048;
+  // 4. The wave's tiles.  m: running max (log2 units); ref: the reference r; z: this lane's share of the normalizer;
+  //    acc: output.  Loads complete in order, and a wait counts the younger ones, so rows are requested in the
+  //    same order and number on every way to a wait: the keys and their scales once the scores are
+  //    formed, the values and theirs after P V, into the registers that these leave, also after the
+  //    last tile.
+  float m = ninf, ref = ninf, z = 0.0f;
+  int e = kExpMin;
   f32x4 acc[kC];
 #pragma unroll
   for (int c = 0; c < kC; ++c) acc[c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   int i = 0, n = tile0 + wave;
-  if (n < tile_end) {
-    find_pages(0);
-    load_keys(n);
-    load_scales(n);
-    load_values(n);
-  }
+  find_pages(0);
+  __builtin_amdgcn_sched_barrier(0);
+  load_keys(n);
+  __builtin_amdgcn_sched_barrier(0);
+  load_values(n);
+  __builtin_amdgcn_sched_barrier(0);
   while (n < tile_end) {
-    const int next = n + kPagedWaves;
     // Which of the tile's keys count, where it is not all of them.
     bool all = n * kKeys >= span.first && (n + 1) * kKeys <= span.len;
-    bool has[kS];
+    uint32_t has = 0;
 #pragma unroll
-    for (int s = 0; s < kS; ++s) {
-      has[s] = page[s] >= 0;
-      all = all && has[s];
-    }
+    for (int s = 0; s < kS; ++s) has |= page[s] >= 0 ? 1u << s : 0u;
+    all = all && has == (1u << kS) - 1;
     float sc[kS][4];
 #pragma unroll
     for (int s = 0; s < kS; ++s) {
@@ -316,28 +326,24 @@ void paged_decode_kernel(PagedDecodeArgs a) {
           c = mfma_16<FORMAT>(kr[s][k], qf[k], c);
         }
       }
+      // Scores are scaled and rounded before the max and the exponent see them.
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        float f = a.scale_log2e;
-        if constexpr (k8) f *= dk[s][r];
-        if constexpr (k8 && TYPE == TILEMIX_BF16) f = __builtin_amdgcn_ldexpf(f, -q_exp);
-        sc[s][r] = c[r] * f;
-      }
+      for (int r = 0; r < 4; ++r) sc[s][r] = c[r] * (k8 ? f_head * dk[s][r] : f_head);
     }
-    f32x4 dvc[kS];
-    if constexpr (k8) {
-#pragma unroll
-      for (int s = 0; s < kS; ++s) dvc[s] = dv[s];
-    }
+    __builtin_amdgcn_sched_barrier(0);
+    ++i;
+    if ((i & (id_tiles - 1)) == 0) ids = load_ids(i);
+    find_pages(i);
+    load_keys(n + kPagedWaves);
     if (!all) {
 #pragma unroll
       for (int s = 0; s < kS; ++s)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int t = n * kKeys + 16 * s + 4 * lq + r;
-          const bool ok = has[s] && t >= span.first && t < span.len;
+          const bool ok = (has >> s & 1) && t >= span.first && t < span.len;
           sc[s][r] = ok ? sc[s][r] : ninf;
-          if constexpr (k8) dvc[s][r] = ok ? dvc[s][r] : 0.0f;
+          if constexpr (k8) dv[s][r] = ok ? dv[s][r] : 0.0f;
           // What a slot behind the sequence holds may be a NaN, which a weight of 0 does not cancel.
           if constexpr (FORMAT != TILEMIX_INT8) {
 #pragma unroll
@@ -345,14 +351,7 @@ void paged_decode_kernel(PagedDecodeArgs a) {
           }
         }
     }
-    // The next tile: its page ids, and its key rows into the registers of this one's.
-    if (next < tile_end) {
-      ++i;
-      if ((i & (id_tiles - 1)) == 0) ids = load_ids(i);
-      find_pages(i);
-      load_keys(next);
-    }
-    // Softmax: the running max, normalizer and output move when the max or the values' exponent grows.
+    // Softmax: reference, normalizer and output move when the max or the value scales' exponent grows.
     float mt = sc[0][0];
 #pragma unroll
     for (int s = 0; s < kS; ++s)
@@ -365,31 +364,34 @@ void paged_decode_kernel(PagedDecodeArgs a) {
 #pragma unroll
       for (int s = 0; s < kS; ++s)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) vm = fmaxf(vm, fabsf(dvc[s][r]));
+        for (int r = 0; r < 4; ++r) vm = fmaxf(vm, fabsf(dv[s][r]));
       vm = quad_rows_max(vm);
       if (vm > 0.0f) e_new = max(e, __builtin_amdgcn_frexp_expf(vm));
     }
     if (__any(m_new > m || e_new > e)) {
-      const float alpha = m == ninf ? 0.0f : __builtin_amdgcn_exp2f(m - m_new);
+      // No finite score so far: p = 2^(-inf - 0) = 0, not a NaN.
+      const float next = m_new == ninf ? ninf : m_new - (k8 ? kHeadroom<FORMAT> - (float)e_new : kHeadroom<FORMAT>);
+      const float alpha = ref == ninf ? 0.0f : __builtin_amdgcn_exp2f(ref - next);
       z *= alpha;
-      const float beta = k8 ? __builtin_amdgcn_ldexpf(alpha, e - e_new) : alpha;
 #pragma unroll
-      for (int c = 0; c < kC; ++c) acc[c] *= beta;
+      for (int c = 0; c < kC; ++c) acc[c] *= alpha;
       m = m_new;
       e = e_new;
+      ref = next;
     }
-    const float msub = m == ninf ? 0.0f : m - kShift<FORMAT>;
+    const float sub = ref == ninf ? 0.0f : ref;
     uint2 hi[kS], lo[kS];
 #pragma unroll
     for (int s = 0; s < kS; ++s) {
       float w[4];
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const float pr = __builtin_amdgcn_exp2f(sc[s][r] - msub);
-        z += pr;
-        w[r] = k8 ? pr * __builtin_amdgcn_ldexpf(dvc[s][r], -e) : pr;
+        w[r] = __builtin_amdgcn_exp2f(sc[s][r] - sub);
+        z += w[r];
+        if constexpr (k8) w[r] *= dv[s][r];
       }
-      split4<FORMAT>(w, hi[s], lo[s]);
+      split2<FORMAT>(w[0], w[1], hi[s].x, lo[s].x);
+      split2<FORMAT>(w[2], w[3], hi[s].y, lo[s].y);
     }
     // O^T += V^T P^T.
 #pragma unroll
@@ -398,7 +400,7 @@ void paged_decode_kernel(PagedDecodeArgs a) {
       const uint4 pl = make_uint4(lo[2 * t].x, lo[2 * t].y, lo[2 * t + 1].x, lo[2 * t + 1].y);
 #pragma unroll
       for (int c2 = 0; c2 < kC / 2; ++c2) {
-        // Channels 2 c2 and 2 c2 + 1 of the lane, in FP16 or BF16, of its 8 keys.
+        // Channels 2 c2 and 2 c2 + 1 of the lane, in FP16 or BF16 (or as codes), of its 8 keys.
         uint32_t x[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -429,34 +431,29 @@ void paged_decode_kernel(PagedDecodeArgs a) {
         }
       }
     }
-    if (next < tile_end) {
-      load_scales(next);
-      load_values(next);
-    }
-    n = next;
+    __builtin_amdgcn_sched_barrier(0);   // not ahead of P V: their registers are in use
+    load_values(n + kPagedWaves);
+    n += kPagedWaves;
   }
 
   // 5. The waves' results joined in LDS.
   z = quad_rows_sum(z);
-  if (lq == 0) red_m[wave][l16] = m;
-  if (lane == 0) red_e[wave] = e;
+  if (lq == 0) red_m[wave][l16] = ref;
   __syncthreads();
-  float mc = red_m[0][l16];
-  int ec = red_e[0];
+  float top = red_m[0][l16];
 #pragma unroll
-  for (int w = 1; w < kPagedWaves; ++w) {
-    mc = fmaxf(mc, red_m[w][l16]);
-    ec = max(ec, red_e[w]);
-  }
-  const float fw = m == ninf ? 0.0f : __builtin_amdgcn_exp2f(m - mc);
+  for (int w = 1; w < kPagedWaves; ++w) top = fmaxf(top, red_m[w][l16]);
+  const float fw = ref == ninf ? 0.0f : __builtin_amdgcn_exp2f(ref - top);
   if (lq == 0) red_z[wave][l16] = z * fw;
-  const float fo = k8 ? __builtin_amdgcn_ldexpf(fw, e - ec) : fw;
 #pragma unroll
   for (int r = 0; r < 4; ++r)
 #pragma unroll
-    for (int c = 0; c < kC; ++c) osum[wave][l16][(4 * lq + r) * kC + c] = m == ninf ? 0.0f : acc[c][r] * fo;
+    for (int c = 0; c < kC; ++c) osum[wave][l16][(4 * lq + r) * kC + c] = ref == ninf ? 0.0f : acc[c][r] * fw;
   __syncthreads();
-  const bool whole = ch.count == 1;
+  const bool whole = take == units;
+  // Partial results: of the workgroup's first units in row 2 w, of units behind others in row 2 w + 1 (they
+  // are its last).
+  const size_t part_row = ((size_t)blockIdx.x * 2 + (left != quota ? 1 : 0)) * a.part_heads;
   for (int o = tid; o < heads * D; o += kPagedWaves * kWave) {
     const int g = o / D, c = o % D;
     float sum = 0.0f, zz = 0.0f;
@@ -466,10 +463,10 @@ void paged_decode_kernel(PagedDecodeArgs a) {
       zz += red_z[w][g];
     }
     if (whole) {
-      const float x = zz == 0.0f ? 0.0f : k8 ? __builtin_amdgcn_ldexpf(sum / zz, ec) : sum / zz;
-      static_cast<uint16_t*>(a.O)[((long long)b * a.Hq + hq0 + g) * D + c] = (uint16_t)float_to_bits<TYPE>(x);
+      static_cast<uint16_t*>(a.O)[((long long)b * a.Hq + hq0 + g) * D + c] =
+          (uint16_t)float_to_bits<TYPE>(zz == 0.0f ? 0.0f : sum / zz);
     } else {
-      a.part_o[((size_t)blockIdx.x * a.part_heads + g) * D + c] = sum;
+      a.part_o[(part_row + g) * D + c] = sum;
     }
   }
   if (tid < heads) {
@@ -482,113 +479,104 @@ void paged_decode_kernel(PagedDecodeArgs a) {
     if (whole) {
       if (a.lse)
         a.lse[(long long)b * a.Hq + hq0 + tid] =
-            zz == 0.0f ? ninf : 0.69314718056f * (mm - kShift<FORMAT> + __builtin_amdgcn_logf(zz));
+            zz == 0.0f ? ninf : 0.69314718056f * (mm + __builtin_amdgcn_logf(zz));
     } else {
-      float* part = a.part_mze + ((size_t)blockIdx.x * a.part_heads + tid) * 3;
-      part[0] = mm;
-      part[1] = zz;
-      part[2] = __builtin_bit_cast(float, ec);
+      reinterpret_cast<float2*>(a.part_rz)[part_row + tid] = make_float2(mm, zz);
     }
   }
-  // Where the sequence's chunks are, for the join.
-  if (a.segments && tid == 0 && ch.index == 0)
-    reinterpret_cast<int2*>(a.segments)[(size_t)b * a.head_blocks + ch.head_block] = make_int2(ch.first_id, ch.count);
+  // For the join: the first row, and how many workgroups there are from this one on.
+  if (a.segments && tid == 0 && unit == 0) {
+    const int beyond = units - take;   // units of the workgroups that follow
+    reinterpret_cast<int2*>(a.segments)[(size_t)b * a.head_blocks + head_block] =
+        make_int2((int)blockIdx.x * 2 + (left != quota ? 1 : 0), 1 + (beyond + quota - 1) / quota);
+  }
+  left -= take;
+  unit = 0;
+  if (++head_block == a.head_blocks) {
+    head_block = 0;
+    ++b;
+  }
+  if (left > 0) __syncthreads();   // the LDS is used again
+  }
 }
 
-// One workgroup per (query head, sequence): thread (part, channel quad) joins every kParts-th chunk.
-constexpr int kJoinThreads = 256;
-template <int D, int TYPE, int FORMAT>
+// One workgroup per (query head, sequence, 32 channels): thread (part, channel quad) joins every kParts-th row.
+constexpr int kJoinThreads = 256, kJoinChannels = 32;
+template <int D, int TYPE>
 __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedDecodeArgs a) {
-  constexpr int kLanes = D / 4, kParts = kJoinThreads / kLanes, kWaves = kJoinThreads / kWave;
+  constexpr int kLanes = kJoinChannels / 4, kParts = kJoinThreads / kLanes, kWaves = kJoinThreads / kWave;
   constexpr int kAhead = 4;
   const int hq = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, wave = tid / kWave;
   const int G = a.Hq / a.pool.Hk, blocks = a.head_blocks / a.pool.Hk, hk = hq / G, g = hq % G;
   const int2 seg = reinterpret_cast<const int2*>(a.segments)[(size_t)b * a.head_blocks + hk * blocks + g / kPagedHeads];
   if (seg.y == 1) return;   // written already
-  const int c4 = tid % kLanes, part = tid / kLanes;
+  const int c4 = tid % kLanes, part = tid / kLanes, c0 = blockIdx.z * kJoinChannels;
   const float ninf = -__builtin_huge_valf();
   __shared__ f32x4 so[kParts][kLanes];
-  __shared__ float sz[kParts], sm[kWaves], se[kWaves];
-  auto row = [&](int i) { return (size_t)(seg.x + i) * a.part_heads + g % kPagedHeads; };
-  auto exp_of = [&](const float* pm) { return __builtin_bit_cast(int, pm[2]); };
-  // The largest max and exponent (a small whole number: exact in FP32) of all chunks.
-  float m = ninf, ef = ninf;
-  for (int i = tid; i < seg.y; i += kJoinThreads) {
-    const float* pm = a.part_mze + 3 * row(i);
-    m = fmaxf(m, pm[0]);
-    ef = fmaxf(ef, (float)exp_of(pm));
-  }
-  m = wave_max(m);
-  ef = wave_max(ef);
-  if (tid % kWave == 0) {
-    sm[wave] = m;
-    se[wave] = ef;
-  }
+  __shared__ float sz[kParts], sm[kWaves];
+  // Row i of the partial results: the first may be its workgroup's second row, the others are first rows.
+  auto row = [&](int i) { return (size_t)(i == 0 ? seg.x : (seg.x & ~1) + 2 * i) * a.part_heads + g % kPagedHeads; };
+  const float2* rz = reinterpret_cast<const float2*>(a.part_rz);
+  float top = ninf;
+  for (int i = tid; i < seg.y; i += kJoinThreads) top = fmaxf(top, rz[row(i)].x);
+  top = wave_max(top);
+  if (tid % kWave == 0) sm[wave] = top;
   __syncthreads();
-  m = sm[0];
-  ef = se[0];
+  top = sm[0];
 #pragma unroll
-  for (int w = 1; w < kWaves; ++w) {
-    m = fmaxf(m, sm[w]);
-    ef = fmaxf(ef, se[w]);
-  }
-  const int e = (int)ef;
+  for (int w = 1; w < kWaves; ++w) top = fmaxf(top, sm[w]);
   float z = 0.0f;
   f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
   for (int i0 = part; i0 < seg.y; i0 += kParts * kAhead) {
-    float f[kAhead], zi[kAhead];
+    float2 x[kAhead];
     f32x4 oi[kAhead];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
-      const int i = i0 + u * kParts;
-      const float* pm = a.part_mze + 3 * row(min(i, seg.y - 1));
-      oi[u] = *reinterpret_cast<const f32x4*>(a.part_o + row(min(i, seg.y - 1)) * D + 4 * c4);
-      zi[u] = i < seg.y ? pm[1] : 0.0f;
-      const bool some = i < seg.y && pm[0] != ninf;
-      f[u] = some ? __builtin_amdgcn_exp2f(pm[0] - m) : 0.0f;
-      z += zi[u] * f[u];
-      if constexpr (is_8bit(FORMAT)) f[u] = __builtin_amdgcn_ldexpf(f[u], exp_of(pm) - e);
-      oi[u] = some ? oi[u] : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      const size_t r = row(min(i0 + u * kParts, seg.y - 1));
+      x[u] = rz[r];
+      oi[u] = *reinterpret_cast<const f32x4*>(a.part_o + r * D + c0 + 4 * c4);
     }
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) o += oi[u] * f[u];
+    for (int u = 0; u < kAhead; ++u) {
+      if (i0 + u * kParts >= seg.y) break;
+      // (A row without a finite score may hold a NaN as its normalizer.)
+      const float f = x[u].x == ninf ? 0.0f : __builtin_amdgcn_exp2f(x[u].x - top);
+      z += x[u].y * f;
+      o += oi[u] * f;
+    }
   }
   so[part][c4] = o;
   if (c4 == 0) sz[part] = z;
   __syncthreads();
-  if (tid < kLanes) {
+  if (tid < kJoinChannels) {
     z = 0.0f;
-    o = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
+    float x = 0.0f;
+#pragma unroll 8
     for (int q = 0; q < kParts; ++q) {
       z += sz[q];
-      o += so[q][tid];
+      x += so[q][tid / 4][tid % 4];
     }
     const long long at = (long long)b * a.Hq + hq;
-    uint32_t h[4];
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-      h[r] = float_to_bits<TYPE>(z == 0.0f ? 0.0f : is_8bit(FORMAT) ? __builtin_amdgcn_ldexpf(o[r] / z, e) : o[r] / z);
-    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.O) + at * D + 4 * tid) = make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
-    if (tid == 0 && a.lse) a.lse[at] = z == 0.0f ? ninf : 0.69314718056f * (m - kShift<FORMAT> + __builtin_amdgcn_logf(z));
+    static_cast<uint16_t*>(a.O)[at * D + c0 + tid] = (uint16_t)float_to_bits<TYPE>(z == 0.0f ? 0.0f : x / z);
+    if (tid == 0 && c0 == 0 && a.lse) a.lse[at] = z == 0.0f ? ninf : 0.69314718056f * (top + __builtin_amdgcn_logf(z));
   }
 }
 
 }  // namespace
 
-PagedDecodePlan plan_paged_decode(const PagedPool& p, int heads_q, int format) {
+PagedDecodePlan plan_paged_decode(const PagedPool& p, int heads_q, int d, int format) {
   const int G = heads_q / p.Hk;
   PagedDecodePlan pl{};
   pl.head_blocks = p.Hk * ((G + kPagedHeads - 1) / kPagedHeads);
   pl.part_heads = std::min(G, kPagedHeads);
   const int keys = tile_keys(format);
   const long long most = (((long long)p.max_pages << p.page_shift) + keys - 1) / keys;   // tiles of a sequence
+  const long long units = (most + kPagedWaves - 1) / kPagedWaves;
   const long long segments = (long long)p.B * pl.head_blocks;
-  pl.tiles = segments * most;
-  pl.chunk_workgroups = kPagedWorkgroups;
-  // Chunks hold kPagedWaves tiles at least; a sequence's last one is not full.
-  pl.workgroups = std::min(pl.chunk_workgroups + segments, segments * ((most + kPagedWaves - 1) / kPagedWaves));
-  pl.join = most > kPagedWaves;
+  pl.tiles = segments * units * kPagedWaves;
+  pl.workgroups = std::min<long long>(kCUs * resident_per_cu(d, format), segments * units);
+  // Where every sequence is one unit at most, none is shared by workgroups.
+  pl.join = units > 1;
   return pl;
 }
 
@@ -597,7 +585,7 @@ hipError_t launch_paged_decode(const PagedDecodeArgs& a, const PagedDecodePlan& 
   return for_paged_types(d, type, format, [&](auto D, auto T, auto F) {
     hipLaunchKernelGGL((paged_decode_kernel<D(), T(), F()>), dim3((unsigned)pl.workgroups), dim3(kPagedWaves * kWave), 0, stream, a);
     if (pl.join)
-      hipLaunchKernelGGL((paged_join_kernel<D(), T(), F()>), dim3(a.Hq, a.pool.B), dim3(kJoinThreads), 0,
+      hipLaunchKernelGGL((paged_join_kernel<D(), T()>), dim3(a.Hq, a.pool.B, D() / kJoinChannels), dim3(kJoinThreads), 0,
                          stream, a);
     return hipGetLastError();
   });

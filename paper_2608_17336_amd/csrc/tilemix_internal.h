@@ -201,20 +201,19 @@ struct PagedDecodeArgs {
   int Hq, window;
   float scale_log2e;
   int head_blocks;         // KV heads x blocks of 16 query heads
-  int chunk_workgroups;    // workgroups among which the tiles of the batch are shared
-  // Partial results of sequences that have several chunks, one row per workgroup (nullptr where none can):
+  // Partial results of sequences that several workgroups share, two rows per workgroup (nullptr where none can be):
   int part_heads;          // query heads of a row
-  float* part_mze;         // [workgroups, part_heads, 3]: max (log2 units), normalizer, exponent of part_o
-  float* part_o;           // [workgroups, part_heads, d]: output, unnormalized, in units of 2^exponent
-  int* segments;           // [B, head_blocks, 2]: first workgroup and number of chunks
+  float* part_rz;          // [rows, part_heads, 2]: reference of the weights (log2 units), normalizer
+  float* part_o;           // [rows, part_heads, d]: output, unnormalized
+  int* segments;           // [B, head_blocks, 2]: first row and number of workgroups
 };
 struct PagedDecodePlan {
-  int head_blocks, part_heads, chunk_workgroups;
+  int head_blocks, part_heads;
   long long tiles;         // the most tiles that the batch can have
   long long workgroups;
-  bool join;               // a sequence may have several chunks
+  bool join;               // workgroups may share a sequence
 };
-PagedDecodePlan plan_paged_decode(const PagedPool& p, int heads_q, int format);
+PagedDecodePlan plan_paged_decode(const PagedPool& p, int heads_q, int d, int format);
 hipError_t launch_paged_decode(const PagedDecodeArgs& args, const PagedDecodePlan& plan, int d, int type, int format,
                                hipStream_t stream);
 
