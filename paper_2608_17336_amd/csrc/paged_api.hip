@@ -114,7 +114,7 @@ tilemix_status check_decode(const tilemix_paged_cache* c, int32_t heads_q) {
   if (st != TILEMIX_OK) return st;
   if (heads_q < 1 || heads_q > 65535 || heads_q % c->heads_kv != 0)
     return fail(TILEMIX_ERR_SHAPE, "heads_q (%d) must be a multiple of heads_kv (%d), at most 65535", heads_q, c->heads_kv);
-  if (tilemix::plan_paged_decode(pool_of(c), heads_q, c->head_dim, c->format).tiles > 0x7fffffffLL)
+  if (tilemix::plan_paged_decode(pool_of(c), heads_q, c->head_dim, c->format).units > 0x7fffffffLL)
     return fail(TILEMIX_ERR_SHAPE, "batch * heads * max_pages * page_size is too large");
   return TILEMIX_OK;
 }
@@ -127,7 +127,7 @@ struct DecodeBytes {
   size_t total() const { return segments + rz + o; }
 };
 DecodeBytes decode_bytes(const tilemix_paged_cache* c, const tilemix::PagedDecodePlan& pl) {
-  if (!pl.join) return {0, 0, 0};
+  if (pl.whole) return {0, 0, 0};
   const size_t rows = 2 * (size_t)pl.workgroups * pl.part_heads;
   return {align256((size_t)c->batch * pl.head_blocks * 2 * sizeof(int)), align256(rows * 2 * sizeof(float)),
           align256(rows * c->head_dim * sizeof(float))};
@@ -199,6 +199,7 @@ tilemix_status tilemix_paged_decode(const tilemix_paged_cache* cache, int32_t ty
     a.part_o = reinterpret_cast<float*>(ws + need.segments + need.rz);
   }
   a.head_blocks = pl.head_blocks;
+  a.whole = pl.whole;
   a.part_heads = pl.part_heads;
   a.Q = Q; a.O = O; a.lse = lse; a.q_stride = q_stride;
   a.Hq = heads_q; a.window = window;

@@ -21,6 +21,8 @@ namespace {
 
 constexpr int kPagedWaves = 4;
 constexpr int kCUs = 256;
+// What it costs to begin and end a sequence and head block, in tiles.
+constexpr int kPartStart = 6;
 constexpr int kPagedHeads = 16;                  // query heads on the columns of a matrix-core tile
 // 16-key slabs per tile: a tile is 16 KiB of K and V for d = 128, 8 KiB for d = 64.
 template <int FORMAT>
@@ -34,7 +36,8 @@ int tile_keys(int format) { return 16 * (is_8bit(format) ? 4 : 2); }
 // The tokens that a sequence's query attends to, as tiles of `keys` tokens: first .. len - 1, of tiles
 // first / keys .. .
 struct Span {
-  int first, len, tile0, tiles;
+  int first = 0, len = 0, tile0 = 0, tiles = 0;
+  Span() = default;
   __device__ __forceinline__ Span(const PagedDecodeArgs& a, int keys, int tokens) {
     const PagedPool& p = a.pool;
     len = min(max(tokens, 0), p.max_pages << p.page_shift);
@@ -42,32 +45,86 @@ struct Span {
     tile0 = first / keys;
     tiles = (len + keys - 1) / keys - tile0;
   }
+  // Tiles as they are shared out: a sequence without tokens has one, so that it is written, too.
+  __device__ __forceinline__ int share() const { return max(1, tiles); }
 };
 
-// How the batch is cut.  A unit is kPagedWaves tiles of one sequence and head block, one per wave; a sequence has
-// one at least, so that one without tokens is written, too.  Units are numbered by sequence, then head block, then
-// token; workgroup w takes units [w quota, (w + 1) quota).  Every wave finds its place for itself: a lane
-// takes a run of sequences.
+// A value that all lanes read from memory that nobody writes meanwhile, through the scalar path.
+__device__ __forceinline__ int load_uniform(const int* p) {
+  return *(const __attribute__((address_space(4))) int*)(uintptr_t)p;
+}
+
+// How the batch is cut into the workgroups' runs.  Sequences and head blocks are lined up, by sequence, then head block.
+//   kPieces: each is cut into equal pieces, the fewest of `quota` tiles at most, and a workgroup takes one piece.
+//   kRuns: each takes kPartStart units, for what it costs to begin and end one, and then a unit for each of its
+//     tiles; workgroup w takes the tiles in units [w quota, (w + 1) quota).
+//   kWhole: a workgroup takes `quota` of them, none is shared by workgroups and nothing has to be joined: where
+//     no sequence can have more than kPagedWaves tiles.
+// Runs share the tiles evenly, pieces begin and end one sequence only: pieces are taken where their number
+// fits the workgroups with at most kPartStart tiles more each than the even share.  Every wave finds its place for
+// itself: a lane takes a run of sequences.
+enum { kPieces, kRuns, kWhole };
+
+// n / d for 0 <= n < 2^31, d >= 1 and quotients below 2^20: an estimate in FP32, off by one at most, and a
+// correction, in a third of the instructions of the compiler's division.
+__device__ __forceinline__ int small_quotient(int n, int d) {
+  const int q = (int)((float)n * __builtin_amdgcn_rcpf((float)d)), r = n - q * d;
+  return q + (r >= d ? 1 : 0) - (r < 0 ? 1 : 0);
+}
+__device__ __forceinline__ int ceil_div(int n, int d) { return small_quotient(n + d - 1, d); }
+
 struct Run {
-  int b = -1, head_block, unit;   // first unit: in its sequence and head block; b = -1: no unit is left
-  int quota;
-  __device__ __forceinline__ static int units(const Span& s) { return max(1, (s.tiles + kPagedWaves - 1) / kPagedWaves); }
+  int b = -1, head_block, unit;   // where it begins (unit, or piece: of its sequence's); b = -1: no tile is left
+  int mode, quota;
+  __device__ __forceinline__ int units(int share) const {
+    return mode == kWhole ? 1 : mode == kPieces ? ceil_div(share, quota) : kPartStart + share;
+  }
   __device__ __forceinline__ Run(const PagedDecodeArgs& a, int w, int lane, int keys) {
-    const int B = a.pool.B, per = (B + kWave - 1) / kWave, b0 = min(lane * per, B), b1 = min(b0 + per, B);
-    int mine = 0;
-    for (int s = b0; s < b1; ++s) mine += units(Span(a, keys, a.pool.seqlens[s]));
-    const int end = wave_scan(mine), all = __builtin_amdgcn_readlane(end, kWave - 1) * a.head_blocks;
-    quota = (all + (int)gridDim.x - 1) / (int)gridDim.x;
-    if ((long long)w * quota >= all) return;
-    const int u = w * quota;
-    int at = (end - mine) * a.head_blocks, seq = 0, hb = 0, in = 0;
+    const int B = a.pool.B, per = (B + kWave - 1) / kWave, b0 = min(lane * per, B), b1 = min(b0 + per, B), W = gridDim.x;
+    auto share = [&](int s) { return Span(a, keys, a.pool.seqlens[s]).share(); };
+    auto wave_total = [](int x) { return __builtin_amdgcn_readlane(wave_scan(x), kWave - 1); };
+    // (Of up to 64 sequences, a lane's length is read once.)
+    const int mine = b0 < b1 ? share(b0) : 0;
+    auto over_lane = [&](auto&& f) {
+      int sum = b0 < b1 ? f(mine) : 0;
+      for (int s = b0 + 1; s < b1; ++s) sum += f(share(s));
+      return sum;
+    };
+    mode = a.whole ? kWhole : kRuns;
+    int own, all;
+    if (mode == kWhole) {
+      own = b1 - b0;
+      all = B * a.head_blocks;
+      quota = (int)a.div_workgroups.quot(all + W - 1);
+    } else {
+      const int tiles = over_lane([](int n) { return n; }), total = wave_total(tiles) * a.head_blocks;
+      const int even = max(kPagedWaves, (int)a.div_workgroups.quot(total + W - 1));
+      if (B * a.head_blocks <= W) {
+        mode = kPieces;
+        for (quota = even; quota <= even + kPartStart; quota += 2) {
+          own = over_lane([&](int n) { return ceil_div(n, quota); });
+          all = wave_total(own) * a.head_blocks;
+          if (all <= W) break;
+        }
+        if (quota > even + kPartStart) mode = kRuns;
+      }
+      if (mode == kRuns) {
+        own = tiles + kPartStart * (b1 - b0);
+        all = total + kPartStart * B * a.head_blocks;
+        quota = max(kPagedWaves, (int)a.div_workgroups.quot(all + W - 1));
+      }
+    }
+    const int end = wave_scan(own), step = mode == kPieces ? 1 : quota;
+    if ((long long)w * step >= all) return;
+    const int u = w * step;
+    int at = (end - own) * a.head_blocks, seq = 0, hb = 0, in = 0;
     const bool hit = u >= at && u < end * a.head_blocks;
     if (hit) {
       for (int s = b0; s < b1; ++s) {
-        const int n = units(Span(a, keys, a.pool.seqlens[s])), next = at + n * a.head_blocks;
+        const int n = units(s == b0 ? mine : share(s)), next = at + n * a.head_blocks;
         if (u < next) {
           seq = s;
-          hb = (u - at) / n;
+          hb = small_quotient(u - at, n);
           in = (u - at) - hb * n;
           break;
         }
@@ -78,6 +135,48 @@ struct Run {
     b = __builtin_amdgcn_readlane(seq, l);
     head_block = __builtin_amdgcn_readlane(hb, l);
     unit = __builtin_amdgcn_readlane(in, l);
+  }
+};
+
+// A workgroup's part of one sequence and head block.  All members are the same in every lane.
+struct Part {
+  Span span;
+  int b = -1, head_block = 0;
+  int lo = 0, hi = 0;          // its tiles, counted from the span's first: lo .. hi - 1 of span.share()
+  int take = 0;                // the units that they are
+  int step = 1;                // tiles of each workgroup that follows in the sequence and head block
+  int tile0 = 0, end = 0;      // its tiles that hold tokens: tile0 .. end - 1
+  int hk = 0, g0 = 0;          // KV head, first query head of the block among the KV head's
+  Part() = default;
+  // From unit `off` of the sequence and head block on, `left` units at most.
+  __device__ __forceinline__ Part(const PagedDecodeArgs& a, int mode, int quota, int b_, int hb, int off, int left, const Span& sp)
+      : span(sp), b(b_), head_block(hb) {
+    const int n = span.share();
+    hk = (int)a.div_blocks.quot(hb);
+    g0 = (hb - hk * (int)a.div_blocks.d) * kPagedHeads;
+    take = 1;
+    hi = n;
+    if (mode == kPieces) {
+      step = ceil_div(n, ceil_div(n, quota));
+      lo = off * step;
+      hi = min(n, lo + step);
+    } else if (mode == kRuns) {
+      take = min(left, kPartStart + n - off);
+      step = quota;
+      lo = max(off - kPartStart, 0);
+      hi = off + take - kPartStart;
+    }
+    tile0 = span.tile0 + lo;
+    end = span.tile0 + min(span.tiles, hi);
+  }
+  __device__ __forceinline__ bool some() const { return hi > lo; }
+  // The same in scalar registers, where the compiler lost track of it.
+  __device__ __forceinline__ Part uniform() const {
+    Part q = *this;
+    for (int* x : {&q.span.first, &q.span.len, &q.span.tile0, &q.span.tiles, &q.b, &q.head_block, &q.lo, &q.hi, &q.take, &q.step, &q.tile0,
+                   &q.end, &q.hk, &q.g0})
+      *x = __builtin_amdgcn_readfirstlane(*x);
+    return q;
   }
 };
 
@@ -166,37 +265,35 @@ void paged_decode_kernel(PagedDecodeArgs a) {
   __shared__ __align__(16) float osum[kPagedWaves][kPagedHeads][kOS];
 
   const Run run(a, blockIdx.x, lane, kKeys);
-  const int quota = __builtin_amdgcn_readfirstlane(run.quota);
-  int b = __builtin_amdgcn_readfirstlane(run.b), head_block = __builtin_amdgcn_readfirstlane(run.head_block);
-  int unit = __builtin_amdgcn_readfirstlane(run.unit);
-  int left = b < 0 ? 0 : quota;   // units
-  while (left > 0 && b < p.B) {
-  const int G = a.Hq / p.Hk, blocks = a.head_blocks / p.Hk;
-  const int hk = head_block / blocks, g0 = head_block % blocks * kPagedHeads;
-  const int heads = min(kPagedHeads, G - g0), hq0 = hk * G + g0;
-  // (The load's result is the same in every lane, which only a scalar register tells the compiler.)
-  const Span span(a, kKeys, __builtin_amdgcn_readfirstlane(p.seqlens[b]));
-  const int units = Run::units(span), take = min(left, units - unit);
-  const int tile0 = span.tile0 + unit * kPagedWaves;
-  const int tile_end = span.tile0 + min(span.tiles, (unit + take) * kPagedWaves);
+  const int quota = __builtin_amdgcn_readfirstlane(run.quota), mode = __builtin_amdgcn_readfirstlane(run.mode);
+  int left = mode == kPieces ? 1 : quota;   // units
+  Part cur;
+  {
+    const int b = __builtin_amdgcn_readfirstlane(run.b);
+    if (b < 0) return;
+    cur = Part(a, mode, quota, b, __builtin_amdgcn_readfirstlane(run.head_block), __builtin_amdgcn_readfirstlane(run.unit), left,
+               Span(a, kKeys, load_uniform(p.seqlens + b)));
+    if (!cur.some()) return;
+  }
+  // The wave's first tile of a part, if f tiles of the workgroup's run lie before it: tile f + t goes to wave
+  // (f + t) % kPagedWaves, so that the waves have the same number over all parts.
+  auto first_tile = [&](const Part& q, int f) { return q.tile0 + ((wave - f) & (kPagedWaves - 1)); };
 
-  // 1. Page ids of the wave's tiles tile0 + wave + i kPagedWaves, 64 at a time: lane (i, j) holds the j-th of
+  // 1. Page ids of the wave's tiles n, n + kPagedWaves, .. of a part, 64 at a time: lane (i, j) holds the j-th of
   //    the 2^per_shift pages of tile i.
   const int keys_shift = 4 + (kS == 8 ? 3 : kS == 4 ? 2 : 1);
   const int per_shift = max(0, keys_shift - p.page_shift);
-  const int* table = p.table + b * p.stride_table;
-  auto load_ids = [&](int i0) {
-    const int i = i0 + (lane >> per_shift), n = tile0 + wave + i * kPagedWaves;
+  auto load_ids = [&](const Part& q, int n0) {
+    const int n = n0 + (lane >> per_shift) * kPagedWaves;
     const int e = (n * kKeys >> p.page_shift) + (lane & ((1 << per_shift) - 1));
     int id = -1;
-    if (n < tile_end && e < p.max_pages && (e << p.page_shift) < span.len) id = table[e];
-    return id >= 0 && id < p.pages ? id : -1;
+    if (n < q.end && e < p.max_pages && (e << p.page_shift) < q.span.len) id = p.table[q.b * p.stride_table + e];
+    return id;
   };
-  int ids = load_ids(0);
   const int id_tiles = kWave >> per_shift;
 
-  // 2. One tile in registers.  Behind its last tile a wave requests one all the same (see 4.), a few cache lines
-  //    of page 0: every lane's offset is 0.
+  // 2. One tile in registers.  Where a wave has no tile to request it requests some all the same (see 4.), a few
+  //    cache lines of page 0: every lane's offset is 0.
   uint4 kr[kS][kKL];
   uint32_t vr[kS][4][kVW];
   f32x4 dk[kS], dv[kS];
@@ -204,37 +301,40 @@ void paged_decode_kernel(PagedDecodeArgs a) {
   const char* poolK = static_cast<const char*>(p.K);
   const char* poolV = static_cast<const char*>(p.V);
   const uint32_t k_lane = l16 * D * kBytes + 16 * lq, v_lane = 4 * lq * D * kBytes + l16 * kC * kBytes;
-  auto find_pages = [&](int i) {
+  auto find_pages = [&](int ids, int i) {
     const int at = (i & (id_tiles - 1)) << per_shift;
 #pragma unroll
-    for (int s = 0; s < kS; ++s) page[s] = __builtin_amdgcn_readlane(ids, at + (16 * s >> p.page_shift));
+    for (int s = 0; s < kS; ++s) {
+      const int id = __builtin_amdgcn_readlane(ids, at + (16 * s >> p.page_shift));
+      page[s] = id < p.pages ? id : -1;
+    }
   };
   // Row of slab s of tile n in its page, or in page 0 where there is none: it is masked.
-  auto slab_row = [&](int n, int s) { return (hk << p.page_shift) + ((n * kKeys + 16 * s) & ((1 << p.page_shift) - 1)); };
-  auto load_keys = [&](int n) {
-    const uint32_t k_off = n < tile_end ? k_lane : 0u, s_off = n < tile_end ? 16u * lq : 0u;
+  auto slab_row = [&](int hk, int n, int s) { return (hk << p.page_shift) + ((n * kKeys + 16 * s) & ((1 << p.page_shift) - 1)); };
+  auto load_keys = [&](int hk, int n, bool some) {
+    const uint32_t k_off = some ? k_lane : 0u, s_off = some ? 16u * lq : 0u;
 #pragma unroll
     for (int s = 0; s < kS; ++s) {
-      const char* base = poolK + kBytes * (max(page[s], 0) * p.stride_k + (long long)slab_row(n, s) * D);
+      const char* base = poolK + kBytes * (max(page[s], 0) * p.stride_k + (long long)slab_row(hk, n, s) * D);
 #pragma unroll
       for (int i = 0; i < kKL; ++i) kr[s][i] = ld_global_16(base + 64 * i + k_off);
     }
     if constexpr (k8) {
 #pragma unroll
       for (int s = 0; s < kS; ++s)
-        dk[s] = *reinterpret_cast<const f32x4*>(reinterpret_cast<const char*>(p.dK + max(page[s], 0) * p.stride_dk + slab_row(n, s)) + s_off);
+        dk[s] = *reinterpret_cast<const f32x4*>(reinterpret_cast<const char*>(p.dK + max(page[s], 0) * p.stride_dk + slab_row(hk, n, s)) + s_off);
     }
   };
-  auto load_values = [&](int n) {
-    const uint32_t v_off = n < tile_end ? v_lane : 0u, s_off = n < tile_end ? 16u * lq : 0u;
+  auto load_values = [&](int hk, int n, bool some) {
+    const uint32_t v_off = some ? v_lane : 0u, s_off = some ? 16u * lq : 0u;
     if constexpr (k8) {
 #pragma unroll
       for (int s = 0; s < kS; ++s)
-        dv[s] = *reinterpret_cast<const f32x4*>(reinterpret_cast<const char*>(p.dV + max(page[s], 0) * p.stride_dv + slab_row(n, s)) + s_off);
+        dv[s] = *reinterpret_cast<const f32x4*>(reinterpret_cast<const char*>(p.dV + max(page[s], 0) * p.stride_dv + slab_row(hk, n, s)) + s_off);
     }
 #pragma unroll
     for (int s = 0; s < kS; ++s) {
-      const char* base = poolV + kBytes * (max(page[s], 0) * p.stride_v + (long long)slab_row(n, s) * D);
+      const char* base = poolV + kBytes * (max(page[s], 0) * p.stride_v + (long long)slab_row(hk, n, s) * D);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const char* at = base + r * D * kBytes + v_off;
@@ -250,19 +350,45 @@ void paged_decode_kernel(PagedDecodeArgs a) {
       }
     }
   };
+  uint4 qf[kQ];
+  auto load_query = [&](const Part& q) {
+    const int G = a.group, heads = min(kPagedHeads, G - q.g0);
+    const char* row = static_cast<const char*>(a.Q) + 2 * (q.b * a.q_stride + (long long)(q.hk * G + q.g0 + min(l16, heads - 1)) * D);
+#pragma unroll
+    for (int i = 0; i < kQ; ++i) qf[i] = ld_global_16(row + 2 * (k8 ? 64 * (i / 2) + 16 * lq + 8 * (i % 2) : 32 * i + 8 * lq));
+  };
+
+  int f = 0, i = 0, n = first_tile(cur, 0);
+  int ids = load_ids(cur, n);
+  load_query(cur);
+  find_pages(ids, 0);
+  __builtin_amdgcn_sched_barrier(0);
+  load_keys(cur.hk, n, n < cur.end);
+  __builtin_amdgcn_sched_barrier(0);
+  load_values(cur.hk, n, n < cur.end);
+  __builtin_amdgcn_sched_barrier(0);
+  for (;;) {
+  const int G = a.group, heads = min(kPagedHeads, G - cur.g0), hq0 = cur.hk * G + cur.g0;
+  cur = cur.uniform();
+  n = __builtin_amdgcn_readfirstlane(n);
+  left = __builtin_amdgcn_readfirstlane(left);
+  // The part that follows, so that its first tiles are requested behind the last ones of this.
+  Part next;
+  const bool whole_head = cur.head_block + 1 == a.head_blocks;
+  bool more = left > cur.take && !(whole_head && cur.b + 1 == p.B);
+  if (more) {
+    next = Part(a, mode, quota, cur.b + (whole_head ? 1 : 0), whole_head ? 0 : cur.head_block + 1, 0, left - cur.take,
+                whole_head ? Span(a, kKeys, load_uniform(p.seqlens + cur.b + 1)) : cur.span);
+    more = next.some();
+  }
+  const int f_next = f + cur.hi - cur.lo, n_next = first_tile(next, f_next);
+  const int ids_next = load_ids(next, n_next);
 
   // 3. Query rows as the B operand of the score products: lane (head l16, lq) holds the channels that it
   //    reads of a key row.  BF16 queries against 8-bit codes are brought to FP16 by a power of two per
   //    head, 2^q_exp: the largest to [2^14, 2^15), so that what FP16 cannot hold lies below 2^-39 of it.
-  uint4 qf[kQ];
   float f_head = a.scale_log2e;   // score of a product, in log2 units, before the key's scale
   {
-    const char* q = static_cast<const char*>(a.Q) + 2 * (b * a.q_stride + (long long)(hq0 + min(l16, heads - 1)) * D);
-#pragma unroll
-    for (int i = 0; i < kQ; ++i) {
-      const int c = k8 ? 64 * (i / 2) + 16 * lq + 8 * (i % 2) : 32 * i + 8 * lq;
-      qf[i] = ld_global_16(q + 2 * c);
-    }
     const uint32_t some = l16 < heads ? ~0u : 0u;
 #pragma unroll
     for (int i = 0; i < kQ; ++i) qf[i] = make_uint4(qf[i].x & some, qf[i].y & some, qf[i].z & some, qf[i].w & some);
@@ -292,23 +418,17 @@ void paged_decode_kernel(PagedDecodeArgs a) {
   // 4. The wave's tiles.  m: running max (log2 units); ref: the reference r; z: this lane's share of the normalizer;
   //    acc: output.  Loads complete in order, and a wait counts the younger ones, so rows are requested in the
   //    same order and number on every way to a wait: the keys and their scales once the scores are
-  //    formed, the values and theirs after P V, into the registers that these leave, also after the
-  //    last tile.
+  //    formed, the values and theirs after P V, into the registers that these leave, whether there is
+  //    another tile in this part, in the next one, or none.
   float m = ninf, ref = ninf, z = 0.0f;
   int e = kExpMin;
   f32x4 acc[kC];
 #pragma unroll
   for (int c = 0; c < kC; ++c) acc[c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  int i = 0, n = tile0 + wave;
-  find_pages(0);
-  __builtin_amdgcn_sched_barrier(0);
-  load_keys(n);
-  __builtin_amdgcn_sched_barrier(0);
-  load_values(n);
-  __builtin_amdgcn_sched_barrier(0);
-  while (n < tile_end) {
+  const bool none = n >= cur.end;
+  while (n < cur.end) {
     // Which of the tile's keys count, where it is not all of them.
-    bool all = n * kKeys >= span.first && (n + 1) * kKeys <= span.len;
+    bool all = n * kKeys >= cur.span.first && (n + 1) * kKeys <= cur.span.len;
     uint32_t has = 0;
 #pragma unroll
     for (int s = 0; s < kS; ++s) has |= page[s] >= 0 ? 1u << s : 0u;
@@ -331,17 +451,29 @@ void paged_decode_kernel(PagedDecodeArgs a) {
       for (int r = 0; r < 4; ++r) sc[s][r] = c[r] * (k8 ? f_head * dk[s][r] : f_head);
     }
     __builtin_amdgcn_sched_barrier(0);
-    ++i;
-    if ((i & (id_tiles - 1)) == 0) ids = load_ids(i);
-    find_pages(i);
-    load_keys(n + kPagedWaves);
+    const bool here = n + kPagedWaves < cur.end;
+    const int to = here ? n + kPagedWaves : n_next, hk = here ? cur.hk : next.hk;
+    const bool some = here || n_next < next.end;
+    if (here) {
+      ++i;
+      if ((i & (id_tiles - 1)) == 0) {
+        ids = load_ids(cur, to);
+        asm volatile("; wait for them here" : "+v"(ids));   // not on the other ways, where rows are in flight
+      }
+    } else {
+      i = 0;
+      ids = ids_next;
+      asm volatile("; and here for the next part's" : "+v"(ids));
+    }
+    find_pages(ids, i);
+    load_keys(hk, to, some);
     if (!all) {
 #pragma unroll
       for (int s = 0; s < kS; ++s)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int t = n * kKeys + 16 * s + 4 * lq + r;
-          const bool ok = (has >> s & 1) && t >= span.first && t < span.len;
+          const bool ok = (has >> s & 1) && t >= cur.span.first && t < cur.span.len;
           sc[s][r] = ok ? sc[s][r] : ninf;
           if constexpr (k8) dv[s][r] = ok ? dv[s][r] : 0.0f;
           // What a slot behind the sequence holds may be a NaN, which a weight of 0 does not cancel.
@@ -432,9 +564,19 @@ void paged_decode_kernel(PagedDecodeArgs a) {
       }
     }
     __builtin_amdgcn_sched_barrier(0);   // not ahead of P V: their registers are in use
-    load_values(n + kPagedWaves);
+    load_values(hk, to, some);
     n += kPagedWaves;
   }
+  if (none) {   // the wave's registers hold nothing of this part
+    i = 0;
+    ids = ids_next;
+    find_pages(ids, 0);
+    load_keys(next.hk, n_next, n_next < next.end);
+    __builtin_amdgcn_sched_barrier(0);
+    load_values(next.hk, n_next, n_next < next.end);
+  }
+  __builtin_amdgcn_sched_barrier(0);
+  if (more) load_query(next);
 
   // 5. The waves' results joined in LDS.
   z = quad_rows_sum(z);
@@ -450,23 +592,27 @@ void paged_decode_kernel(PagedDecodeArgs a) {
 #pragma unroll
     for (int c = 0; c < kC; ++c) osum[wave][l16][(4 * lq + r) * kC + c] = ref == ninf ? 0.0f : acc[c][r] * fw;
   __syncthreads();
-  const bool whole = take == units;
-  // Partial results: of the workgroup's first units in row 2 w, of units behind others in row 2 w + 1 (they
-  // are its last).
-  const size_t part_row = ((size_t)blockIdx.x * 2 + (left != quota ? 1 : 0)) * a.part_heads;
-  for (int o = tid; o < heads * D; o += kPagedWaves * kWave) {
-    const int g = o / D, c = o % D;
-    float sum = 0.0f, zz = 0.0f;
+  const bool whole = cur.lo == 0 && cur.hi == cur.span.share();
+  // Partial results: of the workgroup's first part in row 2 w, of one behind others in row 2 w + 1 (it is the
+  // last, and has its sequence's first tile).
+  const int part_row = (int)blockIdx.x * 2 + (f != 0 ? 1 : 0);
+  for (int o = tid; o < heads * (D / 4); o += kPagedWaves * kWave) {
+    const int g = o / (D / 4), c = o % (D / 4) * 4;
+    f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+    float zz = 0.0f;
 #pragma unroll
     for (int w = 0; w < kPagedWaves; ++w) {
-      sum += osum[w][g][c];
+      sum += *reinterpret_cast<const f32x4*>(&osum[w][g][c]);
       zz += red_z[w][g];
     }
     if (whole) {
-      static_cast<uint16_t*>(a.O)[((long long)b * a.Hq + hq0 + g) * D + c] =
-          (uint16_t)float_to_bits<TYPE>(zz == 0.0f ? 0.0f : sum / zz);
+      uint32_t h[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) h[r] = float_to_bits<TYPE>(zz == 0.0f ? 0.0f : sum[r] / zz);
+      *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.O) + ((long long)cur.b * a.Hq + hq0 + g) * D + c) =
+          make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
     } else {
-      a.part_o[(part_row + g) * D + c] = sum;
+      *reinterpret_cast<f32x4*>(a.part_o + ((size_t)part_row * a.part_heads + g) * D + c) = sum;
     }
   }
   if (tid < heads) {
@@ -478,54 +624,45 @@ void paged_decode_kernel(PagedDecodeArgs a) {
     }
     if (whole) {
       if (a.lse)
-        a.lse[(long long)b * a.Hq + hq0 + tid] =
+        a.lse[(long long)cur.b * a.Hq + hq0 + tid] =
             zz == 0.0f ? ninf : 0.69314718056f * (mm + __builtin_amdgcn_logf(zz));
     } else {
-      reinterpret_cast<float2*>(a.part_rz)[part_row + tid] = make_float2(mm, zz);
+      reinterpret_cast<float2*>(a.part_rz)[(size_t)part_row * a.part_heads + tid] = make_float2(mm, zz);
     }
   }
   // For the join: the first row, and how many workgroups there are from this one on.
-  if (a.segments && tid == 0 && unit == 0) {
-    const int beyond = units - take;   // units of the workgroups that follow
-    reinterpret_cast<int2*>(a.segments)[(size_t)b * a.head_blocks + head_block] =
-        make_int2((int)blockIdx.x * 2 + (left != quota ? 1 : 0), 1 + (beyond + quota - 1) / quota);
+  if (a.segments && tid == 0 && cur.lo == 0) {
+    const int beyond = cur.span.share() - cur.hi;   // tiles of the workgroups that follow
+    reinterpret_cast<int2*>(a.segments)[(size_t)cur.b * a.head_blocks + cur.head_block] =
+        make_int2(part_row, 1 + ceil_div(beyond, cur.step));
   }
-  left -= take;
-  unit = 0;
-  if (++head_block == a.head_blocks) {
-    head_block = 0;
-    ++b;
-  }
-  if (left > 0) __syncthreads();   // the LDS is used again
+  if (!more) return;
+  left -= cur.take;
+  cur = next;
+  f = f_next;
+  n = n_next;
+  __syncthreads();   // the LDS is used again
   }
 }
 
-// One workgroup per (query head, sequence, 32 channels): thread (part, channel quad) joins every kParts-th row.
+// One workgroup per (query head, sequence, 32 channels): thread (part, channel quad) joins every kParts-th row with
+// a running reference of its own; the parts are joined in LDS.
 constexpr int kJoinThreads = 256, kJoinChannels = 32;
 template <int D, int TYPE>
 __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedDecodeArgs a) {
-  constexpr int kLanes = kJoinChannels / 4, kParts = kJoinThreads / kLanes, kWaves = kJoinThreads / kWave;
-  constexpr int kAhead = 4;
-  const int hq = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, wave = tid / kWave;
-  const int G = a.Hq / a.pool.Hk, blocks = a.head_blocks / a.pool.Hk, hk = hq / G, g = hq % G;
+  constexpr int kLanes = kJoinChannels / 4, kParts = kJoinThreads / kLanes, kAhead = 4;
+  const int hq = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
+  const int hk = (int)a.div_group.quot(hq), g = hq - hk * a.group, blocks = (int)a.div_blocks.d;
   const int2 seg = reinterpret_cast<const int2*>(a.segments)[(size_t)b * a.head_blocks + hk * blocks + g / kPagedHeads];
   if (seg.y == 1) return;   // written already
   const int c4 = tid % kLanes, part = tid / kLanes, c0 = blockIdx.z * kJoinChannels;
   const float ninf = -__builtin_huge_valf();
   __shared__ f32x4 so[kParts][kLanes];
-  __shared__ float sz[kParts], sm[kWaves];
+  __shared__ float sz[kParts], sr[kParts];
   // Row i of the partial results: the first may be its workgroup's second row, the others are first rows.
   auto row = [&](int i) { return (size_t)(i == 0 ? seg.x : (seg.x & ~1) + 2 * i) * a.part_heads + g % kPagedHeads; };
   const float2* rz = reinterpret_cast<const float2*>(a.part_rz);
-  float top = ninf;
-  for (int i = tid; i < seg.y; i += kJoinThreads) top = fmaxf(top, rz[row(i)].x);
-  top = wave_max(top);
-  if (tid % kWave == 0) sm[wave] = top;
-  __syncthreads();
-  top = sm[0];
-#pragma unroll
-  for (int w = 1; w < kWaves; ++w) top = fmaxf(top, sm[w]);
-  float z = 0.0f;
+  float ref = ninf, z = 0.0f;
   f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
   for (int i0 = part; i0 < seg.y; i0 += kParts * kAhead) {
     float2 x[kAhead];
@@ -536,25 +673,39 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedDecodeArg
       x[u] = rz[r];
       oi[u] = *reinterpret_cast<const f32x4*>(a.part_o + r * D + c0 + 4 * c4);
     }
+    float top = ref;
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) top = fmaxf(top, x[u].x);
+    const float f = ref == ninf ? 0.0f : __builtin_amdgcn_exp2f(ref - top);
+    z *= f;
+    o *= f;
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       if (i0 + u * kParts >= seg.y) break;
       // (A row without a finite score may hold a NaN as its normalizer.)
-      const float f = x[u].x == ninf ? 0.0f : __builtin_amdgcn_exp2f(x[u].x - top);
-      z += x[u].y * f;
-      o += oi[u] * f;
+      const float fu = x[u].x == ninf ? 0.0f : __builtin_amdgcn_exp2f(x[u].x - top);
+      z += x[u].y * fu;
+      o += oi[u] * fu;
     }
+    ref = top;
   }
   so[part][c4] = o;
-  if (c4 == 0) sz[part] = z;
+  if (c4 == 0) {
+    sz[part] = z;
+    sr[part] = ref;
+  }
   __syncthreads();
   if (tid < kJoinChannels) {
+    float top = ninf;
+#pragma unroll 8
+    for (int q = 0; q < kParts; ++q) top = fmaxf(top, sr[q]);
     z = 0.0f;
     float x = 0.0f;
 #pragma unroll 8
     for (int q = 0; q < kParts; ++q) {
-      z += sz[q];
-      x += so[q][tid / 4][tid % 4];
+      const float f = sr[q] == ninf ? 0.0f : __builtin_amdgcn_exp2f(sr[q] - top);
+      z += sz[q] * f;
+      x += so[q][tid / 4][tid % 4] * f;
     }
     const long long at = (long long)b * a.Hq + hq;
     static_cast<uint16_t*>(a.O)[at * D + c0 + tid] = (uint16_t)float_to_bits<TYPE>(z == 0.0f ? 0.0f : x / z);
@@ -571,20 +722,22 @@ PagedDecodePlan plan_paged_decode(const PagedPool& p, int heads_q, int d, int fo
   pl.part_heads = std::min(G, kPagedHeads);
   const int keys = tile_keys(format);
   const long long most = (((long long)p.max_pages << p.page_shift) + keys - 1) / keys;   // tiles of a sequence
-  const long long units = (most + kPagedWaves - 1) / kPagedWaves;
   const long long segments = (long long)p.B * pl.head_blocks;
-  pl.tiles = segments * units * kPagedWaves;
-  pl.workgroups = std::min<long long>(kCUs * resident_per_cu(d, format), segments * units);
-  // Where every sequence is one unit at most, none is shared by workgroups.
-  pl.join = units > 1;
+  pl.whole = most <= kPagedWaves;
+  pl.units = segments * (most + kPartStart);
+  pl.workgroups = std::min<long long>(kCUs * resident_per_cu(d, format),
+                                      pl.whole ? segments : (segments * most + kPagedWaves - 1) / kPagedWaves);
   return pl;
 }
 
-hipError_t launch_paged_decode(const PagedDecodeArgs& a, const PagedDecodePlan& pl, int d, int type, int format,
-                               hipStream_t stream) {
+hipError_t launch_paged_decode(PagedDecodeArgs a, const PagedDecodePlan& pl, int d, int type, int format, hipStream_t stream) {
+  a.group = a.Hq / a.pool.Hk;
+  a.div_group = FastDiv(a.group);
+  a.div_blocks = FastDiv(pl.head_blocks / a.pool.Hk);
+  a.div_workgroups = FastDiv((uint32_t)pl.workgroups);
   return for_paged_types(d, type, format, [&](auto D, auto T, auto F) {
     hipLaunchKernelGGL((paged_decode_kernel<D(), T(), F()>), dim3((unsigned)pl.workgroups), dim3(kPagedWaves * kWave), 0, stream, a);
-    if (pl.join)
+    if (!pl.whole)
       hipLaunchKernelGGL((paged_join_kernel<D(), T()>), dim3(a.Hq, a.pool.B, D() / kJoinChannels), dim3(kJoinThreads), 0,
                          stream, a);
     return hipGetLastError();

@@ -201,20 +201,23 @@ struct PagedDecodeArgs {
   int Hq, window;
   float scale_log2e;
   int head_blocks;         // KV heads x blocks of 16 query heads
+  int whole;               // 1: no sequence has more tiles than a workgroup has waves, and none is shared
   // Partial results of sequences that several workgroups share, two rows per workgroup (nullptr where none can be):
   int part_heads;          // query heads of a row
   float* part_rz;          // [rows, part_heads, 2]: reference of the weights (log2 units), normalizer
   float* part_o;           // [rows, part_heads, d]: output, unnormalized
   int* segments;           // [B, head_blocks, 2]: first row and number of workgroups
+  int group;               // filled in by the launch, as what follows: query heads per KV head
+  FastDiv div_group, div_blocks, div_workgroups;   // blocks: of 16 query heads per KV head
 };
 struct PagedDecodePlan {
   int head_blocks, part_heads;
-  long long tiles;         // the most tiles that the batch can have
+  bool whole;
+  long long units;         // the most units that the batch can have
   long long workgroups;
-  bool join;               // workgroups may share a sequence
 };
 PagedDecodePlan plan_paged_decode(const PagedPool& p, int heads_q, int d, int format);
-hipError_t launch_paged_decode(const PagedDecodeArgs& args, const PagedDecodePlan& plan, int d, int type, int format,
+hipError_t launch_paged_decode(PagedDecodeArgs args, const PagedDecodePlan& plan, int d, int type, int format,
                                hipStream_t stream);
 
 }  // namespace tilemix
