@@ -12,7 +12,9 @@ from __future__ import annotations
 import ctypes
 import math
 import os
+import struct
 from dataclasses import dataclass
+from typing import NamedTuple
 
 __all__ = [
     "TilemixError",
@@ -204,29 +206,6 @@ class _CDebugExport(ctypes.Structure):
                 ("kinds", ctypes.c_void_p)]
 
 
-class _CPagedCache(ctypes.Structure):
-    _fields_ = [
-        ("format", ctypes.c_int32),
-        ("pages", ctypes.c_int32),
-        ("page_size", ctypes.c_int32),
-        ("heads_kv", ctypes.c_int32),
-        ("head_dim", ctypes.c_int32),
-        ("batch", ctypes.c_int32),
-        ("max_pages", ctypes.c_int32),
-        ("stride_k", ctypes.c_int64),
-        ("stride_v", ctypes.c_int64),
-        ("stride_dk", ctypes.c_int64),
-        ("stride_dv", ctypes.c_int64),
-        ("stride_table", ctypes.c_int64),
-        ("K", ctypes.c_void_p),
-        ("V", ctypes.c_void_p),
-        ("dK", ctypes.c_void_p),
-        ("dV", ctypes.c_void_p),
-        ("page_table", ctypes.c_void_p),
-        ("seqlens_k", ctypes.c_void_p),
-    ]
-
-
 _LIB = None
 
 
@@ -300,7 +279,7 @@ def load_library() -> ctypes.CDLL:
     lib.tilemix_decode.restype = ctypes.c_int
     lib.tilemix_decode_varlen.argtypes = [P, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
     lib.tilemix_decode_varlen.restype = ctypes.c_int
-    CP = ctypes.POINTER(_CPagedCache)
+    CP = ctypes.c_char_p   # tilemix_paged_cache, packed into bytes (which may hold zeros: only its address counts)
     rows_args = [CP, ctypes.c_int32, vp, ctypes.c_int32, ctypes.c_int32, vp]
     lib.tilemix_paged_append.argtypes = rows_args + [ctypes.c_int64, vp, ctypes.c_int64, vp]
     lib.tilemix_paged_append.restype = ctypes.c_int
@@ -796,8 +775,7 @@ def tilemix_decode(Q, K, K8, dK, V8, dV, route_bits, group_size: int, scale: flo
 
 # -------------------------------------------------------------------- paged key/value cache
 
-@dataclass(frozen=True)
-class PagedCache:
+class PagedCache(NamedTuple):
     """A pool of pages for ``tilemix_paged_append``, ``_gather`` and ``_decode``: K, V [P, Hk, page, d] CUDA
     tensors in float16, bfloat16, int8 or float8_e4m3fn, and for the last two dK, dV float32
     [P, Hk, page], one scale per row.  Each page is dense; pages may lie further apart (a slice of a
@@ -820,6 +798,9 @@ class PagedCache:
         return PagedCache(K, V, dK, dV)
 
 
+# tilemix_paged_cache: format, pages, page_size, heads_kv, head_dim, batch, max_pages; stride_k, _v, _dk, _dv,
+# _table; K, V, dK, dV, page_table, seqlens_k.  Packed in one go: a decode step is a few microseconds.
+_PAGED = struct.Struct("<7i4x5q6Q")
 _FORMATS: dict = {}
 
 
@@ -831,18 +812,13 @@ def _format(dtype) -> int:
     return _FORMATS.get(dtype, -1)
 
 
-def _outer_stride(t, dims: int, name: str) -> int:
-    """Elements between the entries of t's first dimension; its last ``dims`` dimensions must be dense (the
-    stride of a dimension of size 1 means nothing)."""
-    inner = 1
-    for i in range(1, dims + 1):
-        if t.shape[-i] != 1 and t.stride(-i) != inner:
-            raise ValueError(f"{name}: the last {dims} dimensions must be dense")
-        inner *= t.shape[-i]
-    return inner if t.shape[0] == 1 else t.stride(0)
-
-
 def _require_like(t, dtype, shape, device, name):
+    """A CUDA tensor of this type and shape on this device (an index)."""
+    try:
+        if t.dtype == dtype and t.shape == shape and t.get_device() == device:
+            return
+    except AttributeError:
+        pass
     import torch
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA (HIP) tensor")
@@ -850,79 +826,102 @@ def _require_like(t, dtype, shape, device, name):
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    if t.get_device() != device:
-        raise ValueError(f"{name} must be on the pool's device")
+    raise ValueError(f"{name} must be on the pool's device")
 
 
-def _paged_c(cache: PagedCache, page_table, seqlens_k) -> _CPagedCache:
+def _require_dense(t, dtype, shape, device, name):
+    _require_like(t, dtype, shape, device, name)
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+
+
+def _outer_stride(shape, stride, dims: int, name: str) -> int:
+    """Elements between the entries of the dimension before the last ``dims``, which must be dense (the stride
+    of a dimension of size 1 means nothing)."""
+    inner = 1
+    for i in range(1, dims + 1):
+        if shape[-i] != 1 and stride[-i] != inner:
+            raise ValueError(f"{name}: the last {dims} dimensions must be dense")
+        inner *= shape[-i]
+    return inner if shape[-dims - 1] == 1 else stride[-dims - 1]
+
+
+def _paged(cache: PagedCache, page_table, seqlens_k):
+    """(tilemix_paged_cache as bytes, format, device index, B, Hk, d)."""
     import torch
-    K, V = cache.K, cache.V
+    K, V, dK, dV = cache
     if not isinstance(K, torch.Tensor) or not K.is_cuda:
         raise TypeError("the pool's K must be a CUDA (HIP) tensor")
-    fmt = _format(K.dtype)
+    dtype, shape, dev = K.dtype, K.shape, K.get_device()
+    fmt = _format(dtype)
     if fmt < 0:
-        raise TypeError(f"the pool must be float16, bfloat16, int8 or float8_e4m3fn, got {K.dtype}")
-    if K.dim() != 4:
-        raise ValueError(f"the pool's K must be [pages, Hk, page, d], got {tuple(K.shape)}")
-    dev = K.get_device()
-    P, Hk, page, d = K.shape
-    _require_like(V, K.dtype, K.shape, dev, "the pool's V")
-    c = _CPagedCache(fmt, P, page, Hk, d)
-    c.stride_k, c.stride_v = _outer_stride(K, 3, "the pool's K"), _outer_stride(V, 3, "the pool's V")
-    c.K, c.V = K.data_ptr(), V.data_ptr()
+        raise TypeError(f"the pool must be float16, bfloat16, int8 or float8_e4m3fn, got {dtype}")
+    if len(shape) != 4:
+        raise ValueError(f"the pool's K must be [pages, Hk, page, d], got {tuple(shape)}")
+    _require_like(V, dtype, shape, dev, "the pool's V")
+    sk, sv = _outer_stride(shape, K.stride(), 3, "the pool's K"), _outer_stride(shape, V.stride(), 3, "the pool's V")
+    sdk = sdv = pdk = pdv = 0
     if fmt >= 2:
-        _require_like(cache.dK, torch.float32, K.shape[:3], dev, "the pool's dK")
-        _require_like(cache.dV, torch.float32, K.shape[:3], dev, "the pool's dV")
-        c.stride_dk, c.stride_dv = _outer_stride(cache.dK, 2, "the pool's dK"), _outer_stride(cache.dV, 2, "the pool's dV")
-        c.dK, c.dV = cache.dK.data_ptr(), cache.dV.data_ptr()
-    if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2:
+        rows = shape[:3]
+        _require_like(dK, torch.float32, rows, dev, "the pool's dK")
+        _require_like(dV, torch.float32, rows, dev, "the pool's dV")
+        sdk, sdv = _outer_stride(rows, dK.stride(), 2, "the pool's dK"), _outer_stride(rows, dV.stride(), 2, "the pool's dV")
+        pdk, pdv = dK.data_ptr(), dV.data_ptr()
+    if getattr(page_table, "ndim", None) != 2:
         raise ValueError("page_table must be a tensor [B, max_pages]")
-    _require_like(page_table, torch.int32, page_table.shape, dev, "page_table")
-    c.batch, c.max_pages = page_table.shape
-    c.stride_table = _outer_stride(page_table, 1, "page_table")
-    c.page_table = page_table.data_ptr()
-    _require_like(seqlens_k, torch.int32, page_table.shape[:1], dev, "seqlens_k")
-    if not seqlens_k.is_contiguous():
-        raise ValueError("seqlens_k must be contiguous")
-    c.seqlens_k = seqlens_k.data_ptr()
-    return c
+    t_shape = page_table.shape
+    _require_like(page_table, torch.int32, t_shape, dev, "page_table")
+    B, per = t_shape
+    _require_dense(seqlens_k, torch.int32, (B,), dev, "seqlens_k")
+    P, Hk, page, d = shape
+    return _PAGED.pack(fmt, P, page, Hk, d, B, per, sk, sv, sdk, sdv,
+                       _outer_stride(t_shape, page_table.stride(), 1, "page_table"), K.data_ptr(), V.data_ptr(), pdk, pdv,
+                       page_table.data_ptr(), seqlens_k.data_ptr()), fmt, dev, B, Hk, d
 
 
-def _paged_rows(c: _CPagedCache, cu_seqlens, max_len, total, device):
-    """(cu_seqlens pointer, len, total, shape of the rows) of an append or gather."""
+def _paged_rows(cu_seqlens, max_len, total, device, B, Hk, d):
+    """(cu_seqlens pointer, total, shape of the rows) of an append or gather."""
     if cu_seqlens is None:
-        return None, max_len, c.batch * max_len, (c.batch, max_len, c.heads_kv, c.head_dim)
+        return None, B * max_len, (B, max_len, Hk, d)
     import torch
-    _require_like(cu_seqlens, torch.int32, (c.batch + 1,), device, "cu_seqlens")
-    if not cu_seqlens.is_contiguous():
-        raise ValueError("cu_seqlens must be contiguous")
-    return cu_seqlens.data_ptr(), max_len, total, (total, c.heads_kv, c.head_dim)
+    _require_dense(cu_seqlens, torch.int32, (B + 1,), device, "cu_seqlens")
+    return cu_seqlens.data_ptr(), total, (total, Hk, d)
 
 
-def _row_stride(t, c: _CPagedCache, name: str) -> int:
+def _row_stride(t, shape, name: str) -> int:
     """Elements between the token rows of t, [total, Hk, d] or [B, len, Hk, d]."""
-    if t.dim() == 3:
-        return _outer_stride(t, 2, name)
-    B, L = t.shape[:2]
-    if B * L == 0:
-        return c.heads_kv * c.head_dim
-    row = _outer_stride(t[:, 0] if L == 1 else t[0], 2, name)
-    if B > 1 and L > 1 and t.stride(0) != L * row:
+    stride = t.stride()
+    if len(shape) == 3:
+        return _outer_stride(shape, stride, 2, name)
+    B, L, Hk, d = shape
+    if L == 1:   # one row per sequence: they are as far apart as the sequences
+        return _outer_stride((B, Hk, d), (stride[0], stride[2], stride[3]), 2, name)
+    row = _outer_stride(shape, stride, 2, name)
+    if B > 1 and L > 1 and stride[0] != L * row:
         raise ValueError(f"{name}: the rows of all sequences must be equally far apart")
     return row
 
 
-def _on_device(device: int):
-    """The library launches on the current device: make it the tensors' one."""
-    import contextlib
-    import torch
-    return contextlib.nullcontext() if torch.cuda.current_device() == device else torch.cuda.device(device)
+class _OnDevice:
+    """The library launches on the current device: the tensors' one is made that for a call.  stream: the handle."""
 
+    def __init__(self, device: int, stream):
+        import torch
+        self.other = None
+        if torch._C._cuda_getDevice() != device:
+            self.other = torch.cuda.device(device)
+        if stream is not None and stream.device_index != device:
+            raise ValueError("stream must be on the pool's device")
+        self.stream = torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
 
-def _stream_on(stream, device: int) -> int:
-    if stream is not None and stream.device_index != device:
-        raise ValueError("stream must be on the pool's device")
-    return _stream(stream)
+    def __enter__(self):
+        if self.other is not None:
+            self.other.__enter__()
+        return self.stream
+
+    def __exit__(self, *args):
+        if self.other is not None:
+            self.other.__exit__(*args)
 
 
 def tilemix_paged_append(cache: PagedCache, K, V, page_table, seqlens_k, cu_seqlens=None,
@@ -932,25 +931,27 @@ def tilemix_paged_append(cache: PagedCache, K, V, page_table, seqlens_k, cu_seql
     ``cu_seqlens`` (int32 CUDA [B + 1]) and ``max_len`` >= the most rows of a sequence, or
     [B, L, Hk, d], L rows for each sequence (1: a decode step).  Tokens may lie any multiple of 8 elements
     apart.  page_table: int32 CUDA [B, max_pages]; ids outside the pool name no page."""
-    c = _paged_c(cache, page_table, seqlens_k)
-    dev = cache.K.get_device()
+    c, _, dev, B, Hk, d = _paged(cache, page_table, seqlens_k)
     packed = cu_seqlens is not None
     if getattr(K, "ndim", None) != (3 if packed else 4):
         raise ValueError("K and V must be [total, Hk, d] with cu_seqlens, and [B, L, Hk, d] without")
-    if packed and max_len is None:
-        raise ValueError("max_len is needed with cu_seqlens")
-    if not packed and max_len not in (None, K.shape[1]):
+    if packed:
+        if max_len is None:
+            raise ValueError("max_len is needed with cu_seqlens")
+    elif max_len is None:
+        max_len = K.shape[1]
+    elif max_len != K.shape[1]:
         raise ValueError("max_len is the rows of K without cu_seqlens")
-    cu, length, total, shape = _paged_rows(c, cu_seqlens, max_len if packed else K.shape[1], K.shape[0], dev)
+    cu, total, shape = _paged_rows(cu_seqlens, max_len, K.shape[0], dev, B, Hk, d)
     dtype = K.dtype
-    if _format(dtype) not in (0, 1):
+    fmt = _format(dtype)
+    if fmt not in (0, 1):
         raise TypeError(f"K must be float16 or bfloat16, got {dtype}")
     _require_like(K, dtype, shape, dev, "K")
     _require_like(V, dtype, shape, dev, "V")
-    ks, vs = _row_stride(K, c, "K"), _row_stride(V, c, "V")
-    with _on_device(dev):
-        _check(load_library().tilemix_paged_append(ctypes.byref(c), _format(dtype), cu, length, total, K.data_ptr(), ks,
-                                                   V.data_ptr(), vs, _stream_on(stream, dev)))
+    with _OnDevice(dev, stream) as handle:
+        _check(load_library().tilemix_paged_append(c, fmt, cu, max_len, total, K.data_ptr(), _row_stride(K, shape, "K"),
+                                                   V.data_ptr(), _row_stride(V, shape, "V"), handle))
 
 
 def tilemix_paged_gather(cache: PagedCache, page_table, seqlens_k, max_len: int, cu_seqlens=None,
@@ -962,34 +963,34 @@ def tilemix_paged_gather(cache: PagedCache, page_table, seqlens_k, max_len: int,
     tilemix_prefill_varlen.  Tokens that the cache does not hold are zeros; packed rows that no sequence
     owns are not written."""
     import torch
-    c = _paged_c(cache, page_table, seqlens_k)
-    dev = cache.K.get_device()
+    c, pool, dev, B, Hk, d = _paged(cache, page_table, seqlens_k)
     if dtype is None:
-        dtype = K.dtype if K is not None else cache.K.dtype if c.format < 2 else torch.float16
-    if _format(dtype) not in (0, 1):
+        dtype = K.dtype if K is not None else cache.K.dtype if pool < 2 else torch.float16
+    fmt = _format(dtype)
+    if fmt not in (0, 1):
         raise TypeError(f"dtype must be float16 or bfloat16, got {dtype}")
     if cu_seqlens is not None and total is None:
         if K is None:
             raise ValueError("total is needed with cu_seqlens")
         total = K.shape[0]
-    if cu_seqlens is None and total not in (None, c.batch * max_len):
+    if cu_seqlens is None and total not in (None, B * max_len):
         raise ValueError("total is B * max_len without cu_seqlens")
-    cu, length, total, shape = _paged_rows(c, cu_seqlens, max_len, total, dev)
-    with _on_device(dev):
-        out = [_alloc(stream, shape, dtype=dtype, device=cache.K.device) if t is None else t for t in (K, V)]
-        for t, name in zip(out, ("K", "V")):
-            _require_like(t, dtype, shape, dev, name)
-            if not t.is_contiguous():
-                raise ValueError(f"{name} must be contiguous")
-        _check(load_library().tilemix_paged_gather(ctypes.byref(c), _format(dtype), cu, length, total,
-                                                   out[0].data_ptr(), out[1].data_ptr(), _stream_on(stream, dev)))
-    return out[0], out[1]
+    cu, total, shape = _paged_rows(cu_seqlens, max_len, total, dev, B, Hk, d)
+    with _OnDevice(dev, stream) as handle:
+        if K is None:
+            K = _alloc(stream, shape, dtype=dtype, device=cache.K.device)
+        if V is None:
+            V = _alloc(stream, shape, dtype=dtype, device=cache.K.device)
+        _require_dense(K, dtype, shape, dev, "K")
+        _require_dense(V, dtype, shape, dev, "V")
+        _check(load_library().tilemix_paged_gather(c, fmt, cu, max_len, total, K.data_ptr(), V.data_ptr(), handle))
+    return K, V
 
 
 def tilemix_paged_decode_workspace_size(cache: PagedCache, page_table, seqlens_k, heads_q: int) -> int:
     n = ctypes.c_size_t(0)
-    _check(load_library().tilemix_paged_decode_workspace_size(ctypes.byref(_paged_c(cache, page_table, seqlens_k)),
-                                                              heads_q, ctypes.byref(n)))
+    _check(load_library().tilemix_paged_decode_workspace_size(_paged(cache, page_table, seqlens_k)[0], heads_q,
+                                                              ctypes.byref(n)))
     return n.value
 
 
@@ -1001,38 +1002,36 @@ def tilemix_paged_decode(cache: PagedCache, Q, page_table, seqlens_k, scale: flo
     the sum of e^score.  A sequence without a token gets O = 0 and lse = -inf.  ``O``, ``lse`` and ``workspace``
     (uint8, >= tilemix_paged_decode_workspace_size) are allocated when not given."""
     import torch
-    c = _paged_c(cache, page_table, seqlens_k)
-    dev = cache.K.get_device()
+    c, _, dev, B, Hk, d = _paged(cache, page_table, seqlens_k)
     if getattr(Q, "ndim", None) != 4:
         raise ValueError("Q must be [B, 1, Hq, d]")
     dtype = Q.dtype
-    if _format(dtype) not in (0, 1):
+    fmt = _format(dtype)
+    if fmt not in (0, 1):
         raise TypeError(f"Q must be float16 or bfloat16, got {dtype}")
-    shape = (c.batch, 1, Q.shape[2], c.head_dim)
+    heads = Q.shape[2]
+    shape = (B, 1, heads, d)
     _require_like(Q, dtype, shape, dev, "Q")
-    heads = shape[2]
-    q_stride = _outer_stride(Q[:, 0], 2, "Q")
-    with _on_device(dev):
+    q_stride = _row_stride(Q, shape, "Q")
+    lib = load_library()
+    with _OnDevice(dev, stream) as handle:
         if O is None:
             O = _alloc(stream, shape, dtype=dtype, device=Q.device)
         else:
-            _require_like(O, dtype, shape, dev, "O")
-            if not O.is_contiguous():
-                raise ValueError("O must be contiguous")
+            _require_dense(O, dtype, shape, dev, "O")
         if lse is not None:
-            _require_like(lse, torch.float32, (c.batch, heads), dev, "lse")
-            if not lse.is_contiguous():
-                raise ValueError("lse must be contiguous")
+            _require_dense(lse, torch.float32, (B, heads), dev, "lse")
         elif return_lse:
-            lse = _alloc(stream, (c.batch, heads), dtype=torch.float32, device=Q.device)
+            lse = _alloc(stream, (B, heads), dtype=torch.float32, device=Q.device)
         if workspace is None:
             n = ctypes.c_size_t(0)
-            _check(load_library().tilemix_paged_decode_workspace_size(ctypes.byref(c), heads, ctypes.byref(n)))
+            _check(lib.tilemix_paged_decode_workspace_size(c, heads, ctypes.byref(n)))
             nbytes = n.value
-            workspace = _alloc(stream, nbytes, dtype=torch.uint8, device=Q.device) if nbytes else None
+            if nbytes:
+                workspace = _alloc(stream, nbytes, dtype=torch.uint8, device=Q.device)
         else:
             nbytes = workspace.numel() * workspace.element_size()
-        _check_call(load_library().tilemix_paged_decode(
-            ctypes.byref(c), _format(dtype), heads, scale if scale is not None else 1.0 / math.sqrt(c.head_dim), window,
-            Q.data_ptr(), q_stride, O.data_ptr(), _ptr(lse), _ptr(workspace), nbytes, _stream_on(stream, dev)))
+        _check_call(lib.tilemix_paged_decode(
+            c, fmt, heads, scale if scale is not None else 1.0 / math.sqrt(d), window, Q.data_ptr(), q_stride, O.data_ptr(),
+            _ptr(lse), _ptr(workspace), nbytes, handle))
     return (O, lse) if return_lse else O

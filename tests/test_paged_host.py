@@ -2,6 +2,7 @@
 
 import ctypes
 import os
+import re
 
 import pytest
 import torch
@@ -15,26 +16,42 @@ OK = 0x100000
 NULL, SHAPE, UNSUPPORTED, ALIGN, WORKSPACE = 1, 2, 3, 4, 5
 
 
+class CPagedCache(ctypes.Structure):
+    """tilemix_paged_cache, as the header declares it."""
+    _fields_ = ([(n, ctypes.c_int32) for n in ("format", "pages", "page_size", "heads_kv", "head_dim", "batch", "max_pages")] +
+                [(n, ctypes.c_int64) for n in ("stride_k", "stride_v", "stride_dk", "stride_dv", "stride_table")] +
+                [(n, ctypes.c_void_p) for n in ("K", "V", "dK", "dV", "page_table", "seqlens_k")])
+
+
 def _cache(**kw):
     base = dict(format=2, pages=10, page_size=64, heads_kv=8, head_dim=128, batch=3, max_pages=5,
                 stride_k=8 * 64 * 128, stride_v=8 * 64 * 128, stride_dk=512, stride_dv=512, stride_table=5,
                 K=OK, V=OK, dK=OK, dV=OK, page_table=OK, seqlens_k=OK)
     base.update(kw)
-    return tm._CPagedCache(**base)
+    return bytes(CPagedCache(**base))
+
+
+def test_packed_struct_is_the_headers():
+    names = [n for n, _ in CPagedCache._fields_]
+    text = open(os.path.join(os.path.dirname(tm.library_path()), "..", "include", "tilemix.h")).read()
+    body = re.sub(r"/\*.*?\*/", "", text, flags=re.S).split("typedef struct tilemix_paged_cache {")[1].split("}")[0]
+    assert re.findall(r"(\w+)\s*[,;]", body) == names
+    values = list(range(3, 3 + len(names)))
+    assert tm._PAGED.pack(*values) == bytes(CPagedCache(*values))
 
 
 def _append(cache, type=0, cu=OK, length=7, total=20, K=OK, ks=1024, V=OK, vs=1024):
-    return tm.load_library().tilemix_paged_append(ctypes.byref(cache) if cache else None, type, cu, length, total, K, ks,
+    return tm.load_library().tilemix_paged_append(cache, type, cu, length, total, K, ks,
                                                   V, vs, None)
 
 
 def _gather(cache, type=0, cu=OK, length=7, total=20, K=OK, V=OK):
-    return tm.load_library().tilemix_paged_gather(ctypes.byref(cache) if cache else None, type, cu, length, total, K, V,
+    return tm.load_library().tilemix_paged_gather(cache, type, cu, length, total, K, V,
                                                   None)
 
 
 def _decode(cache, type=0, heads=32, scale=0.1, window=0, Q=OK, qs=4096, O=OK, lse=None, ws=OK, nbytes=1 << 40):
-    return tm.load_library().tilemix_paged_decode(ctypes.byref(cache) if cache else None, type, heads, scale, window, Q,
+    return tm.load_library().tilemix_paged_decode(cache, type, heads, scale, window, Q,
                                                   qs, O, lse, ws, nbytes, None)
 
 
@@ -66,7 +83,7 @@ def test_null_cache_and_types():
         assert call(_cache(format=1), type=0) == UNSUPPORTED     # a 16-bit pool and rows of another type
         assert call(_cache(format=0), type=1) == UNSUPPORTED
     assert tm.load_library().tilemix_paged_decode_workspace_size(None, 32, None) == NULL
-    assert tm.load_library().tilemix_paged_decode_workspace_size(ctypes.byref(_cache()), 32, None) == NULL
+    assert tm.load_library().tilemix_paged_decode_workspace_size(_cache(), 32, None) == NULL
 
 
 def test_16bit_pools_need_no_scales():
