@@ -410,9 +410,10 @@ typedef struct tilemix_paged_cache {
  *   cu_seqlens   device int32 [B + 1] as for tilemix_prefill_varlen: sequence b brings rows
  *                cu_seqlens[b] .. cu_seqlens[b + 1] - 1 of the packed K_new, V_new [total, H_k, d];
  *                or NULL: each brings len rows, K_new, V_new [B, len, H_k, d]
- *   len          the most new rows of a sequence, 1 .. 2^23 (1: one decode step); rows past it
+ *   len          the most new rows of a sequence, 1 .. 2^28 (1: one decode step); rows past it
  *                are not written
- *   total        rows of K_new and V_new, >= 0; B * len without cu_seqlens
+ *   total        rows of K_new and V_new, 0 .. 2^28, total * H_k * d <= 2^34; B * len without
+ *                cu_seqlens
  *   K_new, V_new device, 16-byte aligned, read only; rows of H_k * d elements, k_stride / v_stride
  *                elements apart (>= 0, multiples of 8: a slice of a fused projection needs no copy)
  * Rows whose token number is negative or past max_pages * page_size are not written, nor are

@@ -19,7 +19,9 @@ tilemix_status hip_status(hipError_t e, const char* what) {
 bool is_8bit(int32_t format) { return format == TILEMIX_INT8 || format == TILEMIX_E4M3; }
 
 constexpr long long kStrideMax = 1LL << 40;
-constexpr int32_t kLenMax = 1 << 23;   // a workgroup a row: 2^31 threads along the grid's x
+// Packed rows, and elements of them: a launch has at most 2^23 workgroups of 256 threads, and one more for each sequence.
+constexpr int32_t kRowsMax = 1 << 28;
+constexpr long long kRowElementsMax = 1LL << 34;
 
 // Sizes, strides and formats of the pool and its sequences (no pointers).
 tilemix_status check_shape(const tilemix_paged_cache* c) {
@@ -91,8 +93,10 @@ tilemix_status rows_args(const tilemix_paged_cache* c, int32_t type, const int32
   tilemix_status st = check_shape(c);
   if (st != TILEMIX_OK) return st;
   if ((st = check_type(c, type)) != TILEMIX_OK) return st;
-  if (len < 1 || len > kLenMax) return fail(TILEMIX_ERR_SHAPE, "len must be 1 .. %d", kLenMax);
-  if (total < 0) return fail(TILEMIX_ERR_SHAPE, "total must be >= 0");
+  if (len < 1 || len > kRowsMax) return fail(TILEMIX_ERR_SHAPE, "len must be 1 .. %d", kRowsMax);
+  if (total < 0 || total > kRowsMax) return fail(TILEMIX_ERR_SHAPE, "total must be 0 .. %d", kRowsMax);
+  if ((long long)total * c->heads_kv * c->head_dim > kRowElementsMax)
+    return fail(TILEMIX_ERR_SHAPE, "total * heads_kv * head_dim must be <= 2^34");
   if (!cu && total != (long long)c->batch * len) return fail(TILEMIX_ERR_SHAPE, "total must be batch * len without cu_seqlens");
   if (k_stride < 0 || v_stride < 0 || k_stride > kStrideMax || v_stride > kStrideMax || k_stride % 8 || v_stride % 8)
     return fail(TILEMIX_ERR_SHAPE, "row strides must be >= 0 and multiples of 8");

@@ -54,48 +54,53 @@ __device__ __forceinline__ Slot find_slot(const PagedPool& p, int b, long long t
   return {page >= 0 && page < p.pages ? page : -1, (int)(t & ((1 << p.page_shift) - 1))};
 }
 
-// The rule that makes the codes of a row with a = max |x| > 0, finite: the exact quotient top x / a, rounded
-// once.  Both are scaled by the same power of two so that a lies in [1, 2) (nothing over- or underflows,
-// subnormal rows included); m x is then exact in FP32 (m = 127, or 7 = 448 / 64: at most 18 bits), and
-// m x * (1 / a) after one residual step is the correctly rounded quotient.  A quotient of two numbers of
-// at most 11 bits that is no tie of the code's grid is further from one than 2^-23 of itself, so rounding
-// it again, to the code, gives the code of the exact quotient (checked for every such pair).
+// The rule that makes the codes of a row with a = max |x| > 0, finite: the exact quotient top x / a, rounded once.
+// Both are scaled by one power of two, 2^e, so that nothing overflows and a loses no bits (subnormal rows
+// included).  t = m 2^e x is then exact in FP32 (m = 127, or 7 = 448 / 64: at most 18 bits), and so is the
+// residual t - q0 a of an estimate q0, so that q = q0 + (t - q0 a) r with r within 2^-22 of 1 / a is the correctly
+// rounded quotient: it errs by 2^-44 of it before it is rounded, and a quotient of 18 by 11 bits is no
+// nearer than 2^-36 to the midpoint of two FP32 numbers.  Such a quotient that is no tie of the codes' grid is
+// further from one than 2^-23 of itself, so rounding q again, to the code, gives the code of the exact
+// quotient (checked for every pair of such numbers).
 template <int FORMAT>
 struct RowScale {
-  int exp;          // x is taken times 2^exp
-  float a, rcp;
+  float a, rcp;     // 2^e a and its reciprocal
+  float m;          // m 2^e
   float scale;      // as stored
   bool plain;       // a > 0 and finite: otherwise all codes are 0
   // amax: bits of max |x| of a row of TYPE.
   template <int TYPE>
   __device__ __forceinline__ static RowScale of(uint32_t amax) {
     RowScale r;
-    const float m = bits_to_float<TYPE>(amax);
+    const float x = bits_to_float<TYPE>(amax);
     const bool finite = amax < Elem<TYPE>::kInf;
     r.plain = finite && amax > 0;
-    r.scale = finite ? m / kTop<FORMAT> : __builtin_nanf("");   // IEEE division
-    r.exp = r.plain ? 1 - __builtin_amdgcn_frexp_expf(m) : 0;
-    r.a = r.plain ? __builtin_amdgcn_ldexpf(m, r.exp) : 1.0f;
-    r.rcp = 1.0f / r.a;
+    r.scale = finite ? x / kTop<FORMAT> : __builtin_nanf("");   // IEEE division
+    // a in [1, 2); for rows below 2^-118 (BF16) less, down to 2^-14, since m 2^e has to be finite.
+    const int e = r.plain ? min(1 - __builtin_amdgcn_frexp_expf(x), 119) : 0;
+    r.a = r.plain ? __builtin_amdgcn_ldexpf(x, e) : 1.0f;
+    r.rcp = __builtin_amdgcn_rcpf(r.a);
+    r.m = __builtin_amdgcn_ldexpf(FORMAT == TILEMIX_INT8 ? 127.0f : 7.0f, e);
     return r;
   }
   // top x / a, INT8 in units of 1 and E4M3 in units of 64 (a power of two: exact either way).
   __device__ __forceinline__ float quot(float x) const {
-    const float t = __builtin_amdgcn_ldexpf(x, exp) * (FORMAT == TILEMIX_INT8 ? 127.0f : 7.0f);
-    return quotient(t, a, rcp);
+    const float t = x * m, q0 = t * rcp;
+    return fmaf(fmaf(-q0, a, t), rcp, q0);
   }
   // Codes of four values as bytes, the first lowest.
   __device__ __forceinline__ uint32_t codes(float x0, float x1, float x2, float x3) const {
-    if (!plain) return 0u;
     const float q0 = quot(x0), q1 = quot(x1), q2 = quot(x2), q3 = quot(x3);
+    uint32_t w;
     if constexpr (FORMAT == TILEMIX_INT8) {
       auto word = [](float q) { return __builtin_bit_cast(uint32_t, q + 12582912.0f); };
-      return pack4(word(q0), word(q1), word(q2), word(q3));
+      w = pack4(word(q0), word(q1), word(q2), word(q3));
     } else {
       // |q| <= 7 (1 + 2^-24), which 448 absorbs: the conversion never saturates.
-      int w = __builtin_amdgcn_cvt_pk_fp8_f32(64.0f * q0, 64.0f * q1, 0, false);
-      return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(64.0f * q2, 64.0f * q3, w, true);
+      w = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(64.0f * q0, 64.0f * q1, 0, false);
+      w = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(64.0f * q2, 64.0f * q3, (int)w, true);
     }
+    return plain ? w : 0u;
   }
 };
 

@@ -186,7 +186,8 @@ struct PagedRowsArgs {
   void* K;                 // packed rows: read by append, written by gather
   void* V;
   long long k_stride, v_stride;   // elements between rows
-  int tile_shift;          // filled in by the launch: log2 of the tokens of a workgroup
+  int tile_shift;          // filled in by the launch: log2 of a workgroup's tokens
+  FastDiv div_tiles;       // filled in by the launch: tiles of len rows
 };
 hipError_t launch_paged_append(PagedRowsArgs args, int d, int type, int format, hipStream_t stream);
 hipError_t launch_paged_gather(PagedRowsArgs args, int d, int type, int format, hipStream_t stream);

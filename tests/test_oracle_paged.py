@@ -93,4 +93,4 @@ def test_row_quotient_is_exact(tmp_path):
     out = subprocess.run([str(exe)], capture_output=True, text=True, timeout=300)
     assert out.returncode == 0, out.stdout + out.stderr
     assert "mismatches 0 wrong_codes 0" in out.stdout
-    assert int(out.stdout.split()[1]) > 5 * 10 ** 7
+    assert int(out.stdout.split()[1]) > 25 * 10 ** 7

@@ -95,8 +95,10 @@ def test_16bit_pools_need_no_scales():
 def test_rows_refusals():
     for call in (_append, _gather):
         assert call(_cache(), length=0) == SHAPE
-        assert call(_cache(), length=(1 << 23) + 1) == SHAPE
+        assert call(_cache(), length=(1 << 28) + 1) == SHAPE
         assert call(_cache(), total=-1) == SHAPE
+        assert call(_cache(), total=(1 << 28) + 1) == SHAPE
+        assert call(_cache(), total=(1 << 24) + 1) == SHAPE            # x 8 heads x 128 channels
         assert call(_cache(), cu=None, length=7, total=20) == SHAPE    # not batch * len
         assert call(_cache(), cu=OK + 2) == ALIGN
         assert call(_cache(), K=None) == NULL
