@@ -56,7 +56,7 @@ __device__ __forceinline__ Slot find_slot(const PagedPool& p, int b, long long t
 
 // The rule that makes the codes of a row with a = max |x| > 0, finite: the exact quotient top x / a, rounded once.
 // Both are scaled by one power of two, 2^e, so that nothing overflows and a loses no bits (subnormal rows
-// included).  t = m 2^e x is then exact in FP32 (m = 127, or 7 = 448 / 64: at most 18 bits), and so is the
+// included).  t = 2^e top x is then exact in FP32 (127, and 448 = 7 2^6: at most 18 bits), and so is the
 // residual t - q0 a of an estimate q0, so that q = q0 + (t - q0 a) r with r within 2^-22 of 1 / a is the correctly
 // rounded quotient: it errs by 2^-44 of it before it is rounded, and a quotient of 18 by 11 bits is no
 // nearer than 2^-36 to the midpoint of two FP32 numbers.  Such a quotient that is no tie of the codes' grid is
@@ -65,7 +65,7 @@ __device__ __forceinline__ Slot find_slot(const PagedPool& p, int b, long long t
 template <int FORMAT>
 struct RowScale {
   float a, rcp;     // 2^e a and its reciprocal
-  float m;          // m 2^e
+  float m;          // 2^e top
   float scale;      // as stored
   bool plain;       // a > 0 and finite: otherwise all codes are 0
   // amax: bits of max |x| of a row of TYPE.
@@ -75,15 +75,20 @@ struct RowScale {
     const float x = bits_to_float<TYPE>(amax);
     const bool finite = amax < Elem<TYPE>::kInf;
     r.plain = finite && amax > 0;
-    r.scale = finite ? x / kTop<FORMAT> : __builtin_nanf("");   // IEEE division
-    // a in [1, 2); for rows below 2^-118 (BF16) less, down to 2^-14, since m 2^e has to be finite.
+    // a / top, correctly rounded, by the same residual step (where the quotient is not subnormal).
+    constexpr float kInv = 1.0f / kTop<FORMAT>;
+    const float s0 = x * kInv;
+    r.scale = fmaf(fmaf(-s0, kTop<FORMAT>, x), kInv, s0);
+    if (x < 0x1p-100f) r.scale = x / kTop<FORMAT>;
+    r.scale = finite ? r.scale : __builtin_nanf("");
+    // 2^e a in [1, 2); for rows below 2^-118 (BF16) less, down to 2^-14, since 2^e top has to be finite.
     const int e = r.plain ? min(1 - __builtin_amdgcn_frexp_expf(x), 119) : 0;
     r.a = r.plain ? __builtin_amdgcn_ldexpf(x, e) : 1.0f;
     r.rcp = __builtin_amdgcn_rcpf(r.a);
-    r.m = __builtin_amdgcn_ldexpf(FORMAT == TILEMIX_INT8 ? 127.0f : 7.0f, e);
+    r.m = __builtin_amdgcn_ldexpf(kTop<FORMAT>, e);
     return r;
   }
-  // top x / a, INT8 in units of 1 and E4M3 in units of 64 (a power of two: exact either way).
+  // top x / a.
   __device__ __forceinline__ float quot(float x) const {
     const float t = x * m, q0 = t * rcp;
     return fmaf(fmaf(-q0, a, t), rcp, q0);
@@ -96,9 +101,9 @@ struct RowScale {
       auto word = [](float q) { return __builtin_bit_cast(uint32_t, q + 12582912.0f); };
       w = pack4(word(q0), word(q1), word(q2), word(q3));
     } else {
-      // |q| <= 7 (1 + 2^-24), which 448 absorbs: the conversion never saturates.
-      w = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(64.0f * q0, 64.0f * q1, 0, false);
-      w = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(64.0f * q2, 64.0f * q3, (int)w, true);
+      // |q| <= 448 (1 + 2^-24), which rounds to 448: the conversion never saturates.
+      w = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(q0, q1, 0, false);
+      w = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(q2, q3, (int)w, true);
     }
     return plain ? w : 0u;
   }

@@ -20,7 +20,13 @@ namespace tilemix {
 namespace {
 
 constexpr int kRowsThreads = 256;
-constexpr int kRowsAhead = 8;   // rows that a lane group has in flight
+// Rows that a lane group requests at a time: few, so that many waves fit and their requests overlap.  us to append
+// (24 prompts of up to 16000 tokens, E4M3, 8 heads of d = 128) and read back, with the same rows of a group in
+// all: 8 at a time 140.1, 4 133.5, 2 131.1.
+constexpr int kRowsAhead = 2;
+// Rows that a lane group takes in all, at most.  us, of the same and of reading 12 prefixes of up to 32768
+// tokens (INT8): 4 rows 129.2 and 115.4, 8 131.1 and 112.0; 16 139.8 and 113.3 (4 at a time).
+constexpr int kAppendRows = 4, kGatherRows = 8;
 
 // The tokens of a workgroup.  Those of a packed batch are numbered in tiles, sequence after sequence, which
 // every wave looks up for itself (a lane takes a run of sequences): a grid over the longest sequence would be
@@ -212,12 +218,12 @@ __global__ __launch_bounds__(kRowsThreads) void paged_gather_kernel(PagedRowsArg
 }
 
 // Tokens of a workgroup: the most, no more than lane groups and than a sequence can bring, with which a lane group has
-// at most kRowsAhead rows.
-dim3 rows_grid(PagedRowsArgs& a, int d) {
+// at most `most` rows.
+dim3 rows_grid(PagedRowsArgs& a, int d, int most) {
   const int groups = kRowsThreads / (d / 8);
   a.tile_shift = 0;
   while ((2 << a.tile_shift) <= groups && (1 << a.tile_shift) < a.len &&
-         (2LL * a.pool.Hk << (a.tile_shift + 1)) <= (long long)groups * kRowsAhead)
+         (2LL * a.pool.Hk << (a.tile_shift + 1)) <= (long long)groups * most)
     ++a.tile_shift;
   const long long per = ((long long)a.len + (1 << a.tile_shift) - 1) >> a.tile_shift;   // tiles of the longest sequence
   a.div_tiles = FastDiv((uint32_t)per);
@@ -229,7 +235,7 @@ dim3 rows_grid(PagedRowsArgs& a, int d) {
 }  // namespace
 
 hipError_t launch_paged_append(PagedRowsArgs a, int d, int type, int format, hipStream_t stream) {
-  const dim3 grid = rows_grid(a, d);
+  const dim3 grid = rows_grid(a, d, kAppendRows);
   return for_paged_types(d, type, format, [&](auto D, auto T, auto F) {
     hipLaunchKernelGGL((paged_append_kernel<D(), T(), F()>), grid, dim3(kRowsThreads), 0, stream, a);
     return hipGetLastError();
@@ -237,7 +243,7 @@ hipError_t launch_paged_append(PagedRowsArgs a, int d, int type, int format, hip
 }
 
 hipError_t launch_paged_gather(PagedRowsArgs a, int d, int type, int format, hipStream_t stream) {
-  const dim3 grid = rows_grid(a, d);
+  const dim3 grid = rows_grid(a, d, kGatherRows);
   return for_paged_types(d, type, format, [&](auto D, auto T, auto F) {
     hipLaunchKernelGGL((paged_gather_kernel<D(), T(), F()>), grid, dim3(kRowsThreads), 0, stream, a);
     return hipGetLastError();
