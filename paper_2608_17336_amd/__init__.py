@@ -802,13 +802,21 @@ class PagedCache(NamedTuple):
 # _table; K, V, dK, dV, page_table, seqlens_k.  Packed in one go: a decode step is a few microseconds.
 _PAGED = struct.Struct("<7i4x5q6Q")
 _FORMATS: dict = {}
+_TORCH = None
+
+
+def _torch():
+    """torch, imported once (an import statement costs 0.3 us each time it is met)."""
+    global _TORCH
+    if _TORCH is None:
+        import torch
+        _FORMATS.update({torch.float16: 0, torch.bfloat16: 1, torch.int8: 2, torch.float8_e4m3fn: 3})
+        _TORCH = torch
+    return _TORCH
 
 
 def _format(dtype) -> int:
     """tilemix_format of a torch dtype, or -1."""
-    if not _FORMATS:
-        import torch
-        _FORMATS.update({torch.float16: 0, torch.bfloat16: 1, torch.int8: 2, torch.float8_e4m3fn: 3})
     return _FORMATS.get(dtype, -1)
 
 
@@ -848,7 +856,7 @@ def _outer_stride(shape, stride, dims: int, name: str) -> int:
 
 def _paged(cache: PagedCache, page_table, seqlens_k):
     """(tilemix_paged_cache as bytes, format, device index, B, Hk, d)."""
-    import torch
+    torch = _torch()
     K, V, dK, dV = cache
     if not isinstance(K, torch.Tensor) or not K.is_cuda:
         raise TypeError("the pool's K must be a CUDA (HIP) tensor")
@@ -883,8 +891,7 @@ def _paged_rows(cu_seqlens, max_len, total, device, B, Hk, d):
     """(cu_seqlens pointer, total, shape of the rows) of an append or gather."""
     if cu_seqlens is None:
         return None, B * max_len, (B, max_len, Hk, d)
-    import torch
-    _require_dense(cu_seqlens, torch.int32, (B + 1,), device, "cu_seqlens")
+    _require_dense(cu_seqlens, _torch().int32, (B + 1,), device, "cu_seqlens")
     return cu_seqlens.data_ptr(), total, (total, Hk, d)
 
 
@@ -902,26 +909,20 @@ def _row_stride(t, shape, name: str) -> int:
     return row
 
 
-class _OnDevice:
-    """The library launches on the current device: the tensors' one is made that for a call.  stream: the handle."""
+def _stream_on(stream, device: int) -> int:
+    """The HIP stream as an integer: ``stream``, or the device's current one."""
+    if stream is None:
+        return _torch()._C._cuda_getCurrentRawStream(device)
+    if stream.device_index != device:
+        raise ValueError("stream must be on the pool's device")
+    return stream.cuda_stream
 
-    def __init__(self, device: int, stream):
-        import torch
-        self.other = None
-        if torch._C._cuda_getDevice() != device:
-            self.other = torch.cuda.device(device)
-        if stream is not None and stream.device_index != device:
-            raise ValueError("stream must be on the pool's device")
-        self.stream = torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
 
-    def __enter__(self):
-        if self.other is not None:
-            self.other.__enter__()
-        return self.stream
-
-    def __exit__(self, *args):
-        if self.other is not None:
-            self.other.__exit__(*args)
+def _elsewhere(device: int):
+    """The library launches on the current device.  None where that is the tensors' own, or a context in which
+    it is: the caller then calls itself again in it."""
+    torch = _torch()
+    return None if torch._C._cuda_getDevice() == device else torch.cuda.device(device)
 
 
 def tilemix_paged_append(cache: PagedCache, K, V, page_table, seqlens_k, cu_seqlens=None,
@@ -949,9 +950,12 @@ def tilemix_paged_append(cache: PagedCache, K, V, page_table, seqlens_k, cu_seql
         raise TypeError(f"K must be float16 or bfloat16, got {dtype}")
     _require_like(K, dtype, shape, dev, "K")
     _require_like(V, dtype, shape, dev, "V")
-    with _OnDevice(dev, stream) as handle:
-        _check(load_library().tilemix_paged_append(c, fmt, cu, max_len, total, K.data_ptr(), _row_stride(K, shape, "K"),
-                                                   V.data_ptr(), _row_stride(V, shape, "V"), handle))
+    other = _elsewhere(dev)
+    if other is not None:
+        with other:
+            return tilemix_paged_append(cache, K, V, page_table, seqlens_k, cu_seqlens, max_len, stream=stream)
+    _check(load_library().tilemix_paged_append(c, fmt, cu, max_len, total, K.data_ptr(), _row_stride(K, shape, "K"),
+                                               V.data_ptr(), _row_stride(V, shape, "V"), _stream_on(stream, dev)))
 
 
 def tilemix_paged_gather(cache: PagedCache, page_table, seqlens_k, max_len: int, cu_seqlens=None,
@@ -962,7 +966,7 @@ def tilemix_paged_gather(cache: PagedCache, page_table, seqlens_k, max_len: int,
     float16 by default for an 8-bit one), written into ``K`` and ``V`` if given: the K and V of
     tilemix_prefill_varlen.  Tokens that the cache does not hold are zeros; packed rows that no sequence
     owns are not written."""
-    import torch
+    torch = _torch()
     c, pool, dev, B, Hk, d = _paged(cache, page_table, seqlens_k)
     if dtype is None:
         dtype = K.dtype if K is not None else cache.K.dtype if pool < 2 else torch.float16
@@ -975,15 +979,22 @@ def tilemix_paged_gather(cache: PagedCache, page_table, seqlens_k, max_len: int,
         total = K.shape[0]
     if cu_seqlens is None and total not in (None, B * max_len):
         raise ValueError("total is B * max_len without cu_seqlens")
-    cu, total, shape = _paged_rows(cu_seqlens, max_len, total, dev, B, Hk, d)
-    with _OnDevice(dev, stream) as handle:
-        if K is None:
-            K = _alloc(stream, shape, dtype=dtype, device=cache.K.device)
-        if V is None:
-            V = _alloc(stream, shape, dtype=dtype, device=cache.K.device)
+    rows, total, shape = _paged_rows(cu_seqlens, max_len, total, dev, B, Hk, d)
+    other = _elsewhere(dev)
+    if other is not None:
+        with other:
+            return tilemix_paged_gather(cache, page_table, seqlens_k, max_len, cu_seqlens, total, dtype=dtype, K=K, V=V,
+                                        stream=stream)
+    handle = _stream_on(stream, dev)
+    if K is None:
+        K = _alloc(stream, shape, dtype=dtype, device=cache.K.device)
+    else:
         _require_dense(K, dtype, shape, dev, "K")
+    if V is None:
+        V = _alloc(stream, shape, dtype=dtype, device=cache.K.device)
+    else:
         _require_dense(V, dtype, shape, dev, "V")
-        _check(load_library().tilemix_paged_gather(c, fmt, cu, max_len, total, K.data_ptr(), V.data_ptr(), handle))
+    _check(load_library().tilemix_paged_gather(c, fmt, rows, max_len, total, K.data_ptr(), V.data_ptr(), handle))
     return K, V
 
 
@@ -1001,7 +1012,7 @@ def tilemix_paged_decode(cache: PagedCache, Q, page_table, seqlens_k, scale: flo
     last ``window`` >= 1.  Returns O, like Q, and with ``return_lse`` (O, lse): float32 [B, Hq], the log of
     the sum of e^score.  A sequence without a token gets O = 0 and lse = -inf.  ``O``, ``lse`` and ``workspace``
     (uint8, >= tilemix_paged_decode_workspace_size) are allocated when not given."""
-    import torch
+    torch = _torch()
     c, _, dev, B, Hk, d = _paged(cache, page_table, seqlens_k)
     if getattr(Q, "ndim", None) != 4:
         raise ValueError("Q must be [B, 1, Hq, d]")
@@ -1013,25 +1024,31 @@ def tilemix_paged_decode(cache: PagedCache, Q, page_table, seqlens_k, scale: flo
     shape = (B, 1, heads, d)
     _require_like(Q, dtype, shape, dev, "Q")
     q_stride = _row_stride(Q, shape, "Q")
-    lib = load_library()
-    with _OnDevice(dev, stream) as handle:
-        if O is None:
-            O = _alloc(stream, shape, dtype=dtype, device=Q.device)
-        else:
-            _require_dense(O, dtype, shape, dev, "O")
-        if lse is not None:
-            _require_dense(lse, torch.float32, (B, heads), dev, "lse")
-        elif return_lse:
-            lse = _alloc(stream, (B, heads), dtype=torch.float32, device=Q.device)
-        if workspace is None:
-            n = ctypes.c_size_t(0)
-            _check(lib.tilemix_paged_decode_workspace_size(c, heads, ctypes.byref(n)))
-            nbytes = n.value
-            if nbytes:
-                workspace = _alloc(stream, nbytes, dtype=torch.uint8, device=Q.device)
-        else:
-            nbytes = workspace.numel() * workspace.element_size()
-        _check_call(lib.tilemix_paged_decode(
-            c, fmt, heads, scale if scale is not None else 1.0 / math.sqrt(d), window, Q.data_ptr(), q_stride, O.data_ptr(),
-            _ptr(lse), _ptr(workspace), nbytes, handle))
+    other = _elsewhere(dev)
+    if other is not None:
+        with other:
+            return tilemix_paged_decode(cache, Q, page_table, seqlens_k, scale, window=window, O=O, lse=lse,
+                                        return_lse=return_lse, workspace=workspace, stream=stream)
+    handle, lib = _stream_on(stream, dev), load_library()
+    if O is None:
+        O = _alloc(stream, shape, dtype=dtype, device=Q.device)
+    else:
+        _require_dense(O, dtype, shape, dev, "O")
+    if lse is not None:
+        _require_dense(lse, torch.float32, (B, heads), dev, "lse")
+    elif return_lse:
+        lse = _alloc(stream, (B, heads), dtype=torch.float32, device=Q.device)
+    if workspace is None:
+        n = ctypes.c_size_t(0)
+        _check(lib.tilemix_paged_decode_workspace_size(c, heads, ctypes.byref(n)))
+        nbytes = n.value
+        if nbytes:
+            workspace = _alloc(stream, nbytes, dtype=torch.uint8, device=Q.device)
+    else:
+        if not isinstance(workspace, torch.Tensor) or workspace.get_device() != dev or not workspace.is_contiguous():
+            raise ValueError("workspace must be a contiguous tensor on the pool's device")
+        nbytes = workspace.numel() * workspace.element_size()
+    _check_call(lib.tilemix_paged_decode(
+        c, fmt, heads, scale if scale is not None else 1.0 / math.sqrt(d), window, Q.data_ptr(), q_stride, O.data_ptr(),
+        _ptr(lse), _ptr(workspace), nbytes, handle))
     return (O, lse) if return_lse else O
