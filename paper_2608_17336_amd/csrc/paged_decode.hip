@@ -24,26 +24,22 @@ constexpr int kCUs = 256;
 // What it costs to begin and end a sequence and head block, in tiles.
 constexpr int kPartStart = 6;
 constexpr int kPagedHeads = 16;                  // query heads on the columns of a matrix-core tile
-// 16-key slabs per tile: a tile is 16 KiB of K and V for d = 128, 8 KiB for d = 64.
-template <int FORMAT>
-constexpr int kSlabs = is_8bit(FORMAT) ? 4 : 2;
-
+// A tile is two slabs of 16 keys.  (Four slabs of an 8-bit cache leave two waves per SIMD instead of three: 32
+// sequences of 64 to 8192 keys 34.9 us, with two slabs 30.9; 4 x 65536 keys 102.9 and 105.1.)
+constexpr int kSlabs = 2, kTileKeys = 16 * kSlabs;
 // Waves that a SIMD holds, by their registers (K and V rows of a tile, the output): workgroups per CU.
-constexpr int resident_per_cu(int d, int format) { return (d == 64 ? 4 : 3) - (is_8bit(format) ? 1 : 0); }
+constexpr int resident_per_cu(int d) { return d == 64 ? 4 : 3; }
 
-int tile_keys(int format) { return 16 * (is_8bit(format) ? 4 : 2); }
-
-// The tokens that a sequence's query attends to, as tiles of `keys` tokens: first .. len - 1, of tiles
-// first / keys .. .
+// The tokens that a sequence's query attends to: first .. len - 1, of tiles tile0 .. .
 struct Span {
   int first = 0, len = 0, tile0 = 0, tiles = 0;
   Span() = default;
-  __device__ __forceinline__ Span(const PagedDecodeArgs& a, int keys, int tokens) {
+  __device__ __forceinline__ Span(const PagedDecodeArgs& a, int tokens) {
     const PagedPool& p = a.pool;
     len = min(max(tokens, 0), p.max_pages << p.page_shift);
     first = a.window > 0 ? max(len - a.window, 0) : 0;
-    tile0 = first / keys;
-    tiles = (len + keys - 1) / keys - tile0;
+    tile0 = first / kTileKeys;
+    tiles = (len + kTileKeys - 1) / kTileKeys - tile0;
   }
   // Tiles as they are shared out: a sequence without tokens has one, so that it is written, too.
   __device__ __forceinline__ int share() const { return max(1, tiles); }
@@ -76,12 +72,13 @@ __device__ __forceinline__ int ceil_div(int n, int d) { return small_quotient(n 
 struct Run {
   int b = -1, head_block, unit;   // where it begins (unit, or piece: of its sequence's); b = -1: no tile is left
   int mode, quota;
+  int total;                      // tiles of all sequences and head blocks
   __device__ __forceinline__ int units(int share) const {
     return mode == kWhole ? 1 : mode == kPieces ? ceil_div(share, quota) : kPartStart + share;
   }
-  __device__ __forceinline__ Run(const PagedDecodeArgs& a, int w, int lane, int keys) {
+  __device__ __forceinline__ Run(const PagedDecodeArgs& a, int w, int lane) {
     const int B = a.pool.B, per = (B + kWave - 1) / kWave, b0 = min(lane * per, B), b1 = min(b0 + per, B), W = gridDim.x;
-    auto share = [&](int s) { return Span(a, keys, a.pool.seqlens[s]).share(); };
+    auto share = [&](int s) { return Span(a, a.pool.seqlens[s]).share(); };
     auto wave_total = [](int x) { return __builtin_amdgcn_readlane(wave_scan(x), kWave - 1); };
     // (Of up to 64 sequences, a lane's length is read once.)
     const int mine = b0 < b1 ? share(b0) : 0;
@@ -95,9 +92,11 @@ struct Run {
     if (mode == kWhole) {
       own = b1 - b0;
       all = B * a.head_blocks;
+      total = kPagedWaves * all;
       quota = (int)a.div_workgroups.quot(all + W - 1);
     } else {
-      const int tiles = over_lane([](int n) { return n; }), total = wave_total(tiles) * a.head_blocks;
+      const int tiles = over_lane([](int n) { return n; });
+      total = wave_total(tiles) * a.head_blocks;
       const int even = max(kPagedWaves, (int)a.div_workgroups.quot(total + W - 1));
       if (B * a.head_blocks <= W) {
         mode = kPieces;
@@ -180,6 +179,18 @@ struct Part {
   }
 };
 
+// A row's bytes.  `stream`: not kept in the caches, for a batch that the last one (256 MiB) cannot keep for the next
+// call either, let alone between layers: 4 x 65536 keys of 8 INT8 heads (554 MB) 105.1 us, streamed 95.3;
+// 131072 keys of 4 E4M3 heads (138 MB) 37.0 and 36.0; but 111 MB 30.9 and 31.4, 82 MB 21.4 and 22.6.
+constexpr long long kStreamBytes = 128 << 20;
+template <bool STREAM, typename V>
+__device__ __forceinline__ V load_row(const char* p) {
+  if constexpr (STREAM) return __builtin_nontemporal_load(reinterpret_cast<const V*>(p));
+  return *reinterpret_cast<const V*>(p);
+}
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
 // Matrix-core products with 16-bit operands as the cache needs them: BF16 for a BF16 cache, else FP16 (8-bit
 // codes are exact in FP16).
 template <int FORMAT>
@@ -245,26 +256,30 @@ __device__ __forceinline__ void split2(float w0, float w1, uint32_t& hi, uint32_
 // channel row l16; row i of product c is given channel i D / 16 + c, so that a lane reads D / 16
 // adjacent channels of a key at once and pairs the keys by byte permutes: no transposed copy of V is
 // kept, and a row can be appended to a page as it is.
-template <int D, int TYPE, int FORMAT>
-__global__ __launch_bounds__(kPagedWaves * kWave) __attribute__((amdgpu_waves_per_eu(resident_per_cu(D, FORMAT))))
-void paged_decode_kernel(PagedDecodeArgs a) {
-  constexpr int kS = kSlabs<FORMAT>, kKeys = 16 * kS;
+template <int D>
+struct DecodeShared {
+  float m[kPagedWaves][kPagedHeads], z[kPagedWaves][kPagedHeads];
+  __align__(16) float o[kPagedWaves][kPagedHeads][D + 4];   // padded rows
+};
+
+template <int D, int TYPE, int FORMAT, bool STREAM>
+__device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run& run, DecodeShared<D>& shared) {
+  constexpr int kS = kSlabs, kKeys = kTileKeys;
   constexpr int kBytes = kElemBytes<FORMAT>;
   constexpr bool k8 = is_8bit(FORMAT);
   constexpr int kKL = D * kBytes / 64;             // 16-byte loads of a key row per lane
   constexpr int kC = D / 16;                       // channels of a lane's value row: output products
   constexpr int kVW = kC * kBytes / 4;             // dwords of them
   constexpr int kQ = D / 32;                       // score products per slab
-  constexpr int kOS = D + 4;                       // padded LDS row
   const PagedPool& p = a.pool;
   const int tid = threadIdx.x, lane = tid & (kWave - 1);
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int l16 = lane & 15, lq = lane >> 4;
   const float ninf = -__builtin_huge_valf();
-  __shared__ float red_m[kPagedWaves][kPagedHeads], red_z[kPagedWaves][kPagedHeads];
-  __shared__ __align__(16) float osum[kPagedWaves][kPagedHeads][kOS];
+  auto& red_m = shared.m;
+  auto& red_z = shared.z;
+  auto& osum = shared.o;
 
-  const Run run(a, blockIdx.x, lane, kKeys);
   const int quota = __builtin_amdgcn_readfirstlane(run.quota), mode = __builtin_amdgcn_readfirstlane(run.mode);
   int left = mode == kPieces ? 1 : quota;   // units
   Part cur;
@@ -272,7 +287,7 @@ void paged_decode_kernel(PagedDecodeArgs a) {
     const int b = __builtin_amdgcn_readfirstlane(run.b);
     if (b < 0) return;
     cur = Part(a, mode, quota, b, __builtin_amdgcn_readfirstlane(run.head_block), __builtin_amdgcn_readfirstlane(run.unit), left,
-               Span(a, kKeys, load_uniform(p.seqlens + b)));
+               Span(a, load_uniform(p.seqlens + b)));
     if (!cur.some()) return;
   }
   // The wave's first tile of a part, if f tiles of the workgroup's run lie before it: tile f + t goes to wave
@@ -281,8 +296,7 @@ void paged_decode_kernel(PagedDecodeArgs a) {
 
   // 1. Page ids of the wave's tiles n, n + kPagedWaves, .. of a part, 64 at a time: lane (i, j) holds the j-th of
   //    the 2^per_shift pages of tile i.
-  const int keys_shift = 4 + (kS == 8 ? 3 : kS == 4 ? 2 : 1);
-  const int per_shift = max(0, keys_shift - p.page_shift);
+  const int per_shift = max(0, 5 - p.page_shift);
   auto load_ids = [&](const Part& q, int n0) {
     const int n = n0 + (lane >> per_shift) * kPagedWaves;
     const int e = (n * kKeys >> p.page_shift) + (lane & ((1 << per_shift) - 1));
@@ -317,7 +331,7 @@ void paged_decode_kernel(PagedDecodeArgs a) {
     for (int s = 0; s < kS; ++s) {
       const char* base = poolK + kBytes * (max(page[s], 0) * p.stride_k + (long long)slab_row(hk, n, s) * D);
 #pragma unroll
-      for (int i = 0; i < kKL; ++i) kr[s][i] = ld_global_16(base + 64 * i + k_off);
+      for (int i = 0; i < kKL; ++i) kr[s][i] = __builtin_bit_cast(uint4, load_row<STREAM, u32x4>(base + 64 * i + k_off));
     }
     if constexpr (k8) {
 #pragma unroll
@@ -339,13 +353,13 @@ void paged_decode_kernel(PagedDecodeArgs a) {
       for (int r = 0; r < 4; ++r) {
         const char* at = base + r * D * kBytes + v_off;
         if constexpr (kVW == 4) {
-          const uint4 x = ld_global_16(at);
-          vr[s][r][0] = x.x; vr[s][r][1] = x.y; vr[s][r][2] = x.z; vr[s][r][3] = x.w;
+          const u32x4 x = load_row<STREAM, u32x4>(at);
+          vr[s][r][0] = x[0]; vr[s][r][1] = x[1]; vr[s][r][2] = x[2]; vr[s][r][3] = x[3];
         } else if constexpr (kVW == 2) {
-          const uint2 x = *reinterpret_cast<const uint2*>(at);
-          vr[s][r][0] = x.x; vr[s][r][1] = x.y;
+          const u32x2 x = load_row<STREAM, u32x2>(at);
+          vr[s][r][0] = x[0]; vr[s][r][1] = x[1];
         } else {
-          vr[s][r][0] = *reinterpret_cast<const uint32_t*>(at);
+          vr[s][r][0] = load_row<STREAM, uint32_t>(at);
         }
       }
     }
@@ -378,7 +392,7 @@ void paged_decode_kernel(PagedDecodeArgs a) {
   bool more = left > cur.take && !(whole_head && cur.b + 1 == p.B);
   if (more) {
     next = Part(a, mode, quota, cur.b + (whole_head ? 1 : 0), whole_head ? 0 : cur.head_block + 1, 0, left - cur.take,
-                whole_head ? Span(a, kKeys, load_uniform(p.seqlens + cur.b + 1)) : cur.span);
+                whole_head ? Span(a, load_uniform(p.seqlens + cur.b + 1)) : cur.span);
     more = next.some();
   }
   const int f_next = f + cur.hi - cur.lo, n_next = first_tile(next, f_next);
@@ -526,41 +540,44 @@ void paged_decode_kernel(PagedDecodeArgs a) {
       split2<FORMAT>(w[2], w[3], hi[s].y, lo[s].y);
     }
     // O^T += V^T P^T.
+    const uint4 ph = make_uint4(hi[0].x, hi[0].y, hi[1].x, hi[1].y), pl = make_uint4(lo[0].x, lo[0].y, lo[1].x, lo[1].y);
+    auto row = [&](int j) -> const uint32_t (&)[kVW] { return vr[j / 4][j % 4]; };   // of the lane's key j < 8
+    auto add = [&](int c, const uint32_t (&v)[4]) {
+      const uint4 va = make_uint4(v[0], v[1], v[2], v[3]);
+      acc[c] = mfma_16<FORMAT>(va, ph, acc[c]);
+      acc[c] = mfma_16<FORMAT>(va, pl, acc[c]);
+    };
+    if constexpr (FORMAT == TILEMIX_E4M3) {
+      // Channels c and c + 1 of two keys in one word, then two conversions.
 #pragma unroll
-    for (int t = 0; t < kS / 2; ++t) {
-      const uint4 ph = make_uint4(hi[2 * t].x, hi[2 * t].y, hi[2 * t + 1].x, hi[2 * t + 1].y);
-      const uint4 pl = make_uint4(lo[2 * t].x, lo[2 * t].y, lo[2 * t + 1].x, lo[2 * t + 1].y);
+      for (int c = 0; c < kC; c += 2) {
+        uint32_t v[2][4];
 #pragma unroll
-      for (int c2 = 0; c2 < kC / 2; ++c2) {
-        // Channels 2 c2 and 2 c2 + 1 of the lane, in FP16 or BF16 (or as codes), of its 8 keys.
-        uint32_t x[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const uint32_t (&row)[kVW] = vr[2 * t + j / 4][j % 4];
-          if constexpr (!k8) x[j] = row[c2];
-          else if constexpr (FORMAT == TILEMIX_E4M3) x[j] = c2 & 1 ? e4m3x2_to_half2<true>(row[c2 / 2]) : e4m3x2_to_half2<false>(row[c2 / 2]);
-          else x[j] = row[c2 / 2];
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t w = __builtin_amdgcn_perm(row(2 * j + 1)[c / 4], row(2 * j)[c / 4], c & 2 ? 0x07030602u : 0x05010400u);
+          v[0][j] = e4m3x2_to_half2<false>(w);
+          v[1][j] = e4m3x2_to_half2<true>(w);
         }
+        add(c, v[0]);
+        add(c + 1, v[1]);
+      }
+    } else {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t v[4];
+      for (int c = 0; c < kC; ++c) {
+        uint32_t v[4];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            if constexpr (FORMAT == TILEMIX_INT8) {
-              // A byte u of a code with the sign bit flipped reads as 1024 + 128 + code in 0x64uu.
-              const uint32_t k = 2 * (c2 & 1) + h;
-              const uint32_t pair = __builtin_amdgcn_perm(x[2 * j + 1], x[2 * j], 0x0c040c00u + k * 0x00010001u) ^ 0x64806480u;
-              const half2_t bias = {(_Float16)-1152.0f, (_Float16)-1152.0f};
-              v[j] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2_t, pair) + bias);
-            } else {
-              v[j] = __builtin_amdgcn_perm(x[2 * j + 1], x[2 * j], h ? 0x07060302u : 0x05040100u);
-            }
+        for (int j = 0; j < 4; ++j) {
+          if constexpr (FORMAT == TILEMIX_INT8) {
+            // A byte u of a code with the sign bit flipped reads as 1024 + 128 + code in 0x64uu.
+            const uint32_t pair = __builtin_amdgcn_perm(row(2 * j + 1)[c / 4], row(2 * j)[c / 4],
+                                                        0x0c040c00u + (uint32_t)(c & 3) * 0x00010001u) ^ 0x64806480u;
+            const half2_t bias = {(_Float16)-1152.0f, (_Float16)-1152.0f};
+            v[j] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2_t, pair) + bias);
+          } else {
+            v[j] = __builtin_amdgcn_perm(row(2 * j + 1)[c / 2], row(2 * j)[c / 2], c & 1 ? 0x07060302u : 0x05040100u);
           }
-          const uint4 va = make_uint4(v[0], v[1], v[2], v[3]);
-          const int c = 2 * c2 + h;
-          acc[c] = mfma_16<FORMAT>(va, ph, acc[c]);
-          acc[c] = mfma_16<FORMAT>(va, pl, acc[c]);
         }
+        add(c, v);
       }
     }
     __builtin_amdgcn_sched_barrier(0);   // not ahead of P V: their registers are in use
@@ -645,6 +662,17 @@ void paged_decode_kernel(PagedDecodeArgs a) {
   }
 }
 
+template <int D, int TYPE, int FORMAT>
+__global__ __launch_bounds__(kPagedWaves * kWave) __attribute__((amdgpu_waves_per_eu(resident_per_cu(D))))
+void paged_decode_kernel(PagedDecodeArgs a) {
+  __shared__ DecodeShared<D> shared;
+  const Run run(a, blockIdx.x, threadIdx.x & (kWave - 1));
+  // (Two copies of the body: a branch at each request would make the waits count loads that were not issued.)
+  const long long bytes = (long long)__builtin_amdgcn_readfirstlane(run.total) * (kTileKeys * 2 * D * kElemBytes<FORMAT>);
+  if (bytes >= kStreamBytes) decode_run<D, TYPE, FORMAT, true>(a, run, shared);
+  else decode_run<D, TYPE, FORMAT, false>(a, run, shared);
+}
+
 // One workgroup per (query head, sequence, 32 channels): thread (part, channel quad) joins every kParts-th row with
 // a running reference of its own; the parts are joined in LDS.
 constexpr int kJoinThreads = 256, kJoinChannels = 32;
@@ -715,17 +743,16 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedDecodeArg
 
 }  // namespace
 
-PagedDecodePlan plan_paged_decode(const PagedPool& p, int heads_q, int d, int format) {
+PagedDecodePlan plan_paged_decode(const PagedPool& p, int heads_q, int d) {
   const int G = heads_q / p.Hk;
   PagedDecodePlan pl{};
   pl.head_blocks = p.Hk * ((G + kPagedHeads - 1) / kPagedHeads);
   pl.part_heads = std::min(G, kPagedHeads);
-  const int keys = tile_keys(format);
-  const long long most = (((long long)p.max_pages << p.page_shift) + keys - 1) / keys;   // tiles of a sequence
+  const long long most = (((long long)p.max_pages << p.page_shift) + kTileKeys - 1) / kTileKeys;   // tiles of a sequence
   const long long segments = (long long)p.B * pl.head_blocks;
   pl.whole = most <= kPagedWaves;
   pl.units = segments * (most + kPartStart);
-  pl.workgroups = std::min<long long>(kCUs * resident_per_cu(d, format),
+  pl.workgroups = std::min<long long>(kCUs * resident_per_cu(d),
                                       pl.whole ? segments : (segments * most + kPagedWaves - 1) / kPagedWaves);
   return pl;
 }
