@@ -118,7 +118,7 @@ tilemix_status check_decode(const tilemix_paged_cache* c, int32_t heads_q) {
   if (st != TILEMIX_OK) return st;
   if (heads_q < 1 || heads_q > 65535 || heads_q % c->heads_kv != 0)
     return fail(TILEMIX_ERR_SHAPE, "heads_q (%d) must be a multiple of heads_kv (%d), at most 65535", heads_q, c->heads_kv);
-  if (tilemix::plan_paged_decode(pool_of(c), heads_q, c->head_dim).units > 0x7fffffffLL)
+  if (tilemix::plan_paged_decode(pool_of(c), heads_q, c->head_dim).units > (1LL << 30))
     return fail(TILEMIX_ERR_SHAPE, "batch * heads * max_pages * page_size is too large");
   return TILEMIX_OK;
 }

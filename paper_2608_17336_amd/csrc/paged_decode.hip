@@ -55,7 +55,7 @@ __device__ __forceinline__ int load_uniform(const int* p) {
 //   kRuns: each takes kPartStart units, for what it costs to begin and end one, and then a unit for each of its
 //     tiles; workgroup w takes the tiles in units [w quota, (w + 1) quota).
 //   kWhole: a workgroup takes `quota` of them, none is shared by workgroups and nothing has to be joined: where
-//     no sequence can have more than kPagedWaves tiles.
+//     no sequence can be long (see plan_paged_decode).
 // Runs share the tiles evenly, pieces begin and end one sequence only: pieces are taken where their number
 // fits the workgroups with at most kPartStart tiles more each than the even share.  Every wave finds its place for
 // itself: a lane takes a run of sequences.
@@ -92,7 +92,7 @@ struct Run {
     if (mode == kWhole) {
       own = b1 - b0;
       all = B * a.head_blocks;
-      total = kPagedWaves * all;
+      total = all * (a.whole / 2);   // (for want of the lengths: half of the most)
       quota = (int)a.div_workgroups.quot(all + W - 1);
     } else {
       const int tiles = over_lane([](int n) { return n; });
@@ -201,8 +201,6 @@ __device__ __forceinline__ f32x4 mfma_16(uint4 x, uint4 y, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(as_half8(x), as_half8(y), c, 0, 0, 0);
 }
 
-typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
-
 // Codes 2 w, 2 w + 1 of four E4M3 codes, in FP16.
 template <bool HIGH>
 __device__ __forceinline__ uint32_t e4m3x2_to_half2(uint32_t w) {
@@ -242,7 +240,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 // Two 16-bit pieces of two weights.
 template <int FORMAT>
 __device__ __forceinline__ void split2(float w0, float w1, uint32_t& hi, uint32_t& lo) {
-  using V = std::conditional_t<FORMAT == TILEMIX_BF16, bf16x2, half2_t>;
+  using V = std::conditional_t<FORMAT == TILEMIX_BF16, bf16x2, half2v>;
   const V h = __builtin_convertvector((f32x2{w0, w1}), V);
   const V l = __builtin_convertvector((f32x2{w0 - (float)h[0], w1 - (float)h[1]}), V);
   hi = __builtin_bit_cast(uint32_t, h);
@@ -382,283 +380,283 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run& 
   load_values(cur.hk, n, n < cur.end);
   __builtin_amdgcn_sched_barrier(0);
   for (;;) {
-  const int G = a.group, heads = min(kPagedHeads, G - cur.g0), hq0 = cur.hk * G + cur.g0;
-  cur = cur.uniform();
-  n = __builtin_amdgcn_readfirstlane(n);
-  left = __builtin_amdgcn_readfirstlane(left);
-  // The part that follows, so that its first tiles are requested behind the last ones of this.
-  Part next;
-  const bool whole_head = cur.head_block + 1 == a.head_blocks;
-  bool more = left > cur.take && !(whole_head && cur.b + 1 == p.B);
-  if (more) {
-    next = Part(a, mode, quota, cur.b + (whole_head ? 1 : 0), whole_head ? 0 : cur.head_block + 1, 0, left - cur.take,
-                whole_head ? Span(a, load_uniform(p.seqlens + cur.b + 1)) : cur.span);
-    more = next.some();
-  }
-  const int f_next = f + cur.hi - cur.lo, n_next = first_tile(next, f_next);
-  const int ids_next = load_ids(next, n_next);
+    const int G = a.group, heads = min(kPagedHeads, G - cur.g0), hq0 = cur.hk * G + cur.g0;
+    cur = cur.uniform();
+    n = __builtin_amdgcn_readfirstlane(n);
+    left = __builtin_amdgcn_readfirstlane(left);
+    // The part that follows, so that its first tiles are requested behind the last ones of this.
+    Part next;
+    const bool whole_head = cur.head_block + 1 == a.head_blocks;
+    bool more = left > cur.take && !(whole_head && cur.b + 1 == p.B);
+    if (more) {
+      next = Part(a, mode, quota, cur.b + (whole_head ? 1 : 0), whole_head ? 0 : cur.head_block + 1, 0, left - cur.take,
+                  whole_head ? Span(a, load_uniform(p.seqlens + cur.b + 1)) : cur.span);
+      more = next.some();
+    }
+    const int f_next = f + cur.hi - cur.lo, n_next = first_tile(next, f_next);
+    const int ids_next = load_ids(next, n_next);
 
-  // 3. Query rows as the B operand of the score products: lane (head l16, lq) holds the channels that it
-  //    reads of a key row.  BF16 queries against 8-bit codes are brought to FP16 by a power of two per
-  //    head, 2^q_exp: the largest to [2^14, 2^15), so that what FP16 cannot hold lies below 2^-39 of it.
-  float f_head = a.scale_log2e;   // score of a product, in log2 units, before the key's scale
-  {
-    const uint32_t some = l16 < heads ? ~0u : 0u;
-#pragma unroll
-    for (int i = 0; i < kQ; ++i) qf[i] = make_uint4(qf[i].x & some, qf[i].y & some, qf[i].z & some, qf[i].w & some);
-    if constexpr (k8 && TYPE == TILEMIX_BF16) {
-      float x[kQ][8], amax = 0.0f;
-#pragma unroll
-      for (int i = 0; i < kQ; ++i) {
-        const uint32_t w[4] = {qf[i].x, qf[i].y, qf[i].z, qf[i].w};
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          x[i][e] = bits_to_float<TILEMIX_BF16>(e & 1 ? w[e >> 1] >> 16 : w[e >> 1] & 0xffffu);
-          amax = fmaxf(amax, fabsf(x[i][e]));
+    // 3. Query rows as the B operand of the score products: lane (head l16, lq) holds the channels that it
+    //    reads of a key row.  BF16 queries against 8-bit codes are brought to FP16 by a power of two per
+    //    head, 2^q_exp: the largest to [2^14, 2^15), so that what FP16 cannot hold lies below 2^-39 of it.
+    float f_head = a.scale_log2e;   // score of a product, in log2 units, before the key's scale
+    {
+      const uint32_t some = l16 < heads ? ~0u : 0u;
+  #pragma unroll
+      for (int i = 0; i < kQ; ++i) qf[i] = make_uint4(qf[i].x & some, qf[i].y & some, qf[i].z & some, qf[i].w & some);
+      if constexpr (k8 && TYPE == TILEMIX_BF16) {
+        float x[kQ][8], amax = 0.0f;
+  #pragma unroll
+        for (int i = 0; i < kQ; ++i) {
+          const uint32_t w[4] = {qf[i].x, qf[i].y, qf[i].z, qf[i].w};
+  #pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            x[i][e] = bits_to_float<TILEMIX_BF16>(e & 1 ? w[e >> 1] >> 16 : w[e >> 1] & 0xffffu);
+            amax = fmaxf(amax, fabsf(x[i][e]));
+          }
+        }
+        const int q_exp = 15 - __builtin_amdgcn_frexp_expf(quad_rows_max(amax));
+        f_head = __builtin_amdgcn_ldexpf(f_head, -q_exp);
+  #pragma unroll
+        for (int i = 0; i < kQ; ++i) {
+          uint32_t w[8];
+  #pragma unroll
+          for (int e = 0; e < 8; ++e) w[e] = float_to_bits<TILEMIX_FP16>(__builtin_amdgcn_ldexpf(x[i][e], q_exp));
+          qf[i] = make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
         }
       }
-      const int q_exp = 15 - __builtin_amdgcn_frexp_expf(quad_rows_max(amax));
-      f_head = __builtin_amdgcn_ldexpf(f_head, -q_exp);
-#pragma unroll
-      for (int i = 0; i < kQ; ++i) {
-        uint32_t w[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = float_to_bits<TILEMIX_FP16>(__builtin_amdgcn_ldexpf(x[i][e], q_exp));
-        qf[i] = make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
-      }
     }
-  }
 
-  // 4. The wave's tiles.  m: running max (log2 units); ref: the reference r; z: this lane's share of the normalizer;
-  //    acc: output.  Loads complete in order, and a wait counts the younger ones, so rows are requested in the
-  //    same order and number on every way to a wait: the keys and their scales once the scores are
-  //    formed, the values and theirs after P V, into the registers that these leave, whether there is
-  //    another tile in this part, in the next one, or none.
-  float m = ninf, ref = ninf, z = 0.0f;
-  int e = kExpMin;
-  f32x4 acc[kC];
-#pragma unroll
-  for (int c = 0; c < kC; ++c) acc[c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  const bool none = n >= cur.end;
-  while (n < cur.end) {
-    // Which of the tile's keys count, where it is not all of them.
-    bool all = n * kKeys >= cur.span.first && (n + 1) * kKeys <= cur.span.len;
-    uint32_t has = 0;
-#pragma unroll
-    for (int s = 0; s < kS; ++s) has |= page[s] >= 0 ? 1u << s : 0u;
-    all = all && has == (1u << kS) - 1;
-    float sc[kS][4];
-#pragma unroll
-    for (int s = 0; s < kS; ++s) {
-      f32x4 c = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-      for (int k = 0; k < kKL; ++k) {
-        if constexpr (k8) {
-          c = mfma_16<FORMAT>(widen8<FORMAT>(kr[s][k].x, kr[s][k].y), qf[2 * k], c);
-          c = mfma_16<FORMAT>(widen8<FORMAT>(kr[s][k].z, kr[s][k].w), qf[2 * k + 1], c);
-        } else {
-          c = mfma_16<FORMAT>(kr[s][k], qf[k], c);
+    // 4. The wave's tiles.  m: running max (log2 units); ref: the reference r; z: this lane's share of the normalizer;
+    //    acc: output.  Loads complete in order, and a wait counts the younger ones, so rows are requested in the
+    //    same order and number on every way to a wait: the keys and their scales once the scores are
+    //    formed, the values and theirs after P V, into the registers that these leave, whether there is
+    //    another tile in this part, in the next one, or none.
+    float m = ninf, ref = ninf, z = 0.0f;
+    int e = kExpMin;
+    f32x4 acc[kC];
+  #pragma unroll
+    for (int c = 0; c < kC; ++c) acc[c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    const bool none = n >= cur.end;
+    while (n < cur.end) {
+      // Which of the tile's keys count, where it is not all of them.
+      bool all = n * kKeys >= cur.span.first && (n + 1) * kKeys <= cur.span.len;
+      uint32_t has = 0;
+  #pragma unroll
+      for (int s = 0; s < kS; ++s) has |= page[s] >= 0 ? 1u << s : 0u;
+      all = all && has == (1u << kS) - 1;
+      float sc[kS][4];
+  #pragma unroll
+      for (int s = 0; s < kS; ++s) {
+        f32x4 c = {0.0f, 0.0f, 0.0f, 0.0f};
+  #pragma unroll
+        for (int k = 0; k < kKL; ++k) {
+          if constexpr (k8) {
+            c = mfma_16<FORMAT>(widen8<FORMAT>(kr[s][k].x, kr[s][k].y), qf[2 * k], c);
+            c = mfma_16<FORMAT>(widen8<FORMAT>(kr[s][k].z, kr[s][k].w), qf[2 * k + 1], c);
+          } else {
+            c = mfma_16<FORMAT>(kr[s][k], qf[k], c);
+          }
+        }
+        // Scores are scaled and rounded before the max and the exponent see them.
+  #pragma unroll
+        for (int r = 0; r < 4; ++r) sc[s][r] = c[r] * (k8 ? f_head * dk[s][r] : f_head);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      const bool here = n + kPagedWaves < cur.end;
+      const int to = here ? n + kPagedWaves : n_next, hk = here ? cur.hk : next.hk;
+      const bool some = here || n_next < next.end;
+      if (here) {
+        ++i;
+        if ((i & (id_tiles - 1)) == 0) {
+          ids = load_ids(cur, to);
+          asm volatile("; wait for them here" : "+v"(ids));   // not on the other ways, where rows are in flight
+        }
+      } else {
+        i = 0;
+        ids = ids_next;
+        asm volatile("; and here for the next part's" : "+v"(ids));
+      }
+      find_pages(ids, i);
+      load_keys(hk, to, some);
+      if (!all) {
+  #pragma unroll
+        for (int s = 0; s < kS; ++s)
+  #pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int t = n * kKeys + 16 * s + 4 * lq + r;
+            const bool ok = (has >> s & 1) && t >= cur.span.first && t < cur.span.len;
+            sc[s][r] = ok ? sc[s][r] : ninf;
+            if constexpr (k8) dv[s][r] = ok ? dv[s][r] : 0.0f;
+            // What a slot behind the sequence holds may be a NaN, which a weight of 0 does not cancel.
+            if constexpr (FORMAT != TILEMIX_INT8) {
+  #pragma unroll
+              for (int w = 0; w < kVW; ++w) vr[s][r][w] = ok ? vr[s][r][w] : 0u;
+            }
+          }
+      }
+      // Softmax: reference, normalizer and output move when the max or the value scales' exponent grows.
+      float mt = sc[0][0];
+  #pragma unroll
+      for (int s = 0; s < kS; ++s)
+  #pragma unroll
+        for (int r = 0; r < 4; ++r) mt = fmaxf(mt, sc[s][r]);
+      const float m_new = fmaxf(m, quad_rows_max(mt));
+      int e_new = e;
+      if constexpr (k8) {
+        float vm = 0.0f;
+  #pragma unroll
+        for (int s = 0; s < kS; ++s)
+  #pragma unroll
+          for (int r = 0; r < 4; ++r) vm = fmaxf(vm, fabsf(dv[s][r]));
+        vm = quad_rows_max(vm);
+        if (vm > 0.0f) e_new = max(e, __builtin_amdgcn_frexp_expf(vm));
+      }
+      if (__any(m_new > m || e_new > e)) {
+        // No finite score so far: p = 2^(-inf - 0) = 0, not a NaN.
+        const float next = m_new == ninf ? ninf : m_new - (k8 ? kHeadroom<FORMAT> - (float)e_new : kHeadroom<FORMAT>);
+        const float alpha = ref == ninf ? 0.0f : __builtin_amdgcn_exp2f(ref - next);
+        z *= alpha;
+  #pragma unroll
+        for (int c = 0; c < kC; ++c) acc[c] *= alpha;
+        m = m_new;
+        e = e_new;
+        ref = next;
+      }
+      const float sub = ref == ninf ? 0.0f : ref;
+      uint2 hi[kS], lo[kS];
+  #pragma unroll
+      for (int s = 0; s < kS; ++s) {
+        float w[4];
+  #pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          w[r] = __builtin_amdgcn_exp2f(sc[s][r] - sub);
+          z += w[r];
+          if constexpr (k8) w[r] *= dv[s][r];
+        }
+        split2<FORMAT>(w[0], w[1], hi[s].x, lo[s].x);
+        split2<FORMAT>(w[2], w[3], hi[s].y, lo[s].y);
+      }
+      // O^T += V^T P^T.
+      const uint4 ph = make_uint4(hi[0].x, hi[0].y, hi[1].x, hi[1].y), pl = make_uint4(lo[0].x, lo[0].y, lo[1].x, lo[1].y);
+      auto row = [&](int j) -> const uint32_t (&)[kVW] { return vr[j / 4][j % 4]; };   // of the lane's key j < 8
+      auto add = [&](int c, const uint32_t (&v)[4]) {
+        const uint4 va = make_uint4(v[0], v[1], v[2], v[3]);
+        acc[c] = mfma_16<FORMAT>(va, ph, acc[c]);
+        acc[c] = mfma_16<FORMAT>(va, pl, acc[c]);
+      };
+      if constexpr (FORMAT == TILEMIX_E4M3) {
+        // Channels c and c + 1 of two keys in one word, then two conversions.
+  #pragma unroll
+        for (int c = 0; c < kC; c += 2) {
+          uint32_t v[2][4];
+  #pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t w = __builtin_amdgcn_perm(row(2 * j + 1)[c / 4], row(2 * j)[c / 4], c & 2 ? 0x07030602u : 0x05010400u);
+            v[0][j] = e4m3x2_to_half2<false>(w);
+            v[1][j] = e4m3x2_to_half2<true>(w);
+          }
+          add(c, v[0]);
+          add(c + 1, v[1]);
+        }
+      } else {
+  #pragma unroll
+        for (int c = 0; c < kC; ++c) {
+          uint32_t v[4];
+  #pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            if constexpr (FORMAT == TILEMIX_INT8) {
+              // A byte u of a code with the sign bit flipped reads as 1024 + 128 + code in 0x64uu.
+              const uint32_t pair = __builtin_amdgcn_perm(row(2 * j + 1)[c / 4], row(2 * j)[c / 4],
+                                                          0x0c040c00u + (uint32_t)(c & 3) * 0x00010001u) ^ 0x64806480u;
+              const half2v bias = {(_Float16)-1152.0f, (_Float16)-1152.0f};
+              v[j] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2v, pair) + bias);
+            } else {
+              v[j] = __builtin_amdgcn_perm(row(2 * j + 1)[c / 2], row(2 * j)[c / 2], c & 1 ? 0x07060302u : 0x05040100u);
+            }
+          }
+          add(c, v);
         }
       }
-      // Scores are scaled and rounded before the max and the exponent see them.
-#pragma unroll
-      for (int r = 0; r < 4; ++r) sc[s][r] = c[r] * (k8 ? f_head * dk[s][r] : f_head);
+      __builtin_amdgcn_sched_barrier(0);   // not ahead of P V: their registers are in use
+      load_values(hk, to, some);
+      n += kPagedWaves;
     }
-    __builtin_amdgcn_sched_barrier(0);
-    const bool here = n + kPagedWaves < cur.end;
-    const int to = here ? n + kPagedWaves : n_next, hk = here ? cur.hk : next.hk;
-    const bool some = here || n_next < next.end;
-    if (here) {
-      ++i;
-      if ((i & (id_tiles - 1)) == 0) {
-        ids = load_ids(cur, to);
-        asm volatile("; wait for them here" : "+v"(ids));   // not on the other ways, where rows are in flight
-      }
-    } else {
+    if (none) {   // the wave's registers hold nothing of this part
       i = 0;
       ids = ids_next;
-      asm volatile("; and here for the next part's" : "+v"(ids));
+      find_pages(ids, 0);
+      load_keys(next.hk, n_next, n_next < next.end);
+      __builtin_amdgcn_sched_barrier(0);
+      load_values(next.hk, n_next, n_next < next.end);
     }
-    find_pages(ids, i);
-    load_keys(hk, to, some);
-    if (!all) {
-#pragma unroll
-      for (int s = 0; s < kS; ++s)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int t = n * kKeys + 16 * s + 4 * lq + r;
-          const bool ok = (has >> s & 1) && t >= cur.span.first && t < cur.span.len;
-          sc[s][r] = ok ? sc[s][r] : ninf;
-          if constexpr (k8) dv[s][r] = ok ? dv[s][r] : 0.0f;
-          // What a slot behind the sequence holds may be a NaN, which a weight of 0 does not cancel.
-          if constexpr (FORMAT != TILEMIX_INT8) {
-#pragma unroll
-            for (int w = 0; w < kVW; ++w) vr[s][r][w] = ok ? vr[s][r][w] : 0u;
-          }
-        }
-    }
-    // Softmax: reference, normalizer and output move when the max or the value scales' exponent grows.
-    float mt = sc[0][0];
-#pragma unroll
-    for (int s = 0; s < kS; ++s)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) mt = fmaxf(mt, sc[s][r]);
-    const float m_new = fmaxf(m, quad_rows_max(mt));
-    int e_new = e;
-    if constexpr (k8) {
-      float vm = 0.0f;
-#pragma unroll
-      for (int s = 0; s < kS; ++s)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) vm = fmaxf(vm, fabsf(dv[s][r]));
-      vm = quad_rows_max(vm);
-      if (vm > 0.0f) e_new = max(e, __builtin_amdgcn_frexp_expf(vm));
-    }
-    if (__any(m_new > m || e_new > e)) {
-      // No finite score so far: p = 2^(-inf - 0) = 0, not a NaN.
-      const float next = m_new == ninf ? ninf : m_new - (k8 ? kHeadroom<FORMAT> - (float)e_new : kHeadroom<FORMAT>);
-      const float alpha = ref == ninf ? 0.0f : __builtin_amdgcn_exp2f(ref - next);
-      z *= alpha;
-#pragma unroll
-      for (int c = 0; c < kC; ++c) acc[c] *= alpha;
-      m = m_new;
-      e = e_new;
-      ref = next;
-    }
-    const float sub = ref == ninf ? 0.0f : ref;
-    uint2 hi[kS], lo[kS];
-#pragma unroll
-    for (int s = 0; s < kS; ++s) {
-      float w[4];
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        w[r] = __builtin_amdgcn_exp2f(sc[s][r] - sub);
-        z += w[r];
-        if constexpr (k8) w[r] *= dv[s][r];
-      }
-      split2<FORMAT>(w[0], w[1], hi[s].x, lo[s].x);
-      split2<FORMAT>(w[2], w[3], hi[s].y, lo[s].y);
-    }
-    // O^T += V^T P^T.
-    const uint4 ph = make_uint4(hi[0].x, hi[0].y, hi[1].x, hi[1].y), pl = make_uint4(lo[0].x, lo[0].y, lo[1].x, lo[1].y);
-    auto row = [&](int j) -> const uint32_t (&)[kVW] { return vr[j / 4][j % 4]; };   // of the lane's key j < 8
-    auto add = [&](int c, const uint32_t (&v)[4]) {
-      const uint4 va = make_uint4(v[0], v[1], v[2], v[3]);
-      acc[c] = mfma_16<FORMAT>(va, ph, acc[c]);
-      acc[c] = mfma_16<FORMAT>(va, pl, acc[c]);
-    };
-    if constexpr (FORMAT == TILEMIX_E4M3) {
-      // Channels c and c + 1 of two keys in one word, then two conversions.
-#pragma unroll
-      for (int c = 0; c < kC; c += 2) {
-        uint32_t v[2][4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const uint32_t w = __builtin_amdgcn_perm(row(2 * j + 1)[c / 4], row(2 * j)[c / 4], c & 2 ? 0x07030602u : 0x05010400u);
-          v[0][j] = e4m3x2_to_half2<false>(w);
-          v[1][j] = e4m3x2_to_half2<true>(w);
-        }
-        add(c, v[0]);
-        add(c + 1, v[1]);
-      }
-    } else {
-#pragma unroll
-      for (int c = 0; c < kC; ++c) {
-        uint32_t v[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if constexpr (FORMAT == TILEMIX_INT8) {
-            // A byte u of a code with the sign bit flipped reads as 1024 + 128 + code in 0x64uu.
-            const uint32_t pair = __builtin_amdgcn_perm(row(2 * j + 1)[c / 4], row(2 * j)[c / 4],
-                                                        0x0c040c00u + (uint32_t)(c & 3) * 0x00010001u) ^ 0x64806480u;
-            const half2_t bias = {(_Float16)-1152.0f, (_Float16)-1152.0f};
-            v[j] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2_t, pair) + bias);
-          } else {
-            v[j] = __builtin_amdgcn_perm(row(2 * j + 1)[c / 2], row(2 * j)[c / 2], c & 1 ? 0x07060302u : 0x05040100u);
-          }
-        }
-        add(c, v);
-      }
-    }
-    __builtin_amdgcn_sched_barrier(0);   // not ahead of P V: their registers are in use
-    load_values(hk, to, some);
-    n += kPagedWaves;
-  }
-  if (none) {   // the wave's registers hold nothing of this part
-    i = 0;
-    ids = ids_next;
-    find_pages(ids, 0);
-    load_keys(next.hk, n_next, n_next < next.end);
     __builtin_amdgcn_sched_barrier(0);
-    load_values(next.hk, n_next, n_next < next.end);
-  }
-  __builtin_amdgcn_sched_barrier(0);
-  if (more) load_query(next);
+    if (more) load_query(next);
 
-  // 5. The waves' results joined in LDS.
-  z = quad_rows_sum(z);
-  if (lq == 0) red_m[wave][l16] = ref;
-  __syncthreads();
-  float top = red_m[0][l16];
-#pragma unroll
-  for (int w = 1; w < kPagedWaves; ++w) top = fmaxf(top, red_m[w][l16]);
-  const float fw = ref == ninf ? 0.0f : __builtin_amdgcn_exp2f(ref - top);
-  if (lq == 0) red_z[wave][l16] = z * fw;
-#pragma unroll
-  for (int r = 0; r < 4; ++r)
-#pragma unroll
-    for (int c = 0; c < kC; ++c) osum[wave][l16][(4 * lq + r) * kC + c] = ref == ninf ? 0.0f : acc[c][r] * fw;
-  __syncthreads();
-  const bool whole = cur.lo == 0 && cur.hi == cur.span.share();
-  // Partial results: of the workgroup's first part in row 2 w, of one behind others in row 2 w + 1 (it is the
-  // last, and has its sequence's first tile).
-  const int part_row = (int)blockIdx.x * 2 + (f != 0 ? 1 : 0);
-  for (int o = tid; o < heads * (D / 4); o += kPagedWaves * kWave) {
-    const int g = o / (D / 4), c = o % (D / 4) * 4;
-    f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
-    float zz = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kPagedWaves; ++w) {
-      sum += *reinterpret_cast<const f32x4*>(&osum[w][g][c]);
-      zz += red_z[w][g];
+    // 5. The waves' results joined in LDS.
+    z = quad_rows_sum(z);
+    if (lq == 0) red_m[wave][l16] = ref;
+    __syncthreads();
+    float top = red_m[0][l16];
+  #pragma unroll
+    for (int w = 1; w < kPagedWaves; ++w) top = fmaxf(top, red_m[w][l16]);
+    const float fw = ref == ninf ? 0.0f : __builtin_amdgcn_exp2f(ref - top);
+    if (lq == 0) red_z[wave][l16] = z * fw;
+  #pragma unroll
+    for (int r = 0; r < 4; ++r)
+  #pragma unroll
+      for (int c = 0; c < kC; ++c) osum[wave][l16][(4 * lq + r) * kC + c] = ref == ninf ? 0.0f : acc[c][r] * fw;
+    __syncthreads();
+    const bool whole = cur.lo == 0 && cur.hi == cur.span.share();
+    // Partial results: of the workgroup's first part in row 2 w, of one behind others in row 2 w + 1 (it is the
+    // last, and has its sequence's first tile).
+    const int part_row = (int)blockIdx.x * 2 + (f != 0 ? 1 : 0);
+    for (int o = tid; o < heads * (D / 4); o += kPagedWaves * kWave) {
+      const int g = o / (D / 4), c = o % (D / 4) * 4;
+      f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+      float zz = 0.0f;
+  #pragma unroll
+      for (int w = 0; w < kPagedWaves; ++w) {
+        sum += *reinterpret_cast<const f32x4*>(&osum[w][g][c]);
+        zz += red_z[w][g];
+      }
+      if (whole) {
+        uint32_t h[4];
+  #pragma unroll
+        for (int r = 0; r < 4; ++r) h[r] = float_to_bits<TYPE>(zz == 0.0f ? 0.0f : sum[r] / zz);
+        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.O) + ((long long)cur.b * a.Hq + hq0 + g) * D + c) =
+            make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
+      } else {
+        *reinterpret_cast<f32x4*>(a.part_o + ((size_t)part_row * a.part_heads + g) * D + c) = sum;
+      }
     }
-    if (whole) {
-      uint32_t h[4];
-#pragma unroll
-      for (int r = 0; r < 4; ++r) h[r] = float_to_bits<TYPE>(zz == 0.0f ? 0.0f : sum[r] / zz);
-      *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.O) + ((long long)cur.b * a.Hq + hq0 + g) * D + c) =
-          make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
-    } else {
-      *reinterpret_cast<f32x4*>(a.part_o + ((size_t)part_row * a.part_heads + g) * D + c) = sum;
+    if (tid < heads) {
+      float zz = 0.0f, mm = red_m[0][tid];
+  #pragma unroll
+      for (int w = 0; w < kPagedWaves; ++w) {
+        zz += red_z[w][tid];
+        mm = fmaxf(mm, red_m[w][tid]);
+      }
+      if (whole) {
+        if (a.lse)
+          a.lse[(long long)cur.b * a.Hq + hq0 + tid] =
+              zz == 0.0f ? ninf : 0.69314718056f * (mm + __builtin_amdgcn_logf(zz));
+      } else {
+        reinterpret_cast<float2*>(a.part_rz)[(size_t)part_row * a.part_heads + tid] = make_float2(mm, zz);
+      }
     }
-  }
-  if (tid < heads) {
-    float zz = 0.0f, mm = red_m[0][tid];
-#pragma unroll
-    for (int w = 0; w < kPagedWaves; ++w) {
-      zz += red_z[w][tid];
-      mm = fmaxf(mm, red_m[w][tid]);
+    // For the join: the first row, and how many workgroups there are from this one on.
+    if (a.segments && tid == 0 && cur.lo == 0) {
+      const int beyond = cur.span.share() - cur.hi;   // tiles of the workgroups that follow
+      reinterpret_cast<int2*>(a.segments)[(size_t)cur.b * a.head_blocks + cur.head_block] =
+          make_int2(part_row, 1 + ceil_div(beyond, cur.step));
     }
-    if (whole) {
-      if (a.lse)
-        a.lse[(long long)cur.b * a.Hq + hq0 + tid] =
-            zz == 0.0f ? ninf : 0.69314718056f * (mm + __builtin_amdgcn_logf(zz));
-    } else {
-      reinterpret_cast<float2*>(a.part_rz)[(size_t)part_row * a.part_heads + tid] = make_float2(mm, zz);
-    }
-  }
-  // For the join: the first row, and how many workgroups there are from this one on.
-  if (a.segments && tid == 0 && cur.lo == 0) {
-    const int beyond = cur.span.share() - cur.hi;   // tiles of the workgroups that follow
-    reinterpret_cast<int2*>(a.segments)[(size_t)cur.b * a.head_blocks + cur.head_block] =
-        make_int2(part_row, 1 + ceil_div(beyond, cur.step));
-  }
-  if (!more) return;
-  left -= cur.take;
-  cur = next;
-  f = f_next;
-  n = n_next;
-  __syncthreads();   // the LDS is used again
+    if (!more) return;
+    left -= cur.take;
+    cur = next;
+    f = f_next;
+    n = n_next;
+    __syncthreads();   // the LDS is used again
   }
 }
 
@@ -750,8 +748,12 @@ PagedDecodePlan plan_paged_decode(const PagedPool& p, int heads_q, int d) {
   pl.part_heads = std::min(G, kPagedHeads);
   const long long most = (((long long)p.max_pages << p.page_shift) + kTileKeys - 1) / kTileKeys;   // tiles of a sequence
   const long long segments = (long long)p.B * pl.head_blocks;
-  pl.whole = most <= kPagedWaves;
   pl.units = segments * (most + kPartStart);
+  // No sequence is split, and the second launch saved, where none can be longer than 16 tiles (8 KV heads, INT8, d
+  // 128: 32 sequences of 500 keys 10.8 us, split 18.3; 1 of 250 7.5 and 9.6), or 32 where there is one for every CU (32
+  // of 1000 keys 15.4 and 22.6, 128 48.2 and 64.0, 200, a little over two rounds of workgroups, 98.7 and 92.3).
+  // Beyond, splitting pays (8 of 1000 keys 14.9 and 13.1; 200 of 2000 keys 181 and 157).
+  pl.whole = most <= (segments >= kCUs ? 32 : 16) ? (int)most : 0;
   pl.workgroups = std::min<long long>(kCUs * resident_per_cu(d),
                                       pl.whole ? segments : (segments * most + kPagedWaves - 1) / kPagedWaves);
   return pl;

@@ -202,7 +202,7 @@ struct PagedDecodeArgs {
   int Hq, window;
   float scale_log2e;
   int head_blocks;         // KV heads x blocks of 16 query heads
-  int whole;               // 1: no sequence has more tiles than a workgroup has waves, and none is shared
+  int whole;               // 0, or the most tiles that a sequence can have, where workgroups share none
   // Partial results of sequences that several workgroups share, two rows per workgroup (nullptr where none can be):
   int part_heads;          // query heads of a row
   float* part_rz;          // [rows, part_heads, 2]: reference of the weights (log2 units), normalizer
@@ -213,7 +213,7 @@ struct PagedDecodeArgs {
 };
 struct PagedDecodePlan {
   int head_blocks, part_heads;
-  bool whole;
+  int whole;
   long long units;         // the most units that the batch can have
   long long workgroups;
 };

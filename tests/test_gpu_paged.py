@@ -187,6 +187,60 @@ def test_append_rows_without_a_slot(fmt, dtype):
     assert gK[kept].any(-1).any(-1).all()
 
 
+@pytest.mark.parametrize("fmt,dtype", PAIRS)
+def test_rows_of_many_sequences(fmt, dtype):
+    """More sequences than lanes of a wave, most with few rows or none; the same through a call that takes the first
+    40 rows of each at most."""
+    tm = _tm()
+    B, Hk, d, page, per = 150, 2, 64, 16, 7
+    new = [(0, 0, 1, 7, 100, 33)[b * b % 6] for b in range(B)]
+    lens = [n + b % 5 for b, n in enumerate(new)]
+    cu = np.concatenate([[0], np.cumsum(new)])
+    total, pages = int(cu[-1]), B * per
+    table = _table(B, per, pages, 40)
+    K, V = _rows(total, Hk, d, dtype, 41), _rows(total, Hk, d, dtype, 42)
+    t_gpu, l_gpu, cu_gpu = table.cuda(), torch.tensor(lens, dtype=torch.int32).cuda(), torch.tensor(cu, dtype=torch.int32).cuda()
+    for longest in (100, 40):
+        pool = _random_pool(fmt, (pages, Hk, page, d), 43)
+        cache = _on_gpu(pool)
+        tm.tilemix_paged_append(cache, K.cuda(), V.cuda(), t_gpu, l_gpu, cu_gpu, longest)
+        rows = new_tokens(lens, cu, B, longest, total)
+        for b, r, t in rows:
+            at = slot_of(table.numpy(), pages, page, b, t)
+            _write(pool, fmt, K[r], 0, *at)
+            _write(pool, fmt, V[r], 1, *at)
+        torch.cuda.synchronize()
+        _same_pool(cache, pool)
+        out = [torch.full((total, Hk, d), 7.0, dtype=FORMATS[dtype], device="cuda") for _ in "KV"]
+        tm.tilemix_paged_gather(cache, t_gpu, l_gpu, longest, cu_gpu, K=out[0], V=out[1])
+        for op in (0, 1):
+            want = torch.full((total, Hk, d), 7.0, dtype=FORMATS[dtype])
+            for b, r, t in rows:
+                p, s = slot_of(table.numpy(), pages, page, b, t)
+                row = pool[op][p, :, s].float()
+                want[r] = (row * pool[op + 2][p, :, s, None] if fmt in TOP else row).to(FORMATS[dtype])
+            assert torch.equal(out[op].cpu(), want)
+
+
+def test_rows_of_broken_offsets():
+    """cu_seqlens that step back or point outside the rows: no row beyond `total` is read or written."""
+    tm = _tm()
+    Hk, d, page, total = 2, 64, 16, 20
+    cache = tm.PagedCache.empty(8, page, Hk, d, torch.float16)
+    cache.K.zero_(), cache.V.zero_()
+    table = torch.arange(8, dtype=torch.int32).view(4, 2).cuda()
+    lens = torch.tensor([30, 30, 30, 30], dtype=torch.int32).cuda()
+    cu = torch.tensor([-5, 12, 3, 2 ** 31 - 1, -2 ** 31], dtype=torch.int32).cuda()
+    buf = torch.full((total + 40, Hk, d), 3.0, dtype=torch.float16, device="cuda")
+    tm.tilemix_paged_append(cache, buf[:total], buf[:total], table, lens, cu, 2 ** 20)
+    tm.tilemix_paged_gather(cache, table, lens, 2 ** 20, cu, K=buf[:total], V=buf[:total].clone())
+    torch.cuda.synchronize()
+    assert (buf[total:] == 3.0).all()
+    for b, n in enumerate((12, 0, 17, 0)):                           # at most rows 0 .. 11, none, rows 3 .. 19, none
+        held = cache.K[2 * b:2 * b + 2].transpose(1, 2).reshape(2 * page, -1)
+        assert ((held[30 - n:30] == 3.0) | (held[30 - n:30] == 0.0)).all() and not held[:30 - n].any() and not held[30:].any()
+
+
 @pytest.mark.parametrize("dtype", ["fp16", "bf16"])
 @pytest.mark.parametrize("fmt", ["int8", "e4m3"])
 @pytest.mark.parametrize("d", [64, 128])
@@ -372,6 +426,62 @@ def test_decode_large_groups(fmt, dtype, Hq, Hk):
 def test_decode_long(fmt, dtype, lens, Hq, Hk, d, page):
     """Caches that are split over workgroups."""
     _decode_case(fmt, dtype, Hq, Hk, d, page, lens, seed=200)
+
+
+@pytest.mark.parametrize("fmt,dtype", PAIRS)
+@pytest.mark.parametrize("Hq,Hk,d,long", [(2, 2, 64, 700), (6, 1, 128, 700), (128, 1, 64, 1100), (96, 2, 128, 1100)])
+def test_decode_many_sequences(fmt, dtype, Hq, Hk, d, long):
+    """More sequences than lanes of a wave, with empty ones at both ends; few and many beside the workgroups that
+    run at once, so that a long sequence is cut, and a workgroup has parts of several."""
+    lens = [(0, 3, 37, 150, 1, 64)[b * b % 6] for b in range(150)]
+    lens[7] = lens[130] = long
+    lens[149] = 0
+    _decode_case(fmt, dtype, Hq, Hk, d, 16, lens, seed=1500)
+
+
+@pytest.mark.parametrize("fmt,dtype", PAIRS)
+@pytest.mark.parametrize("Hq,B,slots", [(4, 3, 480), (4, 3, 512), (4, 3, 544), (64, 64, 992), (64, 64, 1024), (64, 64, 1056),
+                                        (128, 140, 256)])
+def test_decode_capacities(fmt, dtype, Hq, B, slots):
+    """Page tables of 15 to 17 and 31 to 33 tiles of 32 keys, full and empty sequences, one or several a workgroup."""
+    lens = [slots, slots - 1, 0, 1] + [(b * 41 + 5) % 170 for b in range(4, B)]
+    _decode_case(fmt, dtype, Hq, 1, 64, 32, lens[:B], seed=1600, per=slots // 32)
+
+
+@pytest.mark.parametrize("fmt,dtype", PAIRS)
+@pytest.mark.parametrize("lens", [[65900, 0, 1, 100], [22000, 23000, 21100]])
+def test_decode_of_a_large_batch(fmt, dtype, lens):
+    """Caches larger than 2^27 bytes.  Few pages, each named many times (a prefix that sequences share)."""
+    tm = _tm()
+    d, page, pages = 128, 64, 20
+    Hk = 8 if fmt in TOP else 4
+    Hq = 2 * Hk
+    assert sum(lens) * 2 * Hk * d * FORMATS[fmt].itemsize > 2 ** 27
+    pool = _cached_pool(fmt, (pages, Hk, page, d), 1700)
+    table = torch.randint(0, pages, (len(lens), -(-max(lens) // page)), generator=_gen(1701)).to(torch.int32)
+    Q = torch.randn(len(lens), 1, Hq, d, generator=_gen(1702)).to(FORMATS[dtype])
+    log(f"decode of a large batch {fmt}/{dtype} {lens}: start")
+    O, lse = tm.tilemix_paged_decode(_on_gpu(pool), Q.cuda(), table.cuda(), torch.tensor(lens, dtype=torch.int32).cuda(), return_lse=True)
+    torch.cuda.synchronize()
+    # Equal tokens count alike: the oracle's softmax over a token per (page, slot), weighted by how often it occurs.
+    K, V = _values(pool, 0, fmt), _values(pool, 1, fmt)
+    times = np.zeros((len(lens), pages, page))
+    for b, L in enumerate(lens):
+        for t in range(L):
+            times[b, int(table[b, t // page]), t % page] += 1
+    q = Q.double().numpy()[:, 0]
+    want = [np.zeros((len(lens), Hq, d)), np.full((len(lens), Hq), -np.inf), np.zeros((len(lens), Hq, d)), np.zeros((len(lens), Hq))]
+    for b, hq in np.ndindex(len(lens), Hq):
+        if not lens[b]:
+            continue
+        k, v = K[:, hq // 2].reshape(-1, d), V[:, hq // 2].reshape(-1, d)
+        s = d ** -0.5 * (k @ q[b, hq])
+        m = s.max()
+        w = times[b].ravel() * np.exp(s - m)
+        z = w.sum()
+        want[0][b, hq], want[1][b, hq], want[2][b, hq] = w @ v / z, m + np.log(z), w @ np.abs(v) / z
+        want[3][b, hq] = d ** -0.5 * (np.abs(k) @ np.abs(q[b, hq])).max()
+    _check_decode(f"large batch {fmt}/{dtype}", O, lse, want, dtype, max(lens), _v_max(V, fmt))
 
 
 @pytest.mark.parametrize("fmt,dtype", PAIRS)

@@ -135,3 +135,29 @@ def test_binding_refuses_host_tensors():
                  lambda: tm.tilemix_paged_decode(pool, x, table, lens)):
         with pytest.raises(TypeError, match="CUDA"):
             call()
+
+
+def _workspace(cache, heads=32):
+    n = ctypes.c_size_t()
+    assert tm.load_library().tilemix_paged_decode_workspace_size(cache, heads, ctypes.byref(n)) == 0
+    return n.value
+
+
+def test_decode_workspace():
+    """A long page table needs one, a short one none; it is checked before anything runs."""
+    long, short = _cache(max_pages=100, stride_table=100), _cache(max_pages=8, stride_table=8)
+    need = _workspace(long)
+    assert need > 0 and need % 256 == 0 and _workspace(short) == 0
+    assert _decode(long, ws=None) == WORKSPACE
+    assert _decode(long, nbytes=need - 1) == WORKSPACE
+    assert _decode(long, nbytes=0) == WORKSPACE
+    assert _decode(long, ws=OK + 128, nbytes=need) == ALIGN
+
+
+def test_decode_of_too_large_batches():
+    """What the numbering of a batch's tiles cannot hold."""
+    big = dict(max_pages=1 << 24, stride_table=1 << 24)              # 2^30 tokens: 2^25 tiles of 32
+    assert _workspace(_cache(batch=3, **big), heads=8) > 0
+    for kw, heads in ((dict(batch=4), 8), (dict(batch=1, heads_kv=32, stride_k=32 * 64 * 128, stride_v=32 * 64 * 128,
+                                                stride_dk=2048, stride_dv=2048), 32), (dict(batch=1), 8 * 16 * 4)):
+        assert _decode(_cache(**big, **kw), heads=heads) == SHAPE, kw
