@@ -118,7 +118,7 @@ tilemix_status check_decode(const tilemix_paged_cache* c, int32_t heads_q) {
   if (st != TILEMIX_OK) return st;
   if (heads_q < 1 || heads_q > 65535 || heads_q % c->heads_kv != 0)
     return fail(TILEMIX_ERR_SHAPE, "heads_q (%d) must be a multiple of heads_kv (%d), at most 65535", heads_q, c->heads_kv);
-  if (tilemix::plan_paged_decode(pool_of(c), heads_q, c->head_dim).units > (1LL << 30))
+  if (tilemix::plan_paged_decode(pool_of(c), heads_q, c->head_dim, 0).units > (1LL << 30))
     return fail(TILEMIX_ERR_SHAPE, "batch * heads * max_pages * page_size is too large");
   return TILEMIX_OK;
 }
@@ -171,7 +171,7 @@ tilemix_status tilemix_paged_decode_workspace_size(const tilemix_paged_cache* ca
   const tilemix_status st = check_decode(cache, heads_q);
   if (st != TILEMIX_OK) return st;
   if (!bytes) return fail(TILEMIX_ERR_NULL, "bytes is NULL");
-  *bytes = decode_bytes(cache, tilemix::plan_paged_decode(pool_of(cache), heads_q, cache->head_dim)).total();
+  *bytes = decode_bytes(cache, tilemix::plan_paged_decode(pool_of(cache), heads_q, cache->head_dim, 0)).total();
   return ok();
 }
 
@@ -190,7 +190,7 @@ tilemix_status tilemix_paged_decode(const tilemix_paged_cache* cache, int32_t ty
     return fail(TILEMIX_ERR_ALIGN, "Q and O must be 16-byte and lse 4-byte aligned");
   tilemix::PagedDecodeArgs a{};
   a.pool = pool_of(cache);
-  const tilemix::PagedDecodePlan pl = tilemix::plan_paged_decode(a.pool, heads_q, cache->head_dim);
+  const tilemix::PagedDecodePlan pl = tilemix::plan_paged_decode(a.pool, heads_q, cache->head_dim, window);
   const DecodeBytes need = decode_bytes(cache, pl);
   if (need.total()) {
     if (!workspace) return fail(TILEMIX_ERR_WORKSPACE, "workspace is NULL");

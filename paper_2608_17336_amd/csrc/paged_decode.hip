@@ -54,11 +54,13 @@ __device__ __forceinline__ int load_uniform(const int* p) {
 //   kPieces: each is cut into equal pieces, the fewest of `quota` tiles at most, and a workgroup takes one piece.
 //   kRuns: each takes kPartStart units, for what it costs to begin and end one, and then a unit for each of its
 //     tiles; workgroup w takes the tiles in units [w quota, (w + 1) quota).
-//   kWhole: a workgroup takes `quota` of them, none is shared by workgroups and nothing has to be joined: where
-//     no sequence can be long (see plan_paged_decode).
-// Runs share the tiles evenly, pieces begin and end one sequence only: pieces are taken where their number
-// fits the workgroups with at most kPartStart tiles more each than the even share.  Every wave finds its place for
-// itself: a lane takes a run of sequences.
+//   kWhole: a workgroup takes `quota` of them, and none is shared by workgroups.
+// kWhole is taken where that leaves no workgroup with more than 1.6 times the even share of tiles: memory is as busy with
+// fewer waves, and what it costs to cut and join is saved (64 equal sequences of 4000 keys, INT8, 8 KV heads, d = 128,
+// 90.7 us, cut into runs 100.7; 128 of them 173.3 and 187.8; at 2 times the share, 48 of them, 80.6 and 74.7).  Runs
+// share the tiles evenly, pieces begin and end one sequence only: pieces are taken where their number fits the
+// workgroups with at most kPartStart tiles more each than the even share (with up to twice the share 64 sequences of 1
+// to 4000 keys took 67.3 us, in runs 57.5).  Every wave finds its place for itself: a lane takes a run of sequences.
 enum { kPieces, kRuns, kWhole };
 
 // n / d for 0 <= n < 2^31, d >= 1 and quotients below 2^20: an estimate in FP32, off by one at most, and a
@@ -68,6 +70,17 @@ __device__ __forceinline__ int small_quotient(int n, int d) {
   return q + (r >= d ? 1 : 0) - (r < 0 ? 1 : 0);
 }
 __device__ __forceinline__ int ceil_div(int n, int d) { return small_quotient(n + d - 1, d); }
+
+// The largest of the lanes' x >= 0.
+__device__ __forceinline__ int wave_max(int x) {
+  x = max(x, dpp<0x111>(0, x));
+  x = max(x, dpp<0x112>(0, x));
+  x = max(x, dpp<0x114>(0, x));
+  x = max(x, dpp<0x118>(0, x));
+  x = max(x, dpp<0x142, 0xa>(0, x));
+  x = max(x, dpp<0x143, 0xc>(0, x));
+  return __builtin_amdgcn_readlane(x, kWave - 1);
+}
 
 struct Run {
   int b = -1, head_block, unit;   // where it begins (unit, or piece: of its sequence's); b = -1: no tile is left
@@ -95,10 +108,18 @@ struct Run {
       total = all * (a.whole / 2);   // (for want of the lengths: half of the most)
       quota = (int)a.div_workgroups.quot(all + W - 1);
     } else {
-      const int tiles = over_lane([](int n) { return n; });
+      int longest = 0;
+      const int tiles = over_lane([&](int n) { longest = max(longest, n); return n; });
       total = wave_total(tiles) * a.head_blocks;
       const int even = max(kPagedWaves, (int)a.div_workgroups.quot(total + W - 1));
-      if (B * a.head_blocks <= W) {
+      longest = wave_max(longest);
+      const int segments = B * a.head_blocks, each = (int)a.div_workgroups.quot(segments + W - 1);
+      if (5ll * each * longest <= 8ll * even) {
+        mode = kWhole;
+        own = b1 - b0;
+        all = segments;
+        quota = each;
+      } else if (segments <= W) {
         mode = kPieces;
         for (quota = even; quota <= even + kPartStart; quota += 2) {
           own = over_lane([&](int n) { return ceil_div(n, quota); });
@@ -741,20 +762,25 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedDecodeArg
 
 }  // namespace
 
-PagedDecodePlan plan_paged_decode(const PagedPool& p, int heads_q, int d) {
+PagedDecodePlan plan_paged_decode(const PagedPool& p, int heads_q, int d, int window) {
   const int G = heads_q / p.Hk;
   PagedDecodePlan pl{};
   pl.head_blocks = p.Hk * ((G + kPagedHeads - 1) / kPagedHeads);
   pl.part_heads = std::min(G, kPagedHeads);
-  const long long most = (((long long)p.max_pages << p.page_shift) + kTileKeys - 1) / kTileKeys;   // tiles of a sequence
+  long long most = (((long long)p.max_pages << p.page_shift) + kTileKeys - 1) / kTileKeys;   // tiles of a sequence
+  if (window > 0) most = std::min<long long>(most, (window + kTileKeys - 2LL) / kTileKeys + 1);
   const long long segments = (long long)p.B * pl.head_blocks;
   pl.units = segments * (most + kPartStart);
-  // No sequence is split, and the second launch saved, where none can be longer than 16 tiles (8 KV heads, INT8, d
-  // 128: 32 sequences of 500 keys 10.8 us, split 18.3; 1 of 250 7.5 and 9.6), or 32 where there is one for every CU (32
-  // of 1000 keys 15.4 and 22.6, 128 48.2 and 64.0, 200, a little over two rounds of workgroups, 98.7 and 92.3).
-  // Beyond, splitting pays (8 of 1000 keys 14.9 and 13.1; 200 of 2000 keys 181 and 157).
-  pl.whole = most <= (segments >= kCUs ? 32 : 16) ? (int)most : 0;
-  pl.workgroups = std::min<long long>(kCUs * resident_per_cu(d),
+  const long long resident = kCUs * resident_per_cu(d);
+  // Where sequences cannot be long none is split whatever their lengths, and no second launch joins them.  How long,
+  // depends on how many workgroups that leaves; us without and with a split, INT8, 8 KV heads, d = 128:
+  //   16 tiles     1 sequence of 250 keys 7.5 and 9.6; 8 of 1000 keys 14.9 and 13.1
+  //   32 from 128  16 of 1000 keys 15.0 and 16.6, 24 15.1 and 19.1; 16 of 1500 keys 19.5 and 18.3
+  //   64 from 192  24 of 2000 keys 25.7 and 27.5, 32 28.4 and 35.9, 64 47.5 and 59.3; 24 of 4000 keys 45.1 and 42.7
+  //   32 where workgroups take several: 128 of 1 to 2000 keys 75.4 and 65.5, of 1 to 1000 41.3 and 41.1
+  const long long limit = segments < kCUs / 2 ? 16 : segments < kCUs * 3 / 4 || segments > resident ? 32 : 64;
+  pl.whole = most <= limit ? (int)most : 0;
+  pl.workgroups = std::min<long long>(resident,
                                       pl.whole ? segments : (segments * most + kPagedWaves - 1) / kPagedWaves);
   return pl;
 }

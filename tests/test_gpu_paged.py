@@ -449,6 +449,13 @@ def test_decode_capacities(fmt, dtype, Hq, B, slots):
 
 
 @pytest.mark.parametrize("fmt,dtype", PAIRS)
+@pytest.mark.parametrize("B,per", [(100, 17), (250, 9)])
+def test_decode_alike_lengths_in_long_page_tables(fmt, dtype, B, per):
+    """Nearly equal sequences, as many as the workgroups that run at once or twice as many."""
+    _decode_case(fmt, dtype, 128, 1, 64, 128, [300 - b % 7 for b in range(B - 1)] + [0], seed=1800, per=per)
+
+
+@pytest.mark.parametrize("fmt,dtype", PAIRS)
 @pytest.mark.parametrize("lens", [[65900, 0, 1, 100], [22000, 23000, 21100]])
 def test_decode_of_a_large_batch(fmt, dtype, lens):
     """Caches larger than 2^27 bytes.  Few pages, each named many times (a prefix that sequences share)."""
