@@ -693,19 +693,24 @@ void paged_decode_kernel(PagedDecodeArgs a) {
 }
 
 // One workgroup per (query head, sequence, 32 channels): thread (part, channel quad) joins every kParts-th row with
-// a running reference of its own; the parts are joined in LDS.
+// a running reference of its own.
 constexpr int kJoinThreads = 256, kJoinChannels = 32;
+static_assert(kJoinChannels == 32);   // lanes l and l ^ 8 have the same channels
+__device__ __forceinline__ float ror8(float x) {
+  const int v = __builtin_bit_cast(int, x);
+  return __builtin_bit_cast(float, dpp<0x128>(v, v));
+}
 template <int D, int TYPE>
 __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedDecodeArgs a) {
-  constexpr int kLanes = kJoinChannels / 4, kParts = kJoinThreads / kLanes, kAhead = 4;
+  constexpr int kLanes = kJoinChannels / 4, kParts = kJoinThreads / kLanes, kWaves = kJoinThreads / kWave, kAhead = 4;
   const int hq = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
   const int hk = (int)a.div_group.quot(hq), g = hq - hk * a.group, blocks = (int)a.div_blocks.d;
   const int2 seg = reinterpret_cast<const int2*>(a.segments)[(size_t)b * a.head_blocks + hk * blocks + g / kPagedHeads];
   if (seg.y == 1) return;   // written already
   const int c4 = tid % kLanes, part = tid / kLanes, c0 = blockIdx.z * kJoinChannels;
   const float ninf = -__builtin_huge_valf();
-  __shared__ f32x4 so[kParts][kLanes];
-  __shared__ float sz[kParts], sr[kParts];
+  __shared__ f32x4 so[kWaves][kLanes];
+  __shared__ float sz[kWaves], sr[kWaves];
   // Row i of the partial results: the first may be its workgroup's second row, the others are first rows.
   auto row = [&](int i) { return (size_t)(i == 0 ? seg.x : (seg.x & ~1) + 2 * i) * a.part_heads + g % kPagedHeads; };
   const float2* rz = reinterpret_cast<const float2*>(a.part_rz);
@@ -736,23 +741,35 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedDecodeArg
     }
     ref = top;
   }
-  so[part][c4] = o;
-  if (c4 == 0) {
-    sz[part] = z;
-    sr[part] = ref;
+  // A wave's parts are joined by lane exchanges, the waves in LDS.
+  float top = fmaxf(ref, ror8(ref));
+  top = quad_rows_max(top);
+  const float f = ref == ninf ? 0.0f : __builtin_amdgcn_exp2f(ref - top);
+  auto over_parts = [&](float x) {
+    x *= f;
+    return quad_rows_sum(x + ror8(x));
+  };
+  z = over_parts(z);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) o[i] = over_parts(o[i]);
+  const int wave = tid / kWave;
+  if (tid % kWave < kLanes) so[wave][c4] = o;
+  if (tid % kWave == 0) {
+    sz[wave] = z;
+    sr[wave] = top;
   }
   __syncthreads();
   if (tid < kJoinChannels) {
-    float top = ninf;
-#pragma unroll 8
-    for (int q = 0; q < kParts; ++q) top = fmaxf(top, sr[q]);
+    top = ninf;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sr[w]);
     z = 0.0f;
     float x = 0.0f;
-#pragma unroll 8
-    for (int q = 0; q < kParts; ++q) {
-      const float f = sr[q] == ninf ? 0.0f : __builtin_amdgcn_exp2f(sr[q] - top);
-      z += sz[q] * f;
-      x += so[q][tid / 4][tid % 4] * f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float fw = sr[w] == ninf ? 0.0f : __builtin_amdgcn_exp2f(sr[w] - top);
+      z += sz[w] * fw;
+      x += so[w][tid / 4][tid % 4] * fw;
     }
     const long long at = (long long)b * a.Hq + hq;
     static_cast<uint16_t*>(a.O)[at * D + c0 + tid] = (uint16_t)float_to_bits<TYPE>(z == 0.0f ? 0.0f : x / z);
