@@ -692,22 +692,31 @@ void paged_decode_kernel(PagedDecodeArgs a) {
   else decode_run<D, TYPE, FORMAT, false>(a, run, shared);
 }
 
-// One workgroup per (query head, sequence, 32 channels): thread (part, channel quad) joins every kParts-th row with
-// a running reference of its own.
-constexpr int kJoinThreads = 256, kJoinChannels = 32;
-static_assert(kJoinChannels == 32);   // lanes l and l ^ 8 have the same channels
-__device__ __forceinline__ float ror8(float x) {
-  const int v = __builtin_bit_cast(int, x);
-  return __builtin_bit_cast(float, dpp<0x128>(v, v));
+// op over the lanes that agree in lane % LANES (8, 16 or 32).
+template <int LANES, typename OP>
+__device__ __forceinline__ float across(float x, OP op) {
+  auto bits = [](float y) { return __builtin_bit_cast(int, y); };
+  auto join = [&](int y, int z) { return op(__builtin_bit_cast(float, y), __builtin_bit_cast(float, z)); };
+  if constexpr (LANES == 8) x = join(bits(x), dpp<0x128>(bits(x), bits(x)));   // lane ^ 8
+  if constexpr (LANES <= 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(bits(x), bits(x), false, false);
+    x = join((int)r[0], (int)r[1]);
+  }
+  const auto r = __builtin_amdgcn_permlane32_swap(bits(x), bits(x), false, false);
+  return join((int)r[0], (int)r[1]);
 }
-template <int D, int TYPE>
+
+// One workgroup per (query head, sequence, CHANNELS channels): thread (part, channel quad) joins every kParts-th row
+// with a running reference of its own.
+constexpr int kJoinThreads = 256;
+template <int D, int TYPE, int CHANNELS>
 __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedDecodeArgs a) {
-  constexpr int kLanes = kJoinChannels / 4, kParts = kJoinThreads / kLanes, kWaves = kJoinThreads / kWave, kAhead = 4;
+  constexpr int kLanes = CHANNELS / 4, kParts = kJoinThreads / kLanes, kWaves = kJoinThreads / kWave, kAhead = 4;
   const int hq = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
   const int hk = (int)a.div_group.quot(hq), g = hq - hk * a.group, blocks = (int)a.div_blocks.d;
   const int2 seg = reinterpret_cast<const int2*>(a.segments)[(size_t)b * a.head_blocks + hk * blocks + g / kPagedHeads];
   if (seg.y == 1) return;   // written already
-  const int c4 = tid % kLanes, part = tid / kLanes, c0 = blockIdx.z * kJoinChannels;
+  const int c4 = tid % kLanes, part = tid / kLanes, c0 = blockIdx.z * CHANNELS;
   const float ninf = -__builtin_huge_valf();
   __shared__ f32x4 so[kWaves][kLanes];
   __shared__ float sz[kWaves], sr[kWaves];
@@ -742,13 +751,9 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedDecodeArg
     ref = top;
   }
   // A wave's parts are joined by lane exchanges, the waves in LDS.
-  float top = fmaxf(ref, ror8(ref));
-  top = quad_rows_max(top);
+  float top = across<kLanes>(ref, [](float x, float y) { return fmaxf(x, y); });
   const float f = ref == ninf ? 0.0f : __builtin_amdgcn_exp2f(ref - top);
-  auto over_parts = [&](float x) {
-    x *= f;
-    return quad_rows_sum(x + ror8(x));
-  };
+  auto over_parts = [&](float x) { return across<kLanes>(x * f, [](float x, float y) { return x + y; }); };
   z = over_parts(z);
 #pragma unroll
   for (int i = 0; i < 4; ++i) o[i] = over_parts(o[i]);
@@ -759,7 +764,7 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedDecodeArg
     sr[wave] = top;
   }
   __syncthreads();
-  if (tid < kJoinChannels) {
+  if (tid < CHANNELS) {
     top = ninf;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sr[w]);
@@ -809,9 +814,16 @@ hipError_t launch_paged_decode(PagedDecodeArgs a, const PagedDecodePlan& pl, int
   a.div_workgroups = FastDiv((uint32_t)pl.workgroups);
   return for_paged_types(d, type, format, [&](auto D, auto T, auto F) {
     hipLaunchKernelGGL((paged_decode_kernel<D(), T(), F()>), dim3((unsigned)pl.workgroups), dim3(kPagedWaves * kWave), 0, stream, a);
-    if (!pl.whole)
-      hipLaunchKernelGGL((paged_join_kernel<D(), T()>), dim3(a.Hq, a.pool.B, D() / kJoinChannels), dim3(kJoinThreads), 0,
-                         stream, a);
+    if (pl.whole) return hipGetLastError();
+    // All channels in a workgroup where there are many, most of them with nothing to join; 32 of them, and so more parts
+    // at a time, where there are few or a sequence may have many rows (one has at most as many as there are
+    // workgroups for a head block).  us, 32 and all channels, sequences of up to 4000 keys, INT8, 32 / 8 heads of d = 128:
+    // 8 sequences 12.6 and 13.0, 16 20.3 and 19.7, 64 54.9 and 51.6, 128 105.9 and 101.2; one of 32000 keys 20.5 and 23.6.
+    const dim3 grid(a.Hq, a.pool.B);
+    if ((long long)a.Hq * a.pool.B >= 512 && pl.workgroups <= 256 * pl.head_blocks)
+      hipLaunchKernelGGL((paged_join_kernel<D(), T(), D()>), grid, dim3(kJoinThreads), 0, stream, a);
+    else
+      hipLaunchKernelGGL((paged_join_kernel<D(), T(), 32>), dim3(grid.x, grid.y, D() / 32), dim3(kJoinThreads), 0, stream, a);
     return hipGetLastError();
   });
 }
