@@ -21,7 +21,8 @@ namespace {
 
 constexpr int kPagedWaves = 4;
 constexpr int kCUs = 256;
-// What it costs to begin and end a sequence and head block, in tiles.
+// What it costs to begin and end a sequence and head block, in tiles.  (us, 64 sequences of 1 to 4000 keys, INT8, 8
+// heads of d = 128: 3 tiles 58.6, 6 53.6, 9 54.6, 14 57.5.)
 constexpr int kPartStart = 6;
 constexpr int kPagedHeads = 16;                  // query heads on the columns of a matrix-core tile
 // A tile is two slabs of 16 keys.  (Four slabs of an 8-bit cache leave two waves per SIMD instead of three: 32
