@@ -441,7 +441,7 @@ tilemix_status tilemix_paged_gather(const tilemix_paged_cache* cache, int32_t ty
                                     const int32_t* cu_seqlens, int32_t len, int32_t total,
                                     void* K_out, void* V_out, void* stream);
 
-/* Bytes of device workspace tilemix_paged_decode uses for heads_q query heads (0: none). */
+/* Bytes of device workspace tilemix_paged_decode uses at most for heads_q query heads (0: none). */
 tilemix_status tilemix_paged_decode_workspace_size(const tilemix_paged_cache* cache, int32_t heads_q,
                                                    size_t* bytes);
 
@@ -460,7 +460,10 @@ tilemix_status tilemix_paged_decode_workspace_size(const tilemix_paged_cache* ca
  *             be shared with a concurrently running call; may be NULL if that size is 0
  * O = sum_j p_j v_j with p = softmax(scale q . k_j) over the tokens attended to.  Lengths are clamped
  * to [0, max_pages * page_size]; a sequence without any such token gets O = 0 and lse = -inf.
- * Scores, softmax and sums are FP32; the query is not quantised.
+ * Scores, softmax and sums are FP32; the query is not quantised.  Weights are multiplied as two
+ * 16-bit pieces: 22 significant bits down to 2^-40 of the largest possible contribution (a
+ * BF16 cache: 16 bits, whatever their size).
+ * Limit: B * H_k * ceil(G / 16) * (max_pages * page_size / 32 + 6) <= 2^30, G = H_q / H_k.
  */
 tilemix_status tilemix_paged_decode(const tilemix_paged_cache* cache, int32_t type, int32_t heads_q,
                                     float scale, int32_t window, const void* Q, int64_t q_stride,
