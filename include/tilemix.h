@@ -418,7 +418,7 @@ typedef struct tilemix_paged_cache {
  *                elements apart (>= 0, multiples of 8: a slice of a fused projection needs no copy)
  * Rows whose token number is negative or past max_pages * page_size are not written, nor are
  * packed rows that no sequence owns read.  Two rows for one slot (pages shared by sequences that
- * both write them) leave either.  Out-of-range cu_seqlens are clamped as in
+ * both write them) leave any mixture of the two.  Out-of-range cu_seqlens are clamped as in
  * tilemix_prefill_varlen.
  */
 tilemix_status tilemix_paged_append(const tilemix_paged_cache* cache, int32_t type,
@@ -462,7 +462,8 @@ tilemix_status tilemix_paged_decode_workspace_size(const tilemix_paged_cache* ca
  * to [0, max_pages * page_size]; a sequence without any such token gets O = 0 and lse = -inf.
  * Scores, softmax and sums are FP32; the query is not quantised.  Weights are multiplied as two
  * 16-bit pieces: 22 significant bits down to 2^-40 of the largest possible contribution (a
- * BF16 cache: 16 bits, whatever their size).
+ * BF16 cache: 16 bits, whatever their size).  An infinity in a value that is attended to makes its
+ * channel of O infinite or NaN.
  * Limit: B * H_k * ceil(G / 16) * (max_pages * page_size / 32 + 6) <= 2^30, G = H_q / H_k.
  */
 tilemix_status tilemix_paged_decode(const tilemix_paged_cache* cache, int32_t type, int32_t heads_q,

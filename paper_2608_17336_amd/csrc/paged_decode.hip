@@ -3,11 +3,11 @@
 // For query head hq of sequence b, over the tokens j attended to (the last `window`, or all, whose page
 // exists): s_j = scale q . k_j, O = sum_j e^(s_j - m) v_j / sum_j e^(s_j - m), lse = m + ln of that sum.
 //
-//   paged_decode_kernel: as many workgroups of 4 waves as run at once share the tiles of the batch equally, each
-//     a run of consecutive ones, whatever sequences and heads they belong to.  In each (sequence, head block) of
-//     its run a workgroup's waves stream tiles with a running (max, normalizer, output) of their own in
-//     registers; they are joined in LDS, and the workgroup writes O, or a partial result where others
-//     have tiles of the same sequence and heads.
+//   paged_decode_kernel: as many workgroups of 4 waves as run at once, at most, share the tiles of the batch (see
+//     Run); a workgroup has tiles of one or several (sequence, head block)s that follow one another.  In each of
+//     them its waves stream tiles with a running (max, normalizer, output) of their own in registers; they are
+//     joined in LDS, and the workgroup writes O, or a partial result where others have tiles of the same
+//     sequence and heads.
 //   paged_join_kernel: joins the partial results of one (sequence, query head) by their log-sum-exp.
 //
 // Bound: HBM.  Each cached row is read once per block of 16 query heads, with O(1) work per byte.

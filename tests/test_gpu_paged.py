@@ -586,6 +586,24 @@ def test_decode_nan_stays_in_its_sequence(fmt, dtype):
         assert torch.equal(_bits(after[b]), _bits(before[b]))
 
 
+@pytest.mark.parametrize("fmt", ["fp16", "bf16"])
+def test_decode_infinity_stays_in_its_channel(fmt):
+    """An infinite value of a 16-bit cache reaches its channel of its sequence's heads, and nothing else."""
+    tm = _tm()
+    d, page = 128, 16
+    pool = _cached_pool(fmt, (12, 2, page, d), 820)
+    table = _table(3, 4, 12, 821)
+    lens = torch.tensor([60, 60, 60], dtype=torch.int32).cuda()
+    Q = torch.randn(3, 1, 4, d, generator=_gen(822)).to(FORMATS[fmt]).cuda()
+    before = tm.tilemix_paged_decode(_on_gpu(pool), Q, table.cuda(), lens)
+    pool[1][int(table[1, 2]), 1, 5, 9] = float("inf")                # token 37 of sequence 1, KV head 1, channel 9
+    after = tm.tilemix_paged_decode(_on_gpu(pool), Q, table.cuda(), lens)
+    hit = torch.zeros_like(before, dtype=torch.bool)
+    hit[1, 0, 2:, 9] = True
+    assert not torch.isfinite(after[hit]).any()
+    assert torch.equal(_bits(after[~hit]), _bits(before[~hit]))
+
+
 def test_decode_strided_queries_and_given_outputs():
     tm = _tm()
     d, page, B, Hq, Hk = 128, 16, 5, 8, 2
