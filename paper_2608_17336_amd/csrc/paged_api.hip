@@ -125,15 +125,15 @@ tilemix_status check_decode(const tilemix_paged_cache* c, int32_t heads_q) {
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// Workspace: [segments][part_rz][part_o], each 256-byte aligned.
+// Workspace: [segments][part_mzx][part_o], each 256-byte aligned.
 struct DecodeBytes {
-  size_t segments, rz, o;
-  size_t total() const { return segments + rz + o; }
+  size_t segments, mzx, o;
+  size_t total() const { return segments + mzx + o; }
 };
 DecodeBytes decode_bytes(const tilemix_paged_cache* c, const tilemix::PagedDecodePlan& pl) {
   if (pl.whole) return {0, 0, 0};
   const size_t rows = 2 * (size_t)pl.workgroups * pl.part_heads;
-  return {align256((size_t)c->batch * pl.head_blocks * 2 * sizeof(int)), align256(rows * 2 * sizeof(float)),
+  return {align256((size_t)c->batch * pl.head_blocks * 2 * sizeof(int)), align256(rows * 4 * sizeof(float)),
           align256(rows * c->head_dim * sizeof(float))};
 }
 
@@ -199,8 +199,8 @@ tilemix_status tilemix_paged_decode(const tilemix_paged_cache* cache, int32_t ty
       return fail(TILEMIX_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need.total());
     char* ws = static_cast<char*>(workspace);
     a.segments = reinterpret_cast<int*>(ws);
-    a.part_rz = reinterpret_cast<float*>(ws + need.segments);
-    a.part_o = reinterpret_cast<float*>(ws + need.segments + need.rz);
+    a.part_mzx = reinterpret_cast<float*>(ws + need.segments);
+    a.part_o = reinterpret_cast<float*>(ws + need.segments + need.mzx);
   }
   a.head_blocks = pl.head_blocks;
   a.whole = pl.whole;

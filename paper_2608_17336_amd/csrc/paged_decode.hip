@@ -245,16 +245,18 @@ __device__ __forceinline__ float quad_rows_sum(float x) {
   return pair_sum(__builtin_bit_cast(float, (int)r[0]) + __builtin_bit_cast(float, (int)r[1]));
 }
 
-// Weights p = 2^(s - r) are taken against a reference r near the running max m: r = m for a BF16 cache, m - 15 for
-// an FP16 one, and m - 15 + e for an 8-bit one, where 2^e is above every value scale dV so far.  The
-// weights of the codes, p dV (p for 16 bits), then stay below 2^15, and are handed to the matrix cores as
+// Weights p = 2^((s - m) - x) are taken against the running max m and a power of two, 2^x: x = 0 for a BF16 cache,
+// -15 for an FP16 one, and e - 15 for an 8-bit one, where 2^e is above every value scale dV so far.  The
+// weights of the codes, p dV (p for 16 bits), then stay at 2^15 at most, and are handed to the matrix cores as
 // two 16-bit pieces: FP16 pieces hold them to 2^-22 of themselves, and to 2^-40 of the largest possible
 // weight where they are small; BF16 pieces to 2^-16, with FP32's range.  One piece alone (2^-12 or
-// 2^-9) would add as much error as the output's own rounding.  e >= kExpMin keeps the normalizer, a sum
-// of up to 2^30 terms p <= 2^(15 - e), finite.
+// 2^-9) would add as much error as the output's own rounding.  m and x go through the joins side by side:
+// m + x is another number in FP32 where |m| is large, by more than 1 from 2^25 on, and a weight of 2^16 is no FP16
+// number any more; s - m <= 0 whatever m.  e >= kExpMin keeps the normalizer, a sum of up to 2^30 terms
+// p <= 2^(15 - e), finite.
 constexpr int kExpMin = -80;
 template <int FORMAT>
-constexpr float kHeadroom = FORMAT == TILEMIX_BF16 ? 0.0f : 15.0f;
+constexpr int kHeadroom = FORMAT == TILEMIX_BF16 ? 0 : 15;
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -279,6 +281,7 @@ __device__ __forceinline__ void split2(float w0, float w1, uint32_t& hi, uint32_
 template <int D>
 struct DecodeShared {
   float m[kPagedWaves][kPagedHeads], z[kPagedWaves][kPagedHeads];
+  int x[kPagedWaves];
   __align__(16) float o[kPagedWaves][kPagedHeads][D + 4];   // padded rows
 };
 
@@ -298,6 +301,7 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run& 
   const float ninf = -__builtin_huge_valf();
   auto& red_m = shared.m;
   auto& red_z = shared.z;
+  auto& red_x = shared.x;
   auto& osum = shared.o;
 
   const int quota = __builtin_amdgcn_readfirstlane(run.quota), mode = __builtin_amdgcn_readfirstlane(run.mode);
@@ -449,13 +453,13 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run& 
       }
     }
 
-    // 4. The wave's tiles.  m: running max (log2 units); ref: the reference r; z: this lane's share of the normalizer;
-    //    acc: output.  Loads complete in order, and a wait counts the younger ones, so rows are requested in the
+    // 4. The wave's tiles.  m: running max (log2 units); x: the weights' power of two; z: this lane's share of the
+    //    normalizer; acc: output.  Loads complete in order, and a wait counts the younger ones, so rows are requested in the
     //    same order and number on every way to a wait: the keys and their scales once the scores are
     //    formed, the values and theirs after P V, into the registers that these leave, whether there is
     //    another tile in this part, in the next one, or none.
-    float m = ninf, ref = ninf, z = 0.0f;
-    int e = kExpMin;
+    float m = ninf, z = 0.0f;
+    int x = (k8 ? kExpMin : 0) - kHeadroom<FORMAT>;
     f32x4 acc[kC];
   #pragma unroll
     for (int c = 0; c < kC; ++c) acc[c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -517,14 +521,14 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run& 
             }
           }
       }
-      // Softmax: reference, normalizer and output move when the max or the value scales' exponent grows.
+      // Softmax: normalizer and output move when the max or the value scales' exponent grows.
       float mt = sc[0][0];
   #pragma unroll
       for (int s = 0; s < kS; ++s)
   #pragma unroll
         for (int r = 0; r < 4; ++r) mt = fmaxf(mt, sc[s][r]);
       const float m_new = fmaxf(m, quad_rows_max(mt));
-      int e_new = e;
+      int x_new = x;
       if constexpr (k8) {
         float vm = 0.0f;
   #pragma unroll
@@ -532,27 +536,26 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run& 
   #pragma unroll
           for (int r = 0; r < 4; ++r) vm = fmaxf(vm, fabsf(dv[s][r]));
         vm = quad_rows_max(vm);
-        if (vm > 0.0f) e_new = max(e, __builtin_amdgcn_frexp_expf(vm));
+        if (vm > 0.0f) x_new = max(x, __builtin_amdgcn_frexp_expf(vm) - kHeadroom<FORMAT>);
       }
-      if (__any(m_new > m || e_new > e)) {
-        // No finite score so far: p = 2^(-inf - 0) = 0, not a NaN.
-        const float next = m_new == ninf ? ninf : m_new - (k8 ? kHeadroom<FORMAT> - (float)e_new : kHeadroom<FORMAT>);
-        const float alpha = ref == ninf ? 0.0f : __builtin_amdgcn_exp2f(ref - next);
+      if (__any(m_new > m || x_new > x)) {
+        const float alpha = m == ninf ? 0.0f : __builtin_amdgcn_exp2f((m - m_new) + (float)(x - x_new));
         z *= alpha;
   #pragma unroll
         for (int c = 0; c < kC; ++c) acc[c] *= alpha;
         m = m_new;
-        e = e_new;
-        ref = next;
+        x = x_new;
       }
-      const float sub = ref == ninf ? 0.0f : ref;
+      // No finite score so far: p = 2^(-inf - 0) = 0, not a NaN.
+      const float sub = m == ninf ? 0.0f : m, up = (float)-x;
       uint2 hi[kS], lo[kS];
   #pragma unroll
       for (int s = 0; s < kS; ++s) {
         float w[4];
   #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          w[r] = __builtin_amdgcn_exp2f(sc[s][r] - sub);
+          const float s_m = sc[s][r] - sub;
+          w[r] = __builtin_amdgcn_exp2f(FORMAT == TILEMIX_BF16 ? s_m : s_m + up);
           z += w[r];
           if constexpr (k8) w[r] *= dv[s][r];
         }
@@ -617,17 +620,22 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run& 
 
     // 5. The waves' results joined in LDS.
     z = quad_rows_sum(z);
-    if (lq == 0) red_m[wave][l16] = ref;
+    if (lq == 0) red_m[wave][l16] = m;
+    if (lane == 0) red_x[wave] = x;
     __syncthreads();
     float top = red_m[0][l16];
+    int xx = red_x[0];
   #pragma unroll
-    for (int w = 1; w < kPagedWaves; ++w) top = fmaxf(top, red_m[w][l16]);
-    const float fw = ref == ninf ? 0.0f : __builtin_amdgcn_exp2f(ref - top);
+    for (int w = 1; w < kPagedWaves; ++w) {
+      top = fmaxf(top, red_m[w][l16]);
+      xx = max(xx, red_x[w]);
+    }
+    const float fw = m == ninf ? 0.0f : __builtin_amdgcn_exp2f((m - top) + (float)(x - xx));
     if (lq == 0) red_z[wave][l16] = z * fw;
   #pragma unroll
     for (int r = 0; r < 4; ++r)
   #pragma unroll
-      for (int c = 0; c < kC; ++c) osum[wave][l16][(4 * lq + r) * kC + c] = ref == ninf ? 0.0f : acc[c][r] * fw;
+      for (int c = 0; c < kC; ++c) osum[wave][l16][(4 * lq + r) * kC + c] = m == ninf ? 0.0f : acc[c][r] * fw;
     __syncthreads();
     const bool whole = cur.lo == 0 && cur.hi == cur.span.share();
     // Partial results: of the workgroup's first part in row 2 w, of one behind others in row 2 w + 1 (it is the
@@ -662,9 +670,9 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run& 
       if (whole) {
         if (a.lse)
           a.lse[(long long)cur.b * a.Hq + hq0 + tid] =
-              zz == 0.0f ? ninf : 0.69314718056f * (mm + __builtin_amdgcn_logf(zz));
+              zz == 0.0f ? ninf : 0.69314718056f * (mm + (__builtin_amdgcn_logf(zz) + (float)xx));
       } else {
-        reinterpret_cast<float2*>(a.part_rz)[(size_t)part_row * a.part_heads + tid] = make_float2(mm, zz);
+        reinterpret_cast<float4*>(a.part_mzx)[(size_t)part_row * a.part_heads + tid] = make_float4(mm, zz, (float)xx, 0.0f);
       }
     }
     // For the join: the first row, and how many workgroups there are from this one on.
@@ -708,7 +716,7 @@ __device__ __forceinline__ float across(float x, OP op) {
 }
 
 // One workgroup per (query head, sequence, CHANNELS channels): thread (part, channel quad) joins every kParts-th row
-// with a running reference of its own.
+// with a running max and power of two of its own.
 constexpr int kJoinThreads = 256;
 template <int D, int TYPE, int CHANNELS>
 __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedDecodeArgs a) {
@@ -720,40 +728,45 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedDecodeArg
   const int c4 = tid % kLanes, part = tid / kLanes, c0 = blockIdx.z * CHANNELS;
   const float ninf = -__builtin_huge_valf();
   __shared__ f32x4 so[kWaves][kLanes];
-  __shared__ float sz[kWaves], sr[kWaves];
+  __shared__ float sz[kWaves], sm[kWaves], sx[kWaves];
   // Row i of the partial results: the first may be its workgroup's second row, the others are first rows.
   auto row = [&](int i) { return (size_t)(i == 0 ? seg.x : (seg.x & ~1) + 2 * i) * a.part_heads + g % kPagedHeads; };
-  const float2* rz = reinterpret_cast<const float2*>(a.part_rz);
-  float ref = ninf, z = 0.0f;
+  const float4* mzx = reinterpret_cast<const float4*>(a.part_mzx);
+  float m = ninf, x = ninf, z = 0.0f;
   f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
   for (int i0 = part; i0 < seg.y; i0 += kParts * kAhead) {
-    float2 x[kAhead];
+    float4 ri[kAhead];
     f32x4 oi[kAhead];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       const size_t r = row(min(i0 + u * kParts, seg.y - 1));
-      x[u] = rz[r];
+      ri[u] = mzx[r];
       oi[u] = *reinterpret_cast<const f32x4*>(a.part_o + r * D + c0 + 4 * c4);
     }
-    float top = ref;
+    float top = m, xx = x;
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) top = fmaxf(top, x[u].x);
-    const float f = ref == ninf ? 0.0f : __builtin_amdgcn_exp2f(ref - top);
+    for (int u = 0; u < kAhead; ++u) {
+      top = fmaxf(top, ri[u].x);
+      xx = fmaxf(xx, ri[u].z);
+    }
+    const float f = m == ninf ? 0.0f : __builtin_amdgcn_exp2f((m - top) + (x - xx));
     z *= f;
     o *= f;
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       if (i0 + u * kParts >= seg.y) break;
       // (A row without a finite score may hold a NaN as its normalizer.)
-      const float fu = x[u].x == ninf ? 0.0f : __builtin_amdgcn_exp2f(x[u].x - top);
-      z += x[u].y * fu;
+      const float fu = ri[u].x == ninf ? 0.0f : __builtin_amdgcn_exp2f((ri[u].x - top) + (ri[u].z - xx));
+      z += ri[u].y * fu;
       o += oi[u] * fu;
     }
-    ref = top;
+    m = top;
+    x = xx;
   }
   // A wave's parts are joined by lane exchanges, the waves in LDS.
-  float top = across<kLanes>(ref, [](float x, float y) { return fmaxf(x, y); });
-  const float f = ref == ninf ? 0.0f : __builtin_amdgcn_exp2f(ref - top);
+  auto larger = [](float x, float y) { return fmaxf(x, y); };
+  float top = across<kLanes>(m, larger), xx = across<kLanes>(x, larger);
+  const float f = m == ninf ? 0.0f : __builtin_amdgcn_exp2f((m - top) + (x - xx));
   auto over_parts = [&](float x) { return across<kLanes>(x * f, [](float x, float y) { return x + y; }); };
   z = over_parts(z);
 #pragma unroll
@@ -762,24 +775,28 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedDecodeArg
   if (tid % kWave < kLanes) so[wave][c4] = o;
   if (tid % kWave == 0) {
     sz[wave] = z;
-    sr[wave] = top;
+    sm[wave] = top;
+    sx[wave] = xx;
   }
   __syncthreads();
   if (tid < CHANNELS) {
-    top = ninf;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sr[w]);
-    z = 0.0f;
-    float x = 0.0f;
+    top = xx = ninf;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-      const float fw = sr[w] == ninf ? 0.0f : __builtin_amdgcn_exp2f(sr[w] - top);
+      top = fmaxf(top, sm[w]);
+      xx = fmaxf(xx, sx[w]);
+    }
+    z = 0.0f;
+    float y = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float fw = sm[w] == ninf ? 0.0f : __builtin_amdgcn_exp2f((sm[w] - top) + (sx[w] - xx));
       z += sz[w] * fw;
-      x += so[w][tid / 4][tid % 4] * fw;
+      y += so[w][tid / 4][tid % 4] * fw;
     }
     const long long at = (long long)b * a.Hq + hq;
-    static_cast<uint16_t*>(a.O)[at * D + c0 + tid] = (uint16_t)float_to_bits<TYPE>(z == 0.0f ? 0.0f : x / z);
-    if (tid == 0 && c0 == 0 && a.lse) a.lse[at] = z == 0.0f ? ninf : 0.69314718056f * (top + __builtin_amdgcn_logf(z));
+    static_cast<uint16_t*>(a.O)[at * D + c0 + tid] = (uint16_t)float_to_bits<TYPE>(z == 0.0f ? 0.0f : y / z);
+    if (tid == 0 && c0 == 0 && a.lse) a.lse[at] = z == 0.0f ? ninf : 0.69314718056f * (top + (__builtin_amdgcn_logf(z) + xx));
   }
 }
 

@@ -1,0 +1,67 @@
+"""GPU: decode over the paged cache with scores, values and queries far from 1."""
+
+import numpy as np
+import pytest
+import torch
+
+from gpu_util import log
+from test_gpu_paged import FORMATS, PAIRS, _gen, _tm, _values
+
+pytestmark = pytest.mark.gpu
+
+
+def _cache_of(fmt, K, V, page):
+    """K, V [L, d] (16 bits, CPU) written as the only sequence of a pool with one KV head: cache, table, lengths, and
+    the float64 keys and values that the cache stands for."""
+    tm = _tm()
+    L, d = K.shape
+    pages = -(-L // page)
+    cache = tm.PagedCache.empty(pages, page, 1, d, FORMATS[fmt])
+    table = torch.randperm(pages, generator=_gen(1)).to(torch.int32).view(1, pages)
+    lens = torch.tensor([L], dtype=torch.int32).cuda()
+    tm.tilemix_paged_append(cache, K[None, :, None].cuda(), V[None, :, None].cuda(), table.cuda(), lens)
+    torch.cuda.synchronize()
+    host = [None if t is None else t.cpu() for t in cache]
+    k, v = (_values(host, op, fmt)[table[0].numpy(), 0].reshape(-1, d)[:L] for op in (0, 1))
+    return cache, table.cuda(), lens, k, v
+
+
+def _decode(cache, table, lens, Q, scale=None):
+    """(O [Hq, d], lse [Hq]) as float64."""
+    O, lse = _tm().tilemix_paged_decode(cache, Q.cuda(), table, lens, scale, return_lse=True)
+    torch.cuda.synchronize()
+    return O[0, 0].double().cpu().numpy(), lse[0].double().cpu().numpy()
+
+
+# ------------------------------------------------------------------------------------ large scores
+
+@pytest.mark.parametrize("fmt,dtype", PAIRS)
+@pytest.mark.parametrize("L", [1, 3, 40, 300, 9000])
+def test_large_scores(fmt, dtype, L):
+    """Scores of 2^23 to 2^28 (log2 units), from ordinary FP16 numbers.  Two thirds of the keys equal the query up to a
+    factor, the others are their negatives: the former have the same score, so equal weights, the latter's are 0, and
+    O is the mean of the former's values.  Equal scores are equal to the last bit, whatever they were rounded to, so
+    that what is left is the weights' pieces (2^-15 for a BF16 cache, 2^-22 for the others), sums of n terms and the
+    normalizer (n 2^-24 each), a quotient and the output's rounding.  lse: d products and sums, the scale and its
+    product with log2 e, and the last product, relative to the score."""
+    d, page = 128, 64
+    f = torch.finfo(FORMATS[dtype])
+    for i, (q, v_gain) in enumerate([(300.0, 1.0), (1500.0, 1.0), (1500.0, 0.3), (2600.0, 37.0), (4000.0, 0.6), (7000.0, 1.0)]):
+        sign = torch.ones(L, 1)
+        sign[2::3] = -1
+        K = (sign * 1500.0).expand(L, d).to(FORMATS[dtype])
+        V = (torch.randn(L, d, generator=_gen(10 + i)) * v_gain).to(FORMATS[dtype])
+        cache, table, lens, k, v = _cache_of(fmt, K, V, page)
+        Q = torch.full((1, 1, 3, d), q).to(FORMATS[dtype])
+        log(f"large scores {fmt}/{dtype} L {L} q {q}")
+        O, lse = _decode(cache, table, lens, Q)
+        heavy = sign[:, 0].numpy() > 0
+        n = int(heavy.sum())
+        want, mass = v[heavy].mean(0), np.abs(v[heavy]).mean(0)
+        piece = 2.0 ** -15 if fmt == "bf16" else 2.0 ** -22
+        v_max = 0.0 if fmt == "bf16" else np.abs(v).max()
+        tol = f.eps / 2 * np.abs(want) + f.smallest_normal * f.eps + (piece + (2 * n + 4) * 2.0 ** -24) * mass + n * 2.0 ** -39 * v_max
+        s = d ** -0.5 * (k[0] @ Q[0, 0, 0].double().numpy())
+        for h in range(3):
+            assert (np.abs(O[h] - want) <= tol * (1 + f.eps)).all(), (q, h)
+            assert abs(lse[h] - (s + np.log(n))) <= (d + 8) * 2.0 ** -24 * s, (q, h)
