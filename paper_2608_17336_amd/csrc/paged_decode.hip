@@ -245,15 +245,14 @@ __device__ __forceinline__ float quad_rows_sum(float x) {
   return pair_sum(__builtin_bit_cast(float, (int)r[0]) + __builtin_bit_cast(float, (int)r[1]));
 }
 
-// Weights p = 2^((s - m) - x) are taken against the running max m and a power of two, 2^x: x = 0 for a BF16 cache,
-// -15 for an FP16 one, and e - 15 for an 8-bit one, where 2^e is above every value scale dV so far.  The
-// weights of the codes, p dV (p for 16 bits), then stay at 2^15 at most, and are handed to the matrix cores as
+// p = 2^(s - m) is taken against the running max m, and so is the normalizer z = sum p.  The weights of the codes
+// are p dV 2^-x (p 2^-x for 16 bits): x = 0 for a BF16 cache, -15 for an FP16 one, and e - 15 for an 8-bit
+// one, where 2^e is above every value scale dV so far.  They stay at 2^15 at most, and are handed to the matrix cores as
 // two 16-bit pieces: FP16 pieces hold them to 2^-22 of themselves, and to 2^-40 of the largest possible
 // weight where they are small; BF16 pieces to 2^-16, with FP32's range.  One piece alone (2^-12 or
 // 2^-9) would add as much error as the output's own rounding.  m and x go through the joins side by side:
 // m + x is another number in FP32 where |m| is large, by more than 1 from 2^25 on, and a weight of 2^16 is no FP16
-// number any more; s - m <= 0 whatever m.  e >= kExpMin keeps the normalizer, a sum of up to 2^30 terms
-// p <= 2^(15 - e), finite.
+// number any more; and z, which knows nothing of x, loses nothing to a value's size.  kExpMin: the least e.
 constexpr int kExpMin = -80;
 template <int FORMAT>
 constexpr int kHeadroom = FORMAT == TILEMIX_BF16 ? 0 : 15;
@@ -539,25 +538,26 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run& 
         if (vm > 0.0f) x_new = max(x, __builtin_amdgcn_frexp_expf(vm) - kHeadroom<FORMAT>);
       }
       if (__any(m_new > m || x_new > x)) {
-        const float alpha = m == ninf ? 0.0f : __builtin_amdgcn_exp2f((m - m_new) + (float)(x - x_new));
+        const float alpha = m == ninf ? 0.0f : __builtin_amdgcn_exp2f(m - m_new);
+        const float beta = k8 ? __builtin_amdgcn_ldexpf(alpha, x - x_new) : alpha;
         z *= alpha;
   #pragma unroll
-        for (int c = 0; c < kC; ++c) acc[c] *= alpha;
+        for (int c = 0; c < kC; ++c) acc[c] *= beta;
         m = m_new;
         x = x_new;
       }
       // No finite score so far: p = 2^(-inf - 0) = 0, not a NaN.
-      const float sub = m == ninf ? 0.0f : m, up = (float)-x;
+      const float sub = m == ninf ? 0.0f : m;
       uint2 hi[kS], lo[kS];
   #pragma unroll
       for (int s = 0; s < kS; ++s) {
         float w[4];
   #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const float s_m = sc[s][r] - sub;
-          w[r] = __builtin_amdgcn_exp2f(FORMAT == TILEMIX_BF16 ? s_m : s_m + up);
+          w[r] = __builtin_amdgcn_exp2f(sc[s][r] - sub);
           z += w[r];
-          if constexpr (k8) w[r] *= dv[s][r];
+          if constexpr (k8) w[r] *= __builtin_amdgcn_ldexpf(dv[s][r], -x);
+          else if constexpr (FORMAT == TILEMIX_FP16) w[r] *= 0x1p15f;
         }
         split2<FORMAT>(w[0], w[1], hi[s].x, lo[s].x);
         split2<FORMAT>(w[2], w[3], hi[s].y, lo[s].y);
@@ -630,8 +630,8 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run& 
       top = fmaxf(top, red_m[w][l16]);
       xx = max(xx, red_x[w]);
     }
-    const float fw = m == ninf ? 0.0f : __builtin_amdgcn_exp2f((m - top) + (float)(x - xx));
-    if (lq == 0) red_z[wave][l16] = z * fw;
+    const float fz = m == ninf ? 0.0f : __builtin_amdgcn_exp2f(m - top), fw = k8 ? __builtin_amdgcn_ldexpf(fz, x - xx) : fz;
+    if (lq == 0) red_z[wave][l16] = z * fz;
   #pragma unroll
     for (int r = 0; r < 4; ++r)
   #pragma unroll
@@ -653,7 +653,7 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run& 
       if (whole) {
         uint32_t h[4];
   #pragma unroll
-        for (int r = 0; r < 4; ++r) h[r] = float_to_bits<TYPE>(zz == 0.0f ? 0.0f : sum[r] / zz);
+        for (int r = 0; r < 4; ++r) h[r] = float_to_bits<TYPE>(zz == 0.0f ? 0.0f : __builtin_amdgcn_ldexpf(sum[r] / zz, xx));
         *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.O) + ((long long)cur.b * a.Hq + hq0 + g) * D + c) =
             make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
       } else {
@@ -670,9 +670,9 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run& 
       if (whole) {
         if (a.lse)
           a.lse[(long long)cur.b * a.Hq + hq0 + tid] =
-              zz == 0.0f ? ninf : 0.69314718056f * (mm + (__builtin_amdgcn_logf(zz) + (float)xx));
+              zz == 0.0f ? ninf : 0.69314718056f * (mm + __builtin_amdgcn_logf(zz));
       } else {
-        reinterpret_cast<float4*>(a.part_mzx)[(size_t)part_row * a.part_heads + tid] = make_float4(mm, zz, (float)xx, 0.0f);
+        reinterpret_cast<float4*>(a.part_mzx)[(size_t)part_row * a.part_heads + tid] = make_float4(mm, zz, __int_as_float(xx), 0.0f);
       }
     }
     // For the join: the first row, and how many workgroups there are from this one on.
@@ -702,10 +702,10 @@ void paged_decode_kernel(PagedDecodeArgs a) {
 }
 
 // op over the lanes that agree in lane % LANES (8, 16 or 32).
-template <int LANES, typename OP>
-__device__ __forceinline__ float across(float x, OP op) {
-  auto bits = [](float y) { return __builtin_bit_cast(int, y); };
-  auto join = [&](int y, int z) { return op(__builtin_bit_cast(float, y), __builtin_bit_cast(float, z)); };
+template <int LANES, typename T, typename OP>
+__device__ __forceinline__ T across(T x, OP op) {
+  auto bits = [](T y) { return __builtin_bit_cast(int, y); };
+  auto join = [&](int y, int z) { return op(__builtin_bit_cast(T, y), __builtin_bit_cast(T, z)); };
   if constexpr (LANES == 8) x = join(bits(x), dpp<0x128>(bits(x), bits(x)));   // lane ^ 8
   if constexpr (LANES <= 16) {
     const auto r = __builtin_amdgcn_permlane16_swap(bits(x), bits(x), false, false);
@@ -716,7 +716,8 @@ __device__ __forceinline__ float across(float x, OP op) {
 }
 
 // One workgroup per (query head, sequence, CHANNELS channels): thread (part, channel quad) joins every kParts-th row
-// with a running max and power of two of its own.
+// with a running max and power of two of its own.  kNoExp: below every row's power.
+constexpr int kNoExp = -1024;
 constexpr int kJoinThreads = 256;
 template <int D, int TYPE, int CHANNELS>
 __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedDecodeArgs a) {
@@ -728,11 +729,13 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedDecodeArg
   const int c4 = tid % kLanes, part = tid / kLanes, c0 = blockIdx.z * CHANNELS;
   const float ninf = -__builtin_huge_valf();
   __shared__ f32x4 so[kWaves][kLanes];
-  __shared__ float sz[kWaves], sm[kWaves], sx[kWaves];
+  __shared__ float sz[kWaves], sm[kWaves];
+  __shared__ int sx[kWaves];
   // Row i of the partial results: the first may be its workgroup's second row, the others are first rows.
   auto row = [&](int i) { return (size_t)(i == 0 ? seg.x : (seg.x & ~1) + 2 * i) * a.part_heads + g % kPagedHeads; };
   const float4* mzx = reinterpret_cast<const float4*>(a.part_mzx);
-  float m = ninf, x = ninf, z = 0.0f;
+  float m = ninf, z = 0.0f;
+  int x = kNoExp;
   f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
   for (int i0 = part; i0 < seg.y; i0 += kParts * kAhead) {
     float4 ri[kAhead];
@@ -743,34 +746,36 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedDecodeArg
       ri[u] = mzx[r];
       oi[u] = *reinterpret_cast<const f32x4*>(a.part_o + r * D + c0 + 4 * c4);
     }
-    float top = m, xx = x;
+    float top = m;
+    int xx = x;
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       top = fmaxf(top, ri[u].x);
-      xx = fmaxf(xx, ri[u].z);
+      xx = max(xx, __float_as_int(ri[u].z));
     }
-    const float f = m == ninf ? 0.0f : __builtin_amdgcn_exp2f((m - top) + (x - xx));
+    const float f = m == ninf ? 0.0f : __builtin_amdgcn_exp2f(m - top);
     z *= f;
-    o *= f;
+    o *= __builtin_amdgcn_ldexpf(f, x - xx);
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       if (i0 + u * kParts >= seg.y) break;
       // (A row without a finite score may hold a NaN as its normalizer.)
-      const float fu = ri[u].x == ninf ? 0.0f : __builtin_amdgcn_exp2f((ri[u].x - top) + (ri[u].z - xx));
+      const float fu = ri[u].x == ninf ? 0.0f : __builtin_amdgcn_exp2f(ri[u].x - top);
       z += ri[u].y * fu;
-      o += oi[u] * fu;
+      o += oi[u] * __builtin_amdgcn_ldexpf(fu, __float_as_int(ri[u].z) - xx);
     }
     m = top;
     x = xx;
   }
   // A wave's parts are joined by lane exchanges, the waves in LDS.
-  auto larger = [](float x, float y) { return fmaxf(x, y); };
-  float top = across<kLanes>(m, larger), xx = across<kLanes>(x, larger);
-  const float f = m == ninf ? 0.0f : __builtin_amdgcn_exp2f((m - top) + (x - xx));
-  auto over_parts = [&](float x) { return across<kLanes>(x * f, [](float x, float y) { return x + y; }); };
-  z = over_parts(z);
+  auto larger = [](auto x, auto y) { return x > y ? x : y; };
+  auto plus = [](float x, float y) { return x + y; };
+  float top = across<kLanes>(m, larger);
+  int xx = across<kLanes>(x, larger);
+  const float f = m == ninf ? 0.0f : __builtin_amdgcn_exp2f(m - top), fo = __builtin_amdgcn_ldexpf(f, x - xx);
+  z = across<kLanes>(z * f, plus);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) o[i] = over_parts(o[i]);
+  for (int i = 0; i < 4; ++i) o[i] = across<kLanes>(o[i] * fo, plus);
   const int wave = tid / kWave;
   if (tid % kWave < kLanes) so[wave][c4] = o;
   if (tid % kWave == 0) {
@@ -780,23 +785,24 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedDecodeArg
   }
   __syncthreads();
   if (tid < CHANNELS) {
-    top = xx = ninf;
+    top = ninf;
+    xx = kNoExp;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
       top = fmaxf(top, sm[w]);
-      xx = fmaxf(xx, sx[w]);
+      xx = max(xx, sx[w]);
     }
     z = 0.0f;
     float y = 0.0f;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-      const float fw = sm[w] == ninf ? 0.0f : __builtin_amdgcn_exp2f((sm[w] - top) + (sx[w] - xx));
+      const float fw = sm[w] == ninf ? 0.0f : __builtin_amdgcn_exp2f(sm[w] - top);
       z += sz[w] * fw;
-      y += so[w][tid / 4][tid % 4] * fw;
+      y += so[w][tid / 4][tid % 4] * __builtin_amdgcn_ldexpf(fw, sx[w] - xx);
     }
     const long long at = (long long)b * a.Hq + hq;
-    static_cast<uint16_t*>(a.O)[at * D + c0 + tid] = (uint16_t)float_to_bits<TYPE>(z == 0.0f ? 0.0f : y / z);
-    if (tid == 0 && c0 == 0 && a.lse) a.lse[at] = z == 0.0f ? ninf : 0.69314718056f * (top + (__builtin_amdgcn_logf(z) + xx));
+    static_cast<uint16_t*>(a.O)[at * D + c0 + tid] = (uint16_t)float_to_bits<TYPE>(z == 0.0f ? 0.0f : __builtin_amdgcn_ldexpf(y / z, xx));
+    if (tid == 0 && c0 == 0 && a.lse) a.lse[at] = z == 0.0f ? ninf : 0.69314718056f * (top + __builtin_amdgcn_logf(z));
   }
 }
 

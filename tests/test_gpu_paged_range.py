@@ -65,3 +65,30 @@ def test_large_scores(fmt, dtype, L):
         for h in range(3):
             assert (np.abs(O[h] - want) <= tol * (1 + f.eps)).all(), (q, h)
             assert abs(lse[h] - (s + np.log(n))) <= (d + 8) * 2.0 ** -24 * s, (q, h)
+
+
+# ------------------------------------------------------------- values of very different magnitudes
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("first", [0, 60])
+@pytest.mark.parametrize("L,cut", [(64, 32), (160, 128), (320, 48), (9000, 4500), (9000, 8990)])
+def test_values_of_zero_beside_large_ones(fmt, first, L, cut):
+    """Tokens before `cut` have values 0 (first = 0) or around 2^-60, those behind it around 2^60, and the other way
+    round; all keys are 0, so all scores are.  The cut lies between tiles of one wave, of several, and between
+    workgroups.  Every token counts alike: lse = ln L, and O is the mean of the values.  Weights' pieces (2^-22) and
+    sums (L 2^-24) as ever; lse: the normalizer's sum and the logarithm."""
+    d, page = 64, 16
+    f = torch.finfo(torch.bfloat16)
+    for turn in (False, True):
+        gain = torch.full((L, 1), 2.0 ** 60)
+        gain[:cut] = 2.0 ** -first if first else 0.0
+        V = (torch.randn(L, d, generator=_gen(30)) * (gain.flip(0) if turn else gain)).bfloat16()
+        cache, table, lens, k, v = _cache_of(fmt, torch.zeros(L, d).bfloat16(), V, page)
+        Q = torch.randn(1, 1, 2, d, generator=_gen(31)).bfloat16()
+        log(f"values of zero beside large ones {fmt} 2^-{first} L {L} cut {cut} turned {turn}")
+        O, lse = _decode(cache, table, lens, Q)
+        want, mass = v.mean(0), np.abs(v).mean(0)
+        tol = f.eps / 2 * np.abs(want) + (2.0 ** -22 + (2 * L + 4) * 2.0 ** -24) * mass + L * 2.0 ** -39 * np.abs(v).max()
+        for h in range(2):
+            assert (np.abs(O[h] - want) <= tol * (1 + f.eps)).all(), (turn, h)
+            assert abs(lse[h] - np.log(L)) <= L * 2.0 ** -24 + 2.0 ** -21 * np.log(L), (turn, h)
