@@ -252,8 +252,9 @@ __device__ __forceinline__ float quad_rows_sum(float x) {
 // weight where they are small; BF16 pieces to 2^-16, with FP32's range.  One piece alone (2^-12 or
 // 2^-9) would add as much error as the output's own rounding.  m and x go through the joins side by side:
 // m + x is another number in FP32 where |m| is large, by more than 1 from 2^25 on, and a weight of 2^16 is no FP16
-// number any more; and z, which knows nothing of x, loses nothing to a value's size.  kExpMin: the least e.
-constexpr int kExpMin = -80;
+// number any more; and z, which knows nothing of x, loses nothing to a value's size.  e starts at kExpMin, that of the
+// smallest subnormal scale, 2^-149: values near BF16's smallest are weighted like any others.
+constexpr int kExpMin = -148;
 template <int FORMAT>
 constexpr int kHeadroom = FORMAT == TILEMIX_BF16 ? 0 : 15;
 

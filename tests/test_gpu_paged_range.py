@@ -92,3 +92,30 @@ def test_values_of_zero_beside_large_ones(fmt, first, L, cut):
         for h in range(2):
             assert (np.abs(O[h] - want) <= tol * (1 + f.eps)).all(), (turn, h)
             assert abs(lse[h] - np.log(L)) <= L * 2.0 ** -24 + 2.0 ** -21 * np.log(L), (turn, h)
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("L", [5, 300, 5000])
+@pytest.mark.parametrize("power", [-126, -120, -115, -110, -105, -100, -90, 100, 126])
+def test_values_over_all_of_bf16(fmt, L, power):
+    """BF16 values around 2^power, down to where the scales of their rows are subnormal, and no other ones.  Scores are
+    exact (keys of one channel, +-1): weights are off by the exponent's argument and the exponent (2^-21 of scores up
+    to 2), the pieces and sums; O by its rounding, to a multiple of 2^-133 at the bottom, and by one more in FP32."""
+    d, page = 128, 32
+    f = torch.finfo(torch.bfloat16)
+    K = torch.zeros(L, d)
+    K[:, 0] = torch.where(torch.arange(L) % 5 < 2, 1.0, -1.0)
+    V = (torch.randn(L, d, generator=_gen(40)).clamp(-3, 3).double() * 2.0 ** (power - 1)).bfloat16()
+    cache, table, lens, k, v = _cache_of(fmt, K.bfloat16(), V, page)
+    Q = torch.zeros(1, 1, 2, d)
+    Q[:, :, 0, 0], Q[:, :, 1, 0] = 1.0, -1.0
+    log(f"values of 2^{power} {fmt} L {L}")
+    O, lse = _decode(cache, table, lens, Q.bfloat16(), 0.75)
+    for h, sign in ((0, 1.0), (1, -1.0)):
+        s = 0.75 * sign * k[:, 0]
+        p = np.exp(s)
+        want, mass = p @ v / p.sum(), p @ np.abs(v) / p.sum()
+        tol = (f.eps / 2 * np.abs(want) + 2.0 ** -133 / 2 + 2.0 ** -149 +
+               (2.0 ** -20 + 2.0 ** -22 + (2 * L + 4) * 2.0 ** -24) * mass + L * 2.0 ** -39 * np.abs(v).max())
+        assert (np.abs(O[h] - want) <= tol * (1 + f.eps)).all(), h
+        assert abs(lse[h] - np.log(p.sum())) <= 2.0 ** -20 + L * 2.0 ** -24 + 2.0 ** -21 * np.log(L), h
