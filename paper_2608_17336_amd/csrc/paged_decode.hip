@@ -424,7 +424,9 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run& 
 
     // 3. Query rows as the B operand of the score products: lane (head l16, lq) holds the channels that it
     //    reads of a key row.  BF16 queries against 8-bit codes are brought to FP16 by a power of two per
-    //    head, 2^q_exp: the largest to [2^14, 2^15), so that what FP16 cannot hold lies below 2^-39 of it.
+    //    head, 2^q_exp: the largest to [2^14, 2^15), so that what FP16 cannot hold lies below 2^-39 of it.  2^109 is
+    //    enough: it brings BF16's smallest number to FP16's, so that nothing is lost, and what takes it back in
+    //    f_head is then no subnormal number (for scales of 2^-17 and more).
     float f_head = a.scale_log2e;   // score of a product, in log2 units, before the key's scale
     {
       const uint32_t some = l16 < heads ? ~0u : 0u;
@@ -441,7 +443,7 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run& 
             amax = fmaxf(amax, fabsf(x[i][e]));
           }
         }
-        const int q_exp = 15 - __builtin_amdgcn_frexp_expf(quad_rows_max(amax));
+        const int q_exp = min(15 - __builtin_amdgcn_frexp_expf(quad_rows_max(amax)), 109);
         f_head = __builtin_amdgcn_ldexpf(f_head, -q_exp);
   #pragma unroll
         for (int i = 0; i < kQ; ++i) {

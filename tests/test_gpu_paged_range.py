@@ -119,3 +119,30 @@ def test_values_over_all_of_bf16(fmt, L, power):
                (2.0 ** -20 + 2.0 ** -22 + (2 * L + 4) * 2.0 ** -24) * mass + L * 2.0 ** -39 * np.abs(v).max())
         assert (np.abs(O[h] - want) <= tol * (1 + f.eps)).all(), h
         assert abs(lse[h] - np.log(p.sum())) <= 2.0 ** -20 + L * 2.0 ** -24 + 2.0 ** -21 * np.log(L), h
+
+
+# ---------------------------------------------------------------------------------- small queries
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("power", [-128, -122, -112, -100, 100, 120])
+def test_queries_over_all_of_bf16(fmt, power):
+    """BF16 queries around 2^power against keys around 2^-power, so that scores are ordinary ones: off by
+    (d + 8) 2^-24 of sum |q_c k_c|, as for queries near 1."""
+    d, page, L = 64, 16, 90
+    f = torch.finfo(torch.bfloat16)
+    q_gain, k_gain = 2.0 ** power, 2.0 ** min(-power, 124)
+    K = (torch.randn(L, d, generator=_gen(50)).clamp(-3, 3).double() * k_gain).bfloat16()
+    V = torch.randn(L, d, generator=_gen(51)).bfloat16()
+    cache, table, lens, k, v = _cache_of(fmt, K, V, page)
+    Q = (torch.randn(1, 1, 3, d, generator=_gen(52)).double() * q_gain).bfloat16()
+    log(f"queries of 2^{power} {fmt}")
+    O, lse = _decode(cache, table, lens, Q, 0.5)
+    for h in range(3):
+        q = Q[0, 0, h].double().numpy()
+        s = 0.5 * (k @ q)
+        ds = (d + 8) * 2.0 ** -24 * 0.5 * (np.abs(k) @ np.abs(q)).max()
+        p = np.exp(s - s.max())
+        want, mass = p @ v / p.sum(), p @ np.abs(v) / p.sum()
+        tol = f.eps / 2 * np.abs(want) + (2 * ds + 2.0 ** -20 + (2 * L + 4) * 2.0 ** -24) * mass + L * 2.0 ** -39 * np.abs(v).max()
+        assert (np.abs(O[h] - want) <= tol * (1 + f.eps)).all(), h
+        assert abs(lse[h] - (s.max() + np.log(p.sum()))) <= ds + L * 2.0 ** -24 + 2.0 ** -20, h
