@@ -411,7 +411,7 @@ typedef struct tilemix_paged_cache {
  *                cu_seqlens[b] .. cu_seqlens[b + 1] - 1 of the packed K_new, V_new [total, H_k, d];
  *                or NULL: each brings len rows, K_new, V_new [B, len, H_k, d]
  *   len          the most new rows of a sequence, 1 .. 2^28 (1: one decode step); rows past it
- *                are not written
+ *                are not written.  0 is taken with cu_seqlens and total = 0: nothing to do
  *   total        rows of K_new and V_new, 0 .. 2^28, total * H_k * d <= 2^34; B * len without
  *                cu_seqlens
  *   K_new, V_new device, 16-byte aligned, read only; rows of H_k * d elements, k_stride / v_stride

@@ -93,7 +93,8 @@ tilemix_status rows_args(const tilemix_paged_cache* c, int32_t type, const int32
   tilemix_status st = check_shape(c);
   if (st != TILEMIX_OK) return st;
   if ((st = check_type(c, type)) != TILEMIX_OK) return st;
-  if (len < 1 || len > kRowsMax) return fail(TILEMIX_ERR_SHAPE, "len must be 1 .. %d", kRowsMax);
+  const bool none = cu && total == 0;   // no sequence has a row: the longest has 0
+  if (len < (none ? 0 : 1) || len > kRowsMax) return fail(TILEMIX_ERR_SHAPE, "len must be 1 .. %d", kRowsMax);
   if (total < 0 || total > kRowsMax) return fail(TILEMIX_ERR_SHAPE, "total must be 0 .. %d", kRowsMax);
   if ((long long)total * c->heads_kv * c->head_dim > kRowElementsMax)
     return fail(TILEMIX_ERR_SHAPE, "total * heads_kv * head_dim must be <= 2^34");

@@ -161,3 +161,14 @@ def test_decode_of_too_large_batches():
     for kw, heads in ((dict(batch=4), 8), (dict(batch=1, heads_kv=32, stride_k=32 * 64 * 128, stride_v=32 * 64 * 128,
                                                 stride_dk=2048, stride_dv=2048), 32), (dict(batch=1), 8 * 16 * 4)):
         assert _decode(_cache(**big, **kw), heads=heads) == SHAPE, kw
+
+
+def test_packed_rows_of_nothing():
+    """A packed batch in which no sequence has a row, whose longest then has 0; but no rows and a length do not pair
+    otherwise."""
+    for call in (_append, _gather):
+        assert call(_cache(), length=0, total=0, K=None, V=None) == 0
+        assert call(_cache(), length=0, total=0, cu=None) == SHAPE
+        assert call(_cache(), length=0, total=1) == SHAPE
+        assert call(_cache(), length=-1, total=0) == SHAPE
+        assert call(_cache(page_size=8), length=0, total=0) == UNSUPPORTED     # the cache is checked all the same
