@@ -887,10 +887,19 @@ def _paged(cache: PagedCache, page_table, seqlens_k):
                        page_table.data_ptr(), seqlens_k.data_ptr()), fmt, dev, B, Hk, d
 
 
+def _int32(n: int, name: str) -> int:
+    """n, which ctypes would take modulo 2^32."""
+    if -0x80000000 <= n < 0x80000000:
+        return n
+    raise ValueError(f"{name} ({n}) does not fit in 32 bits")
+
+
 def _paged_rows(cu_seqlens, max_len, total, device, B, Hk, d):
     """(cu_seqlens pointer, total, shape of the rows) of an append or gather."""
+    _int32(max_len, "max_len")
     if cu_seqlens is None:
-        return None, B * max_len, (B, max_len, Hk, d)
+        return None, _int32(B * max_len, "B * max_len"), (B, max_len, Hk, d)
+    _int32(total, "total")
     _require_dense(cu_seqlens, _torch().int32, (B + 1,), device, "cu_seqlens")
     return cu_seqlens.data_ptr(), total, (total, Hk, d)
 
@@ -1000,7 +1009,7 @@ def tilemix_paged_gather(cache: PagedCache, page_table, seqlens_k, max_len: int,
 
 def tilemix_paged_decode_workspace_size(cache: PagedCache, page_table, seqlens_k, heads_q: int) -> int:
     n = ctypes.c_size_t(0)
-    _check(load_library().tilemix_paged_decode_workspace_size(_paged(cache, page_table, seqlens_k)[0], heads_q,
+    _check(load_library().tilemix_paged_decode_workspace_size(_paged(cache, page_table, seqlens_k)[0], _int32(heads_q, "heads_q"),
                                                               ctypes.byref(n)))
     return n.value
 
@@ -1024,6 +1033,7 @@ def tilemix_paged_decode(cache: PagedCache, Q, page_table, seqlens_k, scale: flo
     shape = (B, 1, heads, d)
     _require_like(Q, dtype, shape, dev, "Q")
     q_stride = _row_stride(Q, shape, "Q")
+    _int32(window, "window")
     other = _elsewhere(dev)
     if other is not None:
         with other:
