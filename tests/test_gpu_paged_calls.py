@@ -43,3 +43,41 @@ def test_numbers_past_32_bits(beyond):
         with pytest.raises((ValueError, tm.TilemixError)):
             call()
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("fmt", ["fp16", "int8"])
+def test_broken_offsets_touch_no_other_rows(fmt):
+    """cu_seqlens that step back or point outside the rows, every row of another value: append takes the rows that the
+    clamped offsets name and none behind `total` (NaN there), gather writes those and none behind (9 there)."""
+    tm = _tm()
+    Hk, d, page, total, guard = 2, 64, 16, 20, 40
+    cache = tm.PagedCache.empty(8, page, Hk, d, FORMATS[fmt])
+    for t in cache:
+        if t is not None:
+            t.zero_()
+    table = torch.arange(8, dtype=torch.int32).view(4, 2).cuda()
+    lens = torch.tensor([30, 30, 30, 30], dtype=torch.int32).cuda()
+    cu = torch.tensor([-5, 12, 3, 2 ** 31 - 1, -2 ** 31], dtype=torch.int32).cuda()
+    bufs = []
+    for sign in (1.0, -1.0):   # constant rows: any format holds their values to half a step of FP16
+        x = torch.full((total + guard, Hk, d), float("nan"), dtype=torch.float16)
+        x[:total] = sign * torch.arange(1, total + 1).view(-1, 1, 1)
+        bufs.append(x.cuda())
+    tm.tilemix_paged_append(cache, bufs[0][:total], bufs[1][:total], table, lens, cu, 2 ** 20)
+    torch.cuda.synchronize()
+    owned = {0: (0, 12), 1: (12, 0), 2: (3, 17), 3: (20, 0)}         # first row and number of rows, clamped
+    for X, S, buf in ((cache.K, cache.dK, bufs[0]), (cache.V, cache.dV, bufs[1])):
+        held = X.float() if S is None else X.float() * S[..., None]
+        held = held.half().transpose(1, 2).reshape(4, 2 * page, Hk, d).cpu()
+        for b, (first, n) in owned.items():
+            assert torch.equal(held[b, 30 - n:30], buf[first:first + n].cpu())
+            assert not held[b, :30 - n].any() and not held[b, 30:].any()
+    outs = [torch.full((total + guard, Hk, d), 9.0, dtype=torch.float16, device="cuda") for _ in "KV"]
+    tm.tilemix_paged_gather(cache, table, lens, 2 ** 20, cu, K=outs[0][:total], V=outs[1][:total])
+    torch.cuda.synchronize()
+    for out, buf in zip(outs, bufs):
+        out, buf = out.cpu(), buf.cpu()
+        assert (out[total:] == 9.0).all()
+        assert torch.equal(out[:3], buf[:3]) and torch.equal(out[12:total], buf[12:total])
+        for r in range(3, 12):   # of sequence 0 or of sequence 2, where row r is what append read there
+            assert ((out[r] == buf[r]).all(-1)).all()

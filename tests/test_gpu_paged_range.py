@@ -146,3 +146,47 @@ def test_queries_over_all_of_bf16(fmt, power):
         tol = f.eps / 2 * np.abs(want) + (2 * ds + 2.0 ** -20 + (2 * L + 4) * 2.0 ** -24) * mass + L * 2.0 ** -39 * np.abs(v).max()
         assert (np.abs(O[h] - want) <= tol * (1 + f.eps)).all(), h
         assert abs(lse[h] - (s.max() + np.log(p.sum()))) <= ds + L * 2.0 ** -24 + 2.0 ** -20, h
+
+
+# ------------------------------------------------------------------------------ the weights' pieces
+
+@pytest.mark.parametrize("fmt,dtype", PAIRS)
+@pytest.mark.parametrize("d", [64, 128])
+def test_small_sums_of_large_terms(fmt, dtype, d):
+    """The last token's values cancel the sum of the others, as far as its format can: what is left of O is small, and
+    so is its rounding, beside the weights' (2^-22 in two FP16 pieces, 2^-16 in two BF16 ones; one piece would be
+    2^-12 or 2^-9 off).  Keys and queries are small whole numbers and row maxima the formats' tops, so that products are exact
+    and scores are off by their scaling, log2 e and the exponent's argument only: 2^-24 each of |s| <= 8, a weight by twice
+    that and the exponent, 2^-22; sums by n 2^-24."""
+    n, page = 24, 16
+    f = torch.finfo(FORMATS[dtype])
+    top = {"int8": 127.0, "e4m3": 448.0}.get(fmt, 0.0)
+    g = _gen(60)
+    K = torch.randint(-2, 3, (n, d), generator=g).float()
+    Q = torch.randint(-2, 3, (1, 1, 2, d), generator=g).float()
+    if top:
+        K[:, 0], Q[..., 0] = top, 0.0
+    Q[0, 0, 1] = Q[0, 0, 0]
+    q = Q[0, 0, 0]
+    K[-1, 1:] = q[1:]                                                # the heaviest token
+    if not top:
+        K[-1, 0] = q[0]
+    s = (K @ q).double()
+    scale = 2.0 ** -int(np.ceil(np.log2(float(s.abs().max()) / 4.0)))
+    p = torch.exp(scale * s)
+    V = torch.randn(n, d, generator=g)
+    V[-1] = 0
+    V = V.to(FORMATS[dtype])
+    v0 = _cache_of(fmt, K.to(FORMATS[dtype]), V, page)[4]           # as they are held
+    V[-1] = torch.from_numpy(-(p.numpy() @ v0) / float(p[-1])).to(FORMATS[dtype])
+    cache, table, lens, k, v = _cache_of(fmt, K.to(FORMATS[dtype]), V, page)
+    assert np.array_equal(k, K.double().numpy())
+    O, lse = _decode(cache, table, lens, Q.to(FORMATS[dtype]), scale)
+    P = p.numpy() / float(p.sum())
+    want, mass = P @ v, P @ np.abs(v)
+    assert np.median(np.abs(want)) <= 2.0 ** -6 * np.median(mass)
+    rel = 2 * 3 * 8 * 2.0 ** -24 + 2.0 ** -22 + (2.0 ** -16 if fmt == "bf16" else 2.0 ** -22) + (2 * n + 4) * 2.0 ** -24
+    tol = f.eps / 2 * np.abs(want) + rel * mass + n * 2.0 ** -39 * np.abs(v).max()
+    for h in range(2):
+        log(f"small sums {fmt}/{dtype} d {d}: error/tolerance {np.max(np.abs(O[h] - want) / tol):.3f}, left {np.median(np.abs(want) / mass):.2g}")
+        assert (np.abs(O[h] - want) <= tol * (1 + f.eps)).all(), h
