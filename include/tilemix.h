@@ -427,9 +427,9 @@ tilemix_status tilemix_paged_append(const tilemix_paged_cache* cache, int32_t ty
                                     int64_t v_stride, void* stream);
 
 /*
- * tilemix_paged_gather -- the inverse: the last rows of every sequence's cache as dense K and V, the
- * operands of tilemix_prefill_varlen (all of them, n = seqlens_k[b]: a prefill in chunks over a
- * cached prefix).
+ * tilemix_paged_gather -- the inverse: the last rows of every sequence's cache as dense K and V; in
+ * FP16 they are operands of tilemix_prefill_varlen, which takes no BF16 (all of them, n = seqlens_k[b]:
+ * a prefill in chunks over a cached prefix, from an FP16 or an 8-bit pool).
  *   type   of K_out and V_out: TILEMIX_FP16 or TILEMIX_BF16; that of a 16-bit pool
  *   K_out, V_out   device [total, H_k, d] or [B, len, H_k, d], dense, 16-byte aligned, written: a value
  *          is code * scale in FP32, rounded once.  Rows of tokens that the cache does not hold

@@ -972,9 +972,9 @@ def tilemix_paged_gather(cache: PagedCache, page_table, seqlens_k, max_len: int,
     """Read the last rows of every sequence back: with ``cu_seqlens`` (int32 CUDA [B + 1]) sequence b's last
     cu_seqlens[b + 1] - cu_seqlens[b] rows, packed [total, Hk, d], none with more than ``max_len``; else
     its last max_len rows, [B, max_len, Hk, d].  Returns (K, V) in ``dtype`` (that of a 16-bit pool;
-    float16 by default for an 8-bit one), written into ``K`` and ``V`` if given: the K and V of
-    tilemix_prefill_varlen.  Tokens that the cache does not hold are zeros; packed rows that no sequence
-    owns are not written."""
+    float16 by default for an 8-bit one), written into ``K`` and ``V`` if given; float16 ones are the K and V of
+    tilemix_prefill_varlen (which takes no bfloat16).  Tokens that the cache does not hold are zeros; packed rows
+    that no sequence owns are not written."""
     torch = _torch()
     c, pool, dev, B, Hk, d = _paged(cache, page_table, seqlens_k)
     if dtype is None:
