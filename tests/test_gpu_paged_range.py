@@ -121,6 +121,33 @@ def test_values_over_all_of_bf16(fmt, L, power):
         assert abs(lse[h] - np.log(p.sum())) <= 2.0 ** -20 + L * 2.0 ** -24 + 2.0 ** -21 * np.log(L), h
 
 
+@pytest.mark.parametrize("fmt,power", [("fp16", p) for p in (-24, -20, -15, 0, 14)] +
+                         [("bf16", p) for p in (-133, -130, -127, -120, -60, 60, 112)])
+@pytest.mark.parametrize("L", [5, 300, 5000])
+def test_values_over_all_of_16_bits(fmt, L, power):
+    """The same for caches of 16 bits, subnormal values among them; BF16 up to 2^128 / L."""
+    d, page = 128, 32
+    f = torch.finfo(FORMATS[fmt])
+    K = torch.zeros(L, d)
+    K[:, 0] = torch.where(torch.arange(L) % 5 < 2, 1.0, -1.0)
+    V = (torch.randn(L, d, generator=_gen(45)).clamp(-3, 3).double() * 2.0 ** (power - 1)).to(FORMATS[fmt])
+    cache, table, lens, k, v = _cache_of(fmt, K.to(FORMATS[fmt]), V, page)
+    Q = torch.zeros(1, 1, 2, d)
+    Q[:, :, 0, 0], Q[:, :, 1, 0] = 1.0, -1.0
+    log(f"values of 2^{power} {fmt} L {L}")
+    O, lse = _decode(cache, table, lens, Q.to(FORMATS[fmt]), 0.75)
+    v_max = np.abs(v).max() if fmt == "fp16" else 0.0
+    for h, sign in ((0, 1.0), (1, -1.0)):
+        s = 0.75 * sign * k[:, 0]
+        p = np.exp(s)
+        want, mass = p @ v / p.sum(), p @ np.abs(v) / p.sum()
+        piece = 2.0 ** -16 if fmt == "bf16" else 2.0 ** -22
+        tol = (f.eps / 2 * np.abs(want) + f.smallest_normal * f.eps / 2 + 2.0 ** -149 +
+               (2.0 ** -20 + piece + (2 * L + 4) * 2.0 ** -24) * mass + L * 2.0 ** -39 * v_max)
+        assert (np.abs(O[h] - want) <= tol * (1 + f.eps)).all(), h
+        assert abs(lse[h] - np.log(p.sum())) <= 2.0 ** -20 + L * 2.0 ** -24 + 2.0 ** -21 * np.log(L), h
+
+
 # ---------------------------------------------------------------------------------- small queries
 
 @pytest.mark.parametrize("fmt", ["int8", "e4m3"])
