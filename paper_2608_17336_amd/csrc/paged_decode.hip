@@ -106,7 +106,10 @@ struct Run {
     if (mode == kWhole) {
       own = b1 - b0;
       all = B * a.head_blocks;
-      total = all * (a.whole / 2);   // (for want of the lengths: half of the most)
+      // (For want of the lengths: half of the most.  By the first sequence's length, which the workgroup reads next, 64
+      // sequences in page tables of 2048 slots took, INT8, 8 KV heads, d = 128: of 64 tokens 7.9 and 7.9 us, 200 11.1 and 11.4, 500
+      // 16.7 and 16.1, 1000 27.1 and 27.2.)
+      total = all * (a.whole / 2);
       quota = (int)a.div_workgroups.quot(all + W - 1);
     } else {
       int longest = 0;
@@ -201,9 +204,12 @@ struct Part {
   }
 };
 
-// A row's bytes.  `stream`: not kept in the caches, for a batch that the last one (256 MiB) cannot keep for the next
-// call either, let alone between layers: 4 x 65536 keys of 8 INT8 heads (554 MB) 105.1 us, streamed 95.3;
-// 131072 keys of 4 E4M3 heads (138 MB) 37.0 and 36.0; but 111 MB 30.9 and 31.4, 82 MB 21.4 and 22.6.
+// A row's bytes.  `stream`: not kept in the caches, for batches of many bytes: 4 x 65536 keys of 8 INT8 heads (554 MB)
+// 105.1 us, streamed 95.3; 131072 keys of 4 E4M3 heads (138 MB) 37.0 and 36.0; but 111 MB 30.9 and 31.4, 82 MB 21.4 and
+// 22.6.  Not where a KV head has several blocks of query heads, each of which reads its rows: 8 x 32768 keys of
+// one INT8 head, 32 query heads (69 MB) 30.5 us, streamed 35.6; of 64 query heads 28.0 and 31.0 (16384 keys, 35 MB); 16 x 65536
+// keys (277 MB), 32 query heads, 78.3 and 89.5.  (Pages that sequences share count once for each, for want of
+// a cheap way to know: 64 of 2500 to 3100 tokens of which they share 2048 55.6 us, streamed, as it is, 71.7.)
 constexpr long long kStreamBytes = 128 << 20;
 template <bool STREAM, typename V>
 __device__ __forceinline__ V load_row(const char* p) {
@@ -700,7 +706,7 @@ void paged_decode_kernel(PagedDecodeArgs a) {
   const Run run(a, blockIdx.x, threadIdx.x & (kWave - 1));
   // (Two copies of the body: a branch at each request would make the waits count loads that were not issued.)
   const long long bytes = (long long)__builtin_amdgcn_readfirstlane(run.total) * (kTileKeys * 2 * D * kElemBytes<FORMAT>);
-  if (bytes >= kStreamBytes) decode_run<D, TYPE, FORMAT, true>(a, run, shared);
+  if (bytes >= kStreamBytes && a.head_blocks == a.pool.Hk) decode_run<D, TYPE, FORMAT, true>(a, run, shared);
   else decode_run<D, TYPE, FORMAT, false>(a, run, shared);
 }
 
