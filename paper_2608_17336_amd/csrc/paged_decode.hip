@@ -829,10 +829,13 @@ PagedDecodePlan plan_paged_decode(const PagedPool& p, int heads_q, int d, int wi
   const long long resident = kCUs * resident_per_cu(d);
   // Where sequences cannot be long none is split whatever their lengths, and no second launch joins them.  How long,
   // depends on how many workgroups that leaves; us without and with a split, INT8, 8 KV heads, d = 128:
-  //   16 tiles     1 sequence of 250 keys 7.5 and 9.6; 8 of 1000 keys 14.9 and 13.1
-  //   32 from 128  16 of 1000 keys 15.0 and 16.6, 24 15.1 and 19.1; 16 of 1500 keys 19.5 and 18.3
-  //   64 from 192  24 of 2000 keys 25.7 and 27.5, 32 28.4 and 35.9, 64 47.5 and 59.3; 24 of 4000 keys 45.1 and 42.7
-  //   32 where workgroups take several: 128 of 1 to 2000 keys 75.4 and 65.5, of 1 to 1000 41.3 and 41.1
+  //   16 tiles     1 sequence of 250 keys 7.7 and 9.5; 8 of 1000 keys 15.2 and 12.7
+  //   32 from 128  16 of 1000 keys 15.4 and 16.1, 24 15.6 and 17.8; 16 of 1500 keys 19.9 and 17.8
+  //   64 from 192  24 of 2000 keys 25.7 and 25.7, 32 28.3 and 33.3, 64 47.7 and 49.6; 24 of 4000 keys 45.4 and 40.9
+  //   32 where workgroups take several: 128 of 1 to 2000 keys 75.4 and 65.5, of 1 to 1000 41.0 and 40.1
+  // The same limits for the others: FP16 8 of 1000 14.7 and 13.8, 24 of 1000 19.5 and 23.5, 16 of 1500 23.4 and 23.2, 32 of
+  // 2000 42.8 and 47.8, 24 of 4000 69.5 and 66.7 (but 128 of 1 to 1000 68.0 and 58.3); INT8, d = 64 24 of 1000 12.8 and
+  // 13.8, 16 of 1500 16.4 and 14.0, 32 of 2000 20.0 and 20.6, 24 of 4000 35.2 and 27.0.
   const long long limit = segments < kCUs / 2 ? 16 : segments < kCUs * 3 / 4 || segments > resident ? 32 : 64;
   pl.whole = most <= limit ? (int)most : 0;
   pl.workgroups = std::min<long long>(resident,
