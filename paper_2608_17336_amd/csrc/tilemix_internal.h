@@ -205,7 +205,7 @@ struct PagedDecodeArgs {
   int whole;               // 0, or the most tiles that a sequence can have, where workgroups share none
   // Partial results of sequences that several workgroups share, two rows per workgroup (nullptr where none can be):
   int part_heads;          // query heads of a row
-  float* part_mzx;         // [rows, part_heads, 4]: max (log2 units), normalizer, the weights' power of two, 0
+  float* part_mzx;         // [rows, part_heads, 4]: max (log2 units), normalizer, bits of the output's power of two (int), 0
   float* part_o;           // [rows, part_heads, d]: output, unnormalized
   int* segments;           // [B, head_blocks, 2]: first row and number of workgroups
   int group;               // filled in by the launch, as what follows: query heads per KV head
