@@ -363,14 +363,23 @@ tilemix_status tilemix_decode_varlen(const tilemix_params* params, const int32_t
  * common prefix) as long as no call writes the shared slots.
  *   K, V   [P, H_k, page_size, d] in the pool's format, each page dense, pages stride_k /
  *          stride_v elements apart (so K and V may be interleaved in one tensor)
- *   dK, dV FP32 [P, H_k, page_size], INT8 and E4M3 only: one scale per row (a token's d channels
- *          of one head), pages stride_dk / stride_dv elements apart
+ *          MXFP4: bytes [P, H_k, page_size, d / 2] of two codes each, the even channel's in the low
+ *          four bits; strides count bytes
+ *   dK, dV INT8 and E4M3: FP32 [P, H_k, page_size], one scale per row (a token's d channels of one
+ *          head), pages stride_dk / stride_dv elements apart; MXFP4: bytes [P, H_k, page_size, d / 32],
+ *          one exponent for each 32 channels of a row
  * A row x with a = max |x| is held as codes c and the scale a / top, top = 127 (INT8) or 448
  * (E4M3): c = top x / a rounded once, from the exact quotient, half to even, to a whole number
  * or to an E4M3 number; it stands for c * scale.  A row of zeros has codes and scale 0.  A row
  * that holds an infinity or a NaN has codes 0 and scale NaN: all of it reads as NaN.  (The scale
  * of a row never changes, so a cache can be written one token at a time; the blocks of 64 keys of
  * tilemix_quantize_kv would have to be made anew whenever a token raises their maximum.)
+ * MXFP4: a block, 32 channels of a row, is held as E2M1 codes and an exponent byte e + 127: e is the
+ * least integer >= -127 with all magnitudes of the block below 7 * 2^e, a code the E2M1 number (0, 0.5,
+ * 1, 1.5, 2, 3, 4 or 6, with the sign of x) nearest to x * 2^-e, half to even; it stands for
+ * code * 2^e.  A block of zeros has byte 0.  A block that holds an infinity or a NaN has codes 0 and byte
+ * 255, which stands for a NaN: all of it reads as NaN.  (Magnitudes of 3.5 * 2^126 and more, which only BF16
+ * has, read as 2^128: an infinity.)
  * The library reads seqlens_k, page_table and cu_seqlens on the device only.  A page id outside
  * [0, P) names no page: nothing is written there, it reads as zeros, and its keys are not
  * attended to (so the pages that a sliding window has left behind may be given back).
@@ -379,7 +388,8 @@ typedef enum tilemix_format {
   TILEMIX_FP16 = 0,
   TILEMIX_BF16 = 1,
   TILEMIX_INT8 = 2,
-  TILEMIX_E4M3 = 3   /* 1-4-3 bits, largest value 448, no infinities */
+  TILEMIX_E4M3 = 3,  /* 1-4-3 bits, largest value 448, no infinities */
+  TILEMIX_MXFP4 = 5  /* (4 is no format) E2M1 codes, 1-2-1 bits, and a power of two for each 32 channels */
 } tilemix_format;
 
 /* A pool and the sequences of one call. */
@@ -391,19 +401,20 @@ typedef struct tilemix_paged_cache {
   int32_t head_dim;           /* d: 64 or 128 */
   int32_t batch;              /* B: 1 .. 65535 sequences */
   int32_t max_pages;          /* page-table entries per sequence, >= 1; max_pages * page_size <= 2^30 */
-  int64_t stride_k, stride_v; /* elements between pages: >= H_k * page_size * d, multiples of 16 */
-  int64_t stride_dk, stride_dv; /* >= H_k * page_size, multiples of 4; ignored for FP16 and BF16 */
+  int64_t stride_k, stride_v; /* elements (MXFP4: bytes) between pages: >= a page's, multiples of 16 */
+  int64_t stride_dk, stride_dv; /* >= H_k * page_size, multiples of 4 (MXFP4: bytes, multiples of 16);
+                                   ignored for FP16 and BF16 */
   int64_t stride_table;       /* entries between rows of page_table, >= max_pages */
   void* K;                    /* device, 16-byte aligned */
   void* V;
-  float* dK;                  /* device, 16-byte aligned; ignored for FP16 and BF16 */
-  float* dV;
+  void* dK;                   /* device, 16-byte aligned; ignored for FP16 and BF16 */
+  void* dV;
   const int32_t* page_table;  /* device int32 [B, max_pages], 4-byte aligned */
   const int32_t* seqlens_k;   /* device int32 [B], 4-byte aligned: tokens of each sequence */
 } tilemix_paged_cache;
 
 /*
- * tilemix_paged_append -- write new rows into the cache, quantising them for an 8-bit pool.  The
+ * tilemix_paged_append -- write new rows into the cache, quantising them for an 8-bit or 4-bit pool.  The
  * new rows of a sequence are its last ones: seqlens_k counts them already, and row r of n new
  * ones becomes token seqlens_k[b] - n + r (the bottom-right alignment of tilemix_prefill).
  *   type         TILEMIX_FP16 or TILEMIX_BF16: of K_new and V_new; that of a 16-bit pool
@@ -429,7 +440,7 @@ tilemix_status tilemix_paged_append(const tilemix_paged_cache* cache, int32_t ty
 /*
  * tilemix_paged_gather -- the inverse: the last rows of every sequence's cache as dense K and V; in
  * FP16 they are operands of tilemix_prefill_varlen, which takes no BF16 (all of them, n = seqlens_k[b]:
- * a prefill in chunks over a cached prefix, from an FP16 or an 8-bit pool).
+ * a prefill in chunks over a cached prefix, from an FP16, an 8-bit or a 4-bit pool).
  *   type   of K_out and V_out: TILEMIX_FP16 or TILEMIX_BF16; that of a 16-bit pool
  *   K_out, V_out   device [total, H_k, d] or [B, len, H_k, d], dense, 16-byte aligned, written: a value
  *          is code * scale in FP32, rounded once.  Rows of tokens that the cache does not hold
@@ -462,8 +473,8 @@ tilemix_status tilemix_paged_decode_workspace_size(const tilemix_paged_cache* ca
  * to [0, max_pages * page_size]; a sequence without any such token gets O = 0 and lse = -inf.
  * Scores, softmax and sums are FP32; the query is not quantised.  Weights are multiplied as two
  * 16-bit pieces: 22 significant bits down to 2^-40 of the largest possible contribution (a
- * BF16 cache: 16 bits, whatever their size).  An infinity in a value that is attended to makes its
- * channel of O infinite or NaN; so do values of a BF16 cache of 2^128 / n and more, n the tokens
+ * BF16 or MXFP4 cache: 16 bits, whatever their size).  An infinity in a value that is attended to makes its
+ * channel of O infinite or NaN; so do values of a BF16 or MXFP4 cache of 2^128 / n and more, n the tokens
  * attended to, whose FP32 sum has no room.
  * Limit: B * H_k * ceil(G / 16) * (max_pages * page_size / 32 + 6) <= 2^30, G = H_q / H_k.
  */

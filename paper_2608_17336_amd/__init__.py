@@ -778,7 +778,9 @@ def tilemix_decode(Q, K, K8, dK, V8, dV, route_bits, group_size: int, scale: flo
 class PagedCache(NamedTuple):
     """A pool of pages for ``tilemix_paged_append``, ``_gather`` and ``_decode``: K, V [P, Hk, page, d] CUDA
     tensors in float16, bfloat16, int8 or float8_e4m3fn, and for the last two dK, dV float32
-    [P, Hk, page], one scale per row.  Each page is dense; pages may lie further apart (a slice of a
+    [P, Hk, page], one scale per row; or, in 4 bits, K, V float4_e2m1fn_x2 [P, Hk, page, d / 2] (two
+    channels to an element, the even one in the low bits) and dK, dV float8_e8m0fnu [P, Hk, page, d / 32],
+    a power of two for each 32 channels.  Each page is dense; pages may lie further apart (a slice of a
     larger tensor).  A page holds 16, 32, 64, 128 or 256 tokens, d is 64 or 128."""
     K: object
     V: object
@@ -791,6 +793,9 @@ class PagedCache(NamedTuple):
         import torch
         dtype = torch.int8 if dtype is None else dtype
         shape = (pages, heads_kv, page_size, head_dim)
+        if dtype == torch.float4_e2m1fn_x2:
+            return PagedCache(*(torch.empty((*shape[:3], head_dim // n), dtype=t, device=device)
+                                for n, t in ((2, dtype), (2, dtype), (32, torch.float8_e8m0fnu), (32, torch.float8_e8m0fnu))))
         K, V = (torch.empty(shape, dtype=dtype, device=device) for _ in range(2))
         if dtype.itemsize == 2:
             return PagedCache(K, V)
@@ -810,7 +815,7 @@ def _torch():
     global _TORCH
     if _TORCH is None:
         import torch
-        _FORMATS.update({torch.float16: 0, torch.bfloat16: 1, torch.int8: 2, torch.float8_e4m3fn: 3})
+        _FORMATS.update({torch.float16: 0, torch.bfloat16: 1, torch.int8: 2, torch.float8_e4m3fn: 3, torch.float4_e2m1fn_x2: 5})
         _TORCH = torch
     return _TORCH
 
@@ -863,17 +868,24 @@ def _paged(cache: PagedCache, page_table, seqlens_k):
     dtype, shape, dev = K.dtype, K.shape, K.get_device()
     fmt = _format(dtype)
     if fmt < 0:
-        raise TypeError(f"the pool must be float16, bfloat16, int8 or float8_e4m3fn, got {dtype}")
+        raise TypeError(f"the pool must be float16, bfloat16, int8, float8_e4m3fn or float4_e2m1fn_x2, got {dtype}")
     if len(shape) != 4:
         raise ValueError(f"the pool's K must be [pages, Hk, page, d], got {tuple(shape)}")
     _require_like(V, dtype, shape, dev, "the pool's V")
     sk, sv = _outer_stride(shape, K.stride(), 3, "the pool's K"), _outer_stride(shape, V.stride(), 3, "the pool's V")
     sdk = sdv = pdk = pdv = 0
+    P, Hk, page, d = shape
     if fmt >= 2:
-        rows = shape[:3]
-        _require_like(dK, torch.float32, rows, dev, "the pool's dK")
-        _require_like(dV, torch.float32, rows, dev, "the pool's dV")
-        sdk, sdv = _outer_stride(rows, dK.stride(), 2, "the pool's dK"), _outer_stride(rows, dV.stride(), 2, "the pool's dV")
+        if fmt == 5:
+            if d % 16:   # (where this is refused, the message speaks of d)
+                raise ValueError(f"head_dim {2 * d} not supported (64 or 128)")
+            rows, of, inner = (P, Hk, page, d // 16), torch.float8_e8m0fnu, 3
+            d *= 2
+        else:
+            rows, of, inner = shape[:3], torch.float32, 2
+        _require_like(dK, of, rows, dev, "the pool's dK")
+        _require_like(dV, of, rows, dev, "the pool's dV")
+        sdk, sdv = _outer_stride(rows, dK.stride(), inner, "the pool's dK"), _outer_stride(rows, dV.stride(), inner, "the pool's dV")
         pdk, pdv = dK.data_ptr(), dV.data_ptr()
     if getattr(page_table, "ndim", None) != 2:
         raise ValueError("page_table must be a tensor [B, max_pages]")
@@ -881,7 +893,6 @@ def _paged(cache: PagedCache, page_table, seqlens_k):
     _require_like(page_table, torch.int32, t_shape, dev, "page_table")
     B, per = t_shape
     _require_dense(seqlens_k, torch.int32, (B,), dev, "seqlens_k")
-    P, Hk, page, d = shape
     return _PAGED.pack(fmt, P, page, Hk, d, B, per, sk, sv, sdk, sdv,
                        _outer_stride(t_shape, page_table.stride(), 1, "page_table"), K.data_ptr(), V.data_ptr(), pdk, pdv,
                        page_table.data_ptr(), seqlens_k.data_ptr()), fmt, dev, B, Hk, d
@@ -972,7 +983,7 @@ def tilemix_paged_gather(cache: PagedCache, page_table, seqlens_k, max_len: int,
     """Read the last rows of every sequence back: with ``cu_seqlens`` (int32 CUDA [B + 1]) sequence b's last
     cu_seqlens[b + 1] - cu_seqlens[b] rows, packed [total, Hk, d], none with more than ``max_len``; else
     its last max_len rows, [B, max_len, Hk, d].  Returns (K, V) in ``dtype`` (that of a 16-bit pool;
-    float16 by default for an 8-bit one), written into ``K`` and ``V`` if given; float16 ones are the K and V of
+    float16 by default for the others), written into ``K`` and ``V`` if given; float16 ones are the K and V of
     tilemix_prefill_varlen (which takes no bfloat16).  Tokens that the cache does not hold are zeros; packed rows
     that no sequence owns are not written."""
     torch = _torch()

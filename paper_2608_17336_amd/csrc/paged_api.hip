@@ -16,7 +16,7 @@ tilemix_status hip_status(hipError_t e, const char* what) {
   return fail(TILEMIX_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
 
-bool is_8bit(int32_t format) { return format == TILEMIX_INT8 || format == TILEMIX_E4M3; }
+bool is_16bit(int32_t format) { return format == TILEMIX_FP16 || format == TILEMIX_BF16; }
 
 constexpr long long kStrideMax = 1LL << 40;
 // Packed rows, and elements of them: a launch has at most 2^23 workgroups of 256 threads, and one more for each sequence.
@@ -26,7 +26,7 @@ constexpr long long kRowElementsMax = 1LL << 34;
 // Sizes, strides and formats of the pool and its sequences (no pointers).
 tilemix_status check_shape(const tilemix_paged_cache* c) {
   if (!c) return fail(TILEMIX_ERR_NULL, "cache is NULL");
-  if (c->format < TILEMIX_FP16 || c->format > TILEMIX_E4M3)
+  if ((c->format < TILEMIX_FP16 || c->format > TILEMIX_E4M3) && c->format != TILEMIX_MXFP4)
     return fail(TILEMIX_ERR_UNSUPPORTED, "cache format %d not supported", c->format);
   if (c->head_dim != 64 && c->head_dim != 128)
     return fail(TILEMIX_ERR_UNSUPPORTED, "head_dim %d not supported (64 or 128)", c->head_dim);
@@ -40,13 +40,15 @@ tilemix_status check_shape(const tilemix_paged_cache* c) {
   if (c->stride_table < c->max_pages || c->stride_table > kStrideMax)
     return fail(TILEMIX_ERR_SHAPE, "stride_table must be >= max_pages");
   const long long rows = (long long)c->heads_kv * c->page_size;
+  const bool mx = c->format == TILEMIX_MXFP4;
   for (long long s : {(long long)c->stride_k, (long long)c->stride_v})
-    if (s < rows * c->head_dim || s > kStrideMax || s % 16)
-      return fail(TILEMIX_ERR_SHAPE, "page strides must be >= heads_kv * page_size * head_dim and multiples of 16");
-  if (is_8bit(c->format))
+    if (s < rows * c->head_dim / (mx ? 2 : 1) || s > kStrideMax || s % 16)
+      return fail(TILEMIX_ERR_SHAPE, "page strides must be >= heads_kv * page_size * head_dim%s and multiples of 16", mx ? " / 2" : "");
+  if (!is_16bit(c->format))
     for (long long s : {(long long)c->stride_dk, (long long)c->stride_dv})
-      if (s < rows || s > kStrideMax || s % 4)
-        return fail(TILEMIX_ERR_SHAPE, "scale page strides must be >= heads_kv * page_size and multiples of 4");
+      if (s < (mx ? rows * c->head_dim / 32 : rows) || s > kStrideMax || s % (mx ? 16 : 4))
+        return fail(TILEMIX_ERR_SHAPE, mx ? "exponent page strides must be >= heads_kv * page_size * head_dim / 32 and multiples of 16"
+                                          : "scale page strides must be >= heads_kv * page_size and multiples of 4");
   return TILEMIX_OK;
 }
 
@@ -56,8 +58,8 @@ tilemix_status check_pointers(const tilemix_paged_cache* c) {
   if (!aligned(c->K, 16) || !aligned(c->V, 16)) return fail(TILEMIX_ERR_ALIGN, "K and V must be 16-byte aligned");
   if (!aligned(c->page_table, 4) || !aligned(c->seqlens_k, 4))
     return fail(TILEMIX_ERR_ALIGN, "page_table and seqlens_k must be 4-byte aligned");
-  if (is_8bit(c->format)) {
-    if (!c->dK || !c->dV) return fail(TILEMIX_ERR_NULL, "an 8-bit cache needs dK and dV");
+  if (!is_16bit(c->format)) {
+    if (!c->dK || !c->dV) return fail(TILEMIX_ERR_NULL, "an 8-bit or 4-bit cache needs dK and dV");
     if (!aligned(c->dK, 16) || !aligned(c->dV, 16)) return fail(TILEMIX_ERR_ALIGN, "dK and dV must be 16-byte aligned");
   }
   return TILEMIX_OK;
@@ -66,7 +68,7 @@ tilemix_status check_pointers(const tilemix_paged_cache* c) {
 tilemix_status check_type(const tilemix_paged_cache* c, int32_t type) {
   if (type != TILEMIX_FP16 && type != TILEMIX_BF16)
     return fail(TILEMIX_ERR_UNSUPPORTED, "type %d not supported (FP16 or BF16)", type);
-  if (!is_8bit(c->format) && type != c->format)
+  if (is_16bit(c->format) && type != c->format)
     return fail(TILEMIX_ERR_UNSUPPORTED, "a 16-bit cache takes rows of its own type only");
   return TILEMIX_OK;
 }
@@ -74,7 +76,7 @@ tilemix_status check_type(const tilemix_paged_cache* c, int32_t type) {
 tilemix::PagedPool pool_of(const tilemix_paged_cache* c) {
   tilemix::PagedPool p{};
   p.K = c->K; p.V = c->V;
-  if (is_8bit(c->format)) {
+  if (!is_16bit(c->format)) {
     p.dK = c->dK; p.dV = c->dV;
     p.stride_dk = c->stride_dk; p.stride_dv = c->stride_dv;
   }

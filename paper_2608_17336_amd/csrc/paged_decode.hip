@@ -219,11 +219,12 @@ __device__ __forceinline__ V load_row(const char* p) {
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-// Matrix-core products with 16-bit operands as the cache needs them: BF16 for a BF16 cache, else FP16 (8-bit
-// codes are exact in FP16).
+// Matrix-core products with 16-bit operands as the cache needs them: BF16 for a BF16 cache and for MXFP4, whose
+// values are exact in BF16, else FP16 (8-bit codes are exact in FP16).
+constexpr int operand_type(int format) { return format == TILEMIX_BF16 || is_4bit(format) ? TILEMIX_BF16 : TILEMIX_FP16; }
 template <int FORMAT>
 __device__ __forceinline__ f32x4 mfma_16(uint4 x, uint4 y, f32x4 c) {
-  if constexpr (FORMAT == TILEMIX_BF16)
+  if constexpr (operand_type(FORMAT) == TILEMIX_BF16)
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), c, 0, 0, 0);
   else
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(as_half8(x), as_half8(y), c, 0, 0, 0);
@@ -252,7 +253,7 @@ __device__ __forceinline__ float quad_rows_sum(float x) {
 }
 
 // p = 2^(s - m) is taken against the running max m, and so is the normalizer z = sum p.  The weights of the codes
-// are p dV 2^-x (p 2^-x for 16 bits): x = 0 for a BF16 cache, -15 for an FP16 one, and e - 15 for an 8-bit
+// are p dV 2^-x (p 2^-x for 16 and 4 bits): x = 0 for a BF16 cache and MXFP4, -15 for an FP16 one, and e - 15 for an 8-bit
 // one, where 2^e is above every value scale dV so far.  They stay at 2^15 at most, and are handed to the matrix cores as
 // two 16-bit pieces: FP16 pieces hold them to 2^-22 of themselves, and to 2^-40 of the largest possible
 // weight where they are small; BF16 pieces to 2^-16, with FP32's range.  One piece alone (2^-12 or
@@ -262,7 +263,7 @@ __device__ __forceinline__ float quad_rows_sum(float x) {
 // smallest subnormal scale, 2^-149: values near BF16's smallest are weighted like any others.
 constexpr int kExpMin = -148;
 template <int FORMAT>
-constexpr int kHeadroom = FORMAT == TILEMIX_BF16 ? 0 : 15;
+constexpr int kHeadroom = operand_type(FORMAT) == TILEMIX_BF16 ? 0 : 15;
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -270,7 +271,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 // Two 16-bit pieces of two weights.
 template <int FORMAT>
 __device__ __forceinline__ void split2(float w0, float w1, uint32_t& hi, uint32_t& lo) {
-  using V = std::conditional_t<FORMAT == TILEMIX_BF16, bf16x2, half2v>;
+  using V = std::conditional_t<operand_type(FORMAT) == TILEMIX_BF16, bf16x2, half2v>;
   const V h = __builtin_convertvector((f32x2{w0, w1}), V);
   const V l = __builtin_convertvector((f32x2{w0 - (float)h[0], w1 - (float)h[1]}), V);
   hi = __builtin_bit_cast(uint32_t, h);
@@ -295,11 +296,13 @@ template <int D, int TYPE, int FORMAT, bool STREAM>
 __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run& run, DecodeShared<D>& shared) {
   constexpr int kS = kSlabs, kKeys = kTileKeys;
   constexpr int kBytes = kElemBytes<FORMAT>;
-  constexpr bool k8 = is_8bit(FORMAT);
-  constexpr int kKL = D * kBytes / 64;             // 16-byte loads of a key row per lane
+  constexpr bool k8 = is_8bit(FORMAT), k4 = is_4bit(FORMAT);
+  constexpr int kRow = kRowBytes<D, FORMAT>, kScaleRow = kScaleBytes<D, FORMAT>;
+  constexpr int kKL = k4 ? 1 : kRow / 64;          // loads of a key row per lane, 16 bytes each (MXFP4, d = 64: 8)
   constexpr int kC = D / 16;                       // channels of a lane's value row: output products
-  constexpr int kVW = kC * kBytes / 4;             // dwords of them
+  constexpr int kVW = k4 ? 1 : kC * kBytes / 4;    // dwords of them
   constexpr int kQ = D / 32;                       // score products per slab
+  constexpr int kQueryPieces = k4 && TYPE == TILEMIX_FP16 ? 2 : 1;   // BF16 pieces of the query
   const PagedPool& p = a.pool;
   const int tid = threadIdx.x, lane = tid & (kWave - 1);
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
@@ -341,10 +344,11 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run& 
   uint4 kr[kS][kKL];
   uint32_t vr[kS][4][kVW];
   f32x4 dk[kS], dv[kS];
+  uint32_t ek[kS], ev[kS][kScaleRow ? kScaleRow : 1];              // MXFP4: exponent of the lane's channels of key l16; of all blocks of keys 4 lq ..
   int page[kS];                                    // per slab, of the tile that was requested last
   const char* poolK = static_cast<const char*>(p.K);
   const char* poolV = static_cast<const char*>(p.V);
-  const uint32_t k_lane = l16 * D * kBytes + 16 * lq, v_lane = 4 * lq * D * kBytes + l16 * kC * kBytes;
+  const uint32_t k_lane = l16 * kRow + (k4 ? kRow / 4 : 16) * lq, v_lane = 4 * lq * kRow + l16 * (kRow / 16);
   auto find_pages = [&](int ids, int i) {
     const int at = (i & (id_tiles - 1)) << per_shift;
 #pragma unroll
@@ -359,14 +363,25 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run& 
     const uint32_t k_off = some ? k_lane : 0u, s_off = some ? 16u * lq : 0u;
 #pragma unroll
     for (int s = 0; s < kS; ++s) {
-      const char* base = poolK + kBytes * (max(page[s], 0) * p.stride_k + (long long)slab_row(hk, n, s) * D);
+      const char* base = poolK + kBytes * (max(page[s], 0) * p.stride_k + (long long)slab_row(hk, n, s) * (kRow / kBytes));
+      if constexpr (k4 && D == 64) {
+        const u32x2 x = load_row<STREAM, u32x2>(base + k_off);
+        kr[s][0] = make_uint4(x[0], x[1], 0, 0);
+      } else {
 #pragma unroll
-      for (int i = 0; i < kKL; ++i) kr[s][i] = __builtin_bit_cast(uint4, load_row<STREAM, u32x4>(base + 64 * i + k_off));
+        for (int i = 0; i < kKL; ++i) kr[s][i] = __builtin_bit_cast(uint4, load_row<STREAM, u32x4>(base + 64 * i + k_off));
+      }
     }
     if constexpr (k8) {
 #pragma unroll
       for (int s = 0; s < kS; ++s)
-        dk[s] = *reinterpret_cast<const f32x4*>(reinterpret_cast<const char*>(p.dK + max(page[s], 0) * p.stride_dk + slab_row(hk, n, s)) + s_off);
+        dk[s] = *reinterpret_cast<const f32x4*>(static_cast<const char*>(p.dK) + 4 * (max(page[s], 0) * p.stride_dk + slab_row(hk, n, s)) + s_off);
+    }
+    if constexpr (k4) {
+#pragma unroll
+      for (int s = 0; s < kS; ++s)
+        ek[s] = *reinterpret_cast<const uint8_t*>(static_cast<const char*>(p.dK) + max(page[s], 0) * p.stride_dk +
+                                                  (long long)slab_row(hk, n, s) * kScaleRow + (some ? l16 * kScaleRow + lq * kScaleRow / 4 : 0));
     }
   };
   auto load_values = [&](int hk, int n, bool some) {
@@ -374,15 +389,31 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run& 
     if constexpr (k8) {
 #pragma unroll
       for (int s = 0; s < kS; ++s)
-        dv[s] = *reinterpret_cast<const f32x4*>(reinterpret_cast<const char*>(p.dV + max(page[s], 0) * p.stride_dv + slab_row(hk, n, s)) + s_off);
+        dv[s] = *reinterpret_cast<const f32x4*>(static_cast<const char*>(p.dV) + 4 * (max(page[s], 0) * p.stride_dv + slab_row(hk, n, s)) + s_off);
+    }
+    if constexpr (k4) {
+#pragma unroll
+      for (int s = 0; s < kS; ++s) {
+        const char* at = static_cast<const char*>(p.dV) + max(page[s], 0) * p.stride_dv + (long long)slab_row(hk, n, s) * kScaleRow +
+                         (some ? 4 * kScaleRow * lq : 0);
+        if constexpr (kScaleRow == 4) {
+          const u32x4 x = *reinterpret_cast<const u32x4*>(at);
+          ev[s][0] = x[0]; ev[s][1] = x[1]; ev[s][2] = x[2]; ev[s][3] = x[3];
+        } else {
+          const u32x2 x = *reinterpret_cast<const u32x2*>(at);
+          ev[s][0] = x[0]; ev[s][1] = x[1];
+        }
+      }
     }
 #pragma unroll
     for (int s = 0; s < kS; ++s) {
-      const char* base = poolV + kBytes * (max(page[s], 0) * p.stride_v + (long long)slab_row(hk, n, s) * D);
+      const char* base = poolV + kBytes * (max(page[s], 0) * p.stride_v + (long long)slab_row(hk, n, s) * (kRow / kBytes));
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const char* at = base + r * D * kBytes + v_off;
-        if constexpr (kVW == 4) {
+        const char* at = base + r * kRow + v_off;
+        if constexpr (k4 && D == 64) {
+          vr[s][r][0] = load_row<STREAM, uint16_t>(at);
+        } else if constexpr (kVW == 4) {
           const u32x4 x = load_row<STREAM, u32x4>(at);
           vr[s][r][0] = x[0]; vr[s][r][1] = x[1]; vr[s][r][2] = x[2]; vr[s][r][3] = x[3];
         } else if constexpr (kVW == 2) {
@@ -394,12 +425,12 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run& 
       }
     }
   };
-  uint4 qf[kQ];
+  uint4 qf[kQ], ql[kQ];                            // ql: the second pieces
   auto load_query = [&](const Part& q) {
     const int G = a.group, heads = min(kPagedHeads, G - q.g0);
     const char* row = static_cast<const char*>(a.Q) + 2 * (q.b * a.q_stride + (long long)(q.hk * G + q.g0 + min(l16, heads - 1)) * D);
 #pragma unroll
-    for (int i = 0; i < kQ; ++i) qf[i] = ld_global_16(row + 2 * (k8 ? 64 * (i / 2) + 16 * lq + 8 * (i % 2) : 32 * i + 8 * lq));
+    for (int i = 0; i < kQ; ++i) qf[i] = ld_global_16(row + 2 * (k4 ? D / 4 * lq + 8 * i : k8 ? 64 * (i / 2) + 16 * lq + 8 * (i % 2) : 32 * i + 8 * lq));
   };
 
   int f = 0, i = 0, n = first_tile(cur, 0);
@@ -459,6 +490,18 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run& 
           qf[i] = make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
         }
       }
+      if constexpr (kQueryPieces == 2) {   // FP16's 11 bits are two BF16 numbers of 8 and 3
+  #pragma unroll
+        for (int i = 0; i < kQ; ++i) {
+          const uint32_t w[4] = {qf[i].x, qf[i].y, qf[i].z, qf[i].w};
+          uint32_t h[4], l[4];
+  #pragma unroll
+          for (int e = 0; e < 4; ++e)
+            split2<FORMAT>(bits_to_float<TILEMIX_FP16>(w[e] & 0xffffu), bits_to_float<TILEMIX_FP16>(w[e] >> 16), h[e], l[e]);
+          qf[i] = make_uint4(h[0], h[1], h[2], h[3]);
+          ql[i] = make_uint4(l[0], l[1], l[2], l[3]);
+        }
+      }
     }
 
     // 4. The wave's tiles.  m: running max (log2 units); x: the weights' power of two; z: this lane's share of the
@@ -479,12 +522,22 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run& 
   #pragma unroll
       for (int s = 0; s < kS; ++s) has |= page[s] >= 0 ? 1u << s : 0u;
       all = all && has == (1u << kS) - 1;
-      float sc[kS][4];
+      float sc[kS][4], ve[kS][4];   // ve: MXFP4, scale of the lane's channels of key 4 lq + r
   #pragma unroll
       for (int s = 0; s < kS; ++s) {
         f32x4 c = {0.0f, 0.0f, 0.0f, 0.0f};
+        if constexpr (k4) {
+          const float scale = block_scale(ek[s]);
+          const uint32_t w[4] = {kr[s][0].x, kr[s][0].y, kr[s][0].z, kr[s][0].w};
   #pragma unroll
-        for (int k = 0; k < kKL; ++k) {
+          for (int k = 0; k < kQ; ++k) {
+            const uint4 x = mx_values8<TILEMIX_BF16>(w[k], scale);
+            c = mfma_16<FORMAT>(x, qf[k], c);
+            if constexpr (kQueryPieces == 2) c = mfma_16<FORMAT>(x, ql[k], c);
+          }
+        }
+  #pragma unroll
+        for (int k = 0; k < (k4 ? 0 : kKL); ++k) {
           if constexpr (k8) {
             c = mfma_16<FORMAT>(widen8<FORMAT>(kr[s][k].x, kr[s][k].y), qf[2 * k], c);
             c = mfma_16<FORMAT>(widen8<FORMAT>(kr[s][k].z, kr[s][k].w), qf[2 * k + 1], c);
@@ -513,6 +566,15 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run& 
       }
       find_pages(ids, i);
       load_keys(hk, to, some);
+      if constexpr (k4) {
+  #pragma unroll
+        for (int s = 0; s < kS; ++s)
+  #pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const uint32_t w = ev[s][r * kScaleRow / 4] >> 16 * (r * kScaleRow / 2 % 2);
+            ve[s][r] = block_scale(w >> 8 * (l16 * kC / 32) & 0xffu);
+          }
+      }
       if (!all) {
   #pragma unroll
         for (int s = 0; s < kS; ++s)
@@ -523,7 +585,9 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run& 
             sc[s][r] = ok ? sc[s][r] : ninf;
             if constexpr (k8) dv[s][r] = ok ? dv[s][r] : 0.0f;
             // What a slot behind the sequence holds may be a NaN, which a weight of 0 does not cancel.
-            if constexpr (FORMAT != TILEMIX_INT8) {
+            if constexpr (k4) {
+              ve[s][r] = ok ? ve[s][r] : 0.0f;
+            } else if constexpr (FORMAT != TILEMIX_INT8) {
   #pragma unroll
               for (int w = 0; w < kVW; ++w) vr[s][r][w] = ok ? vr[s][r][w] : 0u;
             }
@@ -579,7 +643,28 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run& 
         acc[c] = mfma_16<FORMAT>(va, ph, acc[c]);
         acc[c] = mfma_16<FORMAT>(va, pl, acc[c]);
       };
-      if constexpr (FORMAT == TILEMIX_E4M3) {
+      if constexpr (k4) {
+        // Two channels of a key in a byte: widened, with the key's scale, then paired.
+  #pragma unroll
+        for (int c = 0; c < kC; c += 2) {
+          uint32_t v[2][4];
+  #pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            uint32_t x[2];
+  #pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              const uint32_t w = row(2 * j + u)[0];
+              const float scale = ve[(2 * j + u) / 4][(2 * j + u) % 4];
+              x[u] = c == 0 ? mx_values<TILEMIX_BF16, 0>(w, scale) : c == 2 ? mx_values<TILEMIX_BF16, 1>(w, scale)
+                   : c == 4 ? mx_values<TILEMIX_BF16, 2>(w, scale) : mx_values<TILEMIX_BF16, 3>(w, scale);
+            }
+            v[0][j] = __builtin_amdgcn_perm(x[1], x[0], 0x05040100u);
+            v[1][j] = __builtin_amdgcn_perm(x[1], x[0], 0x07060302u);
+          }
+          add(c, v[0]);
+          add(c + 1, v[1]);
+        }
+      } else if constexpr (FORMAT == TILEMIX_E4M3) {
         // Channels c and c + 1 of two keys in one word, then two conversions.
   #pragma unroll
         for (int c = 0; c < kC; c += 2) {
@@ -705,7 +790,7 @@ void paged_decode_kernel(PagedDecodeArgs a) {
   __shared__ DecodeShared<D> shared;
   const Run run(a, blockIdx.x, threadIdx.x & (kWave - 1));
   // (Two copies of the body: a branch at each request would make the waits count loads that were not issued.)
-  const long long bytes = (long long)__builtin_amdgcn_readfirstlane(run.total) * (kTileKeys * 2 * D * kElemBytes<FORMAT>);
+  const long long bytes = (long long)__builtin_amdgcn_readfirstlane(run.total) * (kTileKeys * 2 * kRowBytes<D, FORMAT>);
   if (bytes >= kStreamBytes && a.head_blocks == a.pool.Hk) decode_run<D, TYPE, FORMAT, true>(a, run, shared);
   else decode_run<D, TYPE, FORMAT, false>(a, run, shared);
 }

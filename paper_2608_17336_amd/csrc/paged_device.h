@@ -38,8 +38,14 @@ __device__ __forceinline__ uint32_t float_to_bits(float x) {   // round to neare
 }
 
 constexpr bool is_8bit(int format) { return format == TILEMIX_INT8 || format == TILEMIX_E4M3; }
+constexpr bool is_4bit(int format) { return format == TILEMIX_MXFP4; }
+// Bytes of a row's channels and of its scale or exponents, and of a pool's elements (a byte holds two 4-bit codes).
+template <int D, int FORMAT>
+constexpr int kRowBytes = is_4bit(FORMAT) ? D / 2 : is_8bit(FORMAT) ? D : 2 * D;
+template <int D, int FORMAT>
+constexpr int kScaleBytes = is_4bit(FORMAT) ? D / 32 : is_8bit(FORMAT) ? 4 : 0;
 template <int FORMAT>
-constexpr int kElemBytes = is_8bit(FORMAT) ? 1 : 2;
+constexpr int kElemBytes = is_8bit(FORMAT) || is_4bit(FORMAT) ? 1 : 2;
 template <int FORMAT>
 constexpr float kTop = FORMAT == TILEMIX_INT8 ? 127.0f : 448.0f;
 
@@ -130,6 +136,53 @@ __device__ __forceinline__ void widen4(uint32_t w, float scale, float (&x)[4]) {
   for (int i = 0; i < 4; ++i) asm("" : "+v"(x[i]));
 }
 
+// The rule of MXFP4: 32 channels share 2^e, e the least integer >= -127 with all magnitudes below 7 2^e (6 is the
+// nearest code up to there), and a code is the E2M1 number nearest to x 2^-e, half to even.  The hardware's
+// conversions take the scale as the exponent field of an FP32 number, a field of 0 as 2^-127, and round once,
+// subnormal numbers on either side included.
+constexpr uint32_t kBlockNaN = 255;   // exponent byte of a block that holds an infinity or a NaN
+// Exponent byte, from the bits of max |x| of a block of TYPE.
+template <int TYPE>
+__device__ __forceinline__ uint32_t block_exponent(uint32_t amax) {
+  const float x = bits_to_float<TYPE>(amax);
+  const int e = __builtin_amdgcn_frexp_expf(x) - 3 + (__builtin_amdgcn_frexp_mantf(x) >= 0.875f ? 1 : 0);
+  return amax >= Elem<TYPE>::kInf ? kBlockNaN : amax == 0 ? 0u : (uint32_t)(max(e, -127) + 127);
+}
+// Scale operand of the conversions of an exponent byte.
+__device__ __forceinline__ float block_scale(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
+
+// Codes of eight channels of TYPE, two to a word of w, the first in the lowest bits.
+template <int TYPE>
+__device__ __forceinline__ uint32_t codes8(const uint32_t (&w)[4], uint32_t byte) {
+  const float s = block_scale(byte);
+  uint32_t c = 0;
+  if constexpr (TYPE == TILEMIX_BF16) {
+    typedef __bf16 V __attribute__((ext_vector_type(2)));
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(V, w[0]), s, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(V, w[1]), s, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(V, w[2]), s, 2);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(V, w[3]), s, 3);
+  } else {
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, __builtin_bit_cast(half2v, w[0]), s, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, __builtin_bit_cast(half2v, w[1]), s, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, __builtin_bit_cast(half2v, w[2]), s, 2);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, __builtin_bit_cast(half2v, w[3]), s, 3);
+  }
+  return byte == kBlockNaN ? 0u : c;
+}
+
+// Values of the codes in byte I of w, rounded to TYPE: the lower code's in the low half.
+template <int TYPE, int I>
+__device__ __forceinline__ uint32_t mx_values(uint32_t w, float scale) {
+  if constexpr (TYPE == TILEMIX_BF16) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, I));
+  else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, I));
+}
+template <int TYPE>
+__device__ __forceinline__ uint4 mx_values8(uint32_t w, float scale) {
+  return make_uint4(mx_values<TYPE, 0>(w, scale), mx_values<TYPE, 1>(w, scale), mx_values<TYPE, 2>(w, scale),
+                    mx_values<TYPE, 3>(w, scale));
+}
+
 // f(D, TYPE, FORMAT) as integral constants.
 template <typename F>
 inline hipError_t for_paged_types(int d, int type, int format, F&& f) {
@@ -139,14 +192,17 @@ inline hipError_t for_paged_types(int d, int type, int format, F&& f) {
     using B = integral_constant<int, TILEMIX_BF16>;
     using I = integral_constant<int, TILEMIX_INT8>;
     using E = integral_constant<int, TILEMIX_E4M3>;
+    using M = integral_constant<int, TILEMIX_MXFP4>;
     if (type == TILEMIX_FP16) {
       if (format == TILEMIX_FP16) return f(D, H{}, H{});
       if (format == TILEMIX_INT8) return f(D, H{}, I{});
       if (format == TILEMIX_E4M3) return f(D, H{}, E{});
+      if (format == TILEMIX_MXFP4) return f(D, H{}, M{});
     } else if (type == TILEMIX_BF16) {
       if (format == TILEMIX_BF16) return f(D, B{}, B{});
       if (format == TILEMIX_INT8) return f(D, B{}, I{});
       if (format == TILEMIX_E4M3) return f(D, B{}, E{});
+      if (format == TILEMIX_MXFP4) return f(D, B{}, M{});
     }
     return hipErrorInvalidValue;
   };

@@ -2,7 +2,7 @@
 //
 // paged_append_kernel: row r of the n_b new ones of sequence b becomes token L_b - n_b + r, in slot
 //   token % page of page table[b][token / page].  8-bit formats: codes and scale of the row by
-//   RowScale.
+//   RowScale; MXFP4: codes and exponents of its blocks by block_exponent and codes8.
 // paged_gather_kernel: the same rows the other way, value = code * scale.
 //
 // A row (one token, one head) is D channels: D / 8 lanes take 8 each, 16 bytes on the 16-bit side.  A
@@ -105,23 +105,28 @@ __device__ __forceinline__ RowPointers packed_rows(const PagedRowsArgs& a, long 
 
 template <int D, int FORMAT>
 __device__ __forceinline__ RowPointers cached_rows(const PagedPool& p, const Slot& s, int c) {
-  const long long in = (long long)s.slot * D + c;
-  return {static_cast<char*>(p.K) + kElemBytes<FORMAT> * (s.page * p.stride_k + in),
-          static_cast<char*>(p.V) + kElemBytes<FORMAT> * (s.page * p.stride_v + in), (long long)(kElemBytes<FORMAT> * D) << p.page_shift};
+  constexpr int kRow = kRowBytes<D, FORMAT>;
+  const long long in = (long long)s.slot * kRow + c * kRow / D;
+  return {static_cast<char*>(p.K) + s.page * p.stride_k * kElemBytes<FORMAT> + in,
+          static_cast<char*>(p.V) + s.page * p.stride_v * kElemBytes<FORMAT> + in, (long long)kRow << p.page_shift};
 }
 
-__device__ __forceinline__ RowPointers cached_scales(const PagedPool& p, const Slot& s) {
-  return {reinterpret_cast<char*>(p.dK + s.page * p.stride_dk + s.slot),
-          reinterpret_cast<char*>(p.dV + s.page * p.stride_dv + s.slot), 4ll << p.page_shift};
+// The row's scale, or the exponent of the channel's block.
+template <int D, int FORMAT>
+__device__ __forceinline__ RowPointers cached_scales(const PagedPool& p, const Slot& s, int c) {
+  constexpr int kRow = kScaleBytes<D, FORMAT>, kElem = is_4bit(FORMAT) ? 1 : 4;
+  const long long in = (long long)s.slot * kRow + (is_4bit(FORMAT) ? c / 32 : 0);
+  return {static_cast<char*>(p.dK) + s.page * p.stride_dk * kElem + in,
+          static_cast<char*>(p.dV) + s.page * p.stride_dv * kElem + in, (long long)kRow << p.page_shift};
 }
 
-// Maximum over the D / 8 lanes of a row.
-template <int D>
-__device__ __forceinline__ uint32_t row_max(uint32_t x) {
+// Maximum over the LANES lanes of a row or block.
+template <int LANES>
+__device__ __forceinline__ uint32_t lanes_max(uint32_t x) {
   x = max(x, (uint32_t)dpp<0xB1>((int)x, (int)x));
   x = max(x, (uint32_t)dpp<0x4E>((int)x, (int)x));
-  x = max(x, (uint32_t)dpp<0x141>((int)x, (int)x));
-  if constexpr (D == 128) x = max(x, (uint32_t)dpp<0x140>((int)x, (int)x));
+  if constexpr (LANES >= 8) x = max(x, (uint32_t)dpp<0x141>((int)x, (int)x));
+  if constexpr (LANES >= 16) x = max(x, (uint32_t)dpp<0x140>((int)x, (int)x));
   return x;
 }
 
@@ -142,14 +147,14 @@ __global__ __launch_bounds__(kRowsThreads) void paged_append_kernel(PagedRowsArg
   load(g.r0);   // before the slot is looked up
   const Slot s = find_slot(a.pool, tile.b, tile.token + g.tok);
   if (s.page < 0) return;
-  const RowPointers dst = cached_rows<D, FORMAT>(a.pool, s, c), scales = cached_scales(a.pool, s);
+  const RowPointers dst = cached_rows<D, FORMAT>(a.pool, s, c), scales = cached_scales<D, FORMAT>(a.pool, s, c);
   for (int r0 = g.r0; r0 < rows; r0 += g.step * kRowsAhead) {
     if (r0 != g.r0) load(r0);
 #pragma unroll
     for (int u = 0; u < kRowsAhead; ++u) {
       const int r = r0 + u * g.step;
       if (r >= rows) break;
-      if constexpr (!is_8bit(FORMAT)) {
+      if constexpr (!is_8bit(FORMAT) && !is_4bit(FORMAT)) {
         *reinterpret_cast<uint4*>(dst.row(r, Hk)) = v[u];
       } else {
         const uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
@@ -157,13 +162,20 @@ __global__ __launch_bounds__(kRowsThreads) void paged_append_kernel(PagedRowsArg
         u16x2 m = {0, 0};
 #pragma unroll
         for (int k = 0; k < 4; ++k) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, w[k] & 0x7fff7fffu));
-        const auto s8 = RowScale<FORMAT>::template of<TYPE>(row_max<D>(max((uint32_t)m[0], (uint32_t)m[1])));
-        float x[8];
+        const uint32_t own = max((uint32_t)m[0], (uint32_t)m[1]);
+        if constexpr (is_4bit(FORMAT)) {
+          const uint32_t e = block_exponent<TYPE>(lanes_max<4>(own));
+          *reinterpret_cast<uint32_t*>(dst.row(r, Hk)) = codes8<TYPE>(w, e);
+          if (c % 32 == 0) *reinterpret_cast<uint8_t*>(scales.row(r, Hk)) = (uint8_t)e;
+        } else {
+          const auto s8 = RowScale<FORMAT>::template of<TYPE>(lanes_max<kLanes>(own));
+          float x[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] = bits_to_float<TYPE>(k & 1 ? w[k >> 1] >> 16 : w[k >> 1] & 0xffffu);
-        *reinterpret_cast<uint2*>(dst.row(r, Hk)) =
-            make_uint2(s8.codes(x[0], x[1], x[2], x[3]), s8.codes(x[4], x[5], x[6], x[7]));
-        if (c == 0) *reinterpret_cast<float*>(scales.row(r, Hk)) = s8.scale;
+          for (int k = 0; k < 8; ++k) x[k] = bits_to_float<TYPE>(k & 1 ? w[k >> 1] >> 16 : w[k >> 1] & 0xffffu);
+          *reinterpret_cast<uint2*>(dst.row(r, Hk)) =
+              make_uint2(s8.codes(x[0], x[1], x[2], x[3]), s8.codes(x[4], x[5], x[6], x[7]));
+          if (c == 0) *reinterpret_cast<float*>(scales.row(r, Hk)) = s8.scale;
+        }
       }
     }
   }
@@ -180,7 +192,7 @@ __global__ __launch_bounds__(kRowsThreads) void paged_gather_kernel(PagedRowsArg
   Slot s = find_slot(a.pool, tile.b, tile.token + g.tok);
   const bool some = s.page >= 0;
   s.page = max(s.page, 0);   // nothing is read where there is no page
-  const RowPointers src = cached_rows<D, FORMAT>(a.pool, s, c), scales = cached_scales(a.pool, s);
+  const RowPointers src = cached_rows<D, FORMAT>(a.pool, s, c), scales = cached_scales<D, FORMAT>(a.pool, s, c);
   for (int r0 = g.r0; r0 < rows; r0 += g.step * kRowsAhead) {
     uint4 v[kRowsAhead];
     float scale[kRowsAhead];
@@ -190,7 +202,10 @@ __global__ __launch_bounds__(kRowsThreads) void paged_gather_kernel(PagedRowsArg
       v[u] = make_uint4(0, 0, 0, 0);
       scale[u] = 0.0f;
       if (r >= rows || !some) continue;
-      if constexpr (!is_8bit(FORMAT)) {
+      if constexpr (is_4bit(FORMAT)) {
+        v[u].x = *reinterpret_cast<const uint32_t*>(src.row(r, Hk));
+        scale[u] = block_scale(*reinterpret_cast<const uint8_t*>(scales.row(r, Hk)));
+      } else if constexpr (!is_8bit(FORMAT)) {
         v[u] = ld_global_16(src.row(r, Hk));
       } else {
         const uint2 w = *reinterpret_cast<const uint2*>(src.row(r, Hk));
@@ -203,7 +218,9 @@ __global__ __launch_bounds__(kRowsThreads) void paged_gather_kernel(PagedRowsArg
     for (int u = 0; u < kRowsAhead; ++u) {
       const int r = r0 + u * g.step;
       if (r >= rows) break;
-      if constexpr (is_8bit(FORMAT)) {
+      if constexpr (is_4bit(FORMAT)) {
+        v[u] = mx_values8<TYPE>(v[u].x, scale[u]);
+      } else if constexpr (is_8bit(FORMAT)) {
         float x[8];
         widen4<FORMAT>(v[u].x, scale[u], *reinterpret_cast<float(*)[4]>(x));
         widen4<FORMAT>(v[u].y, scale[u], *reinterpret_cast<float(*)[4]>(x + 4));

@@ -167,10 +167,10 @@ hipError_t launch_debug_tiles(const DebugTileArgs& args, int d, int block_m, hip
 
 // A paged cache as the kernels see it.
 struct PagedPool {
-  void* K;                 // [P, Hk, page, d], pages stride_k elements apart
+  void* K;                 // [P, Hk, page, d], pages stride_k elements apart (bytes of an MXFP4 pool, two channels each)
   void* V;
-  float* dK;               // [P, Hk, page], 8-bit formats
-  float* dV;
+  void* dK;                // FP32 [P, Hk, page], 8-bit formats; bytes [P, Hk, page, d / 32], MXFP4
+  void* dV;
   const int* table;        // [B, max_pages], rows stride_table entries apart
   const int* seqlens;      // [B]
   long long stride_k, stride_v, stride_dk, stride_dv, stride_table;
