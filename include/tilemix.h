@@ -483,6 +483,117 @@ tilemix_status tilemix_paged_decode(const tilemix_paged_cache* cache, int32_t ty
                                     void* O, float* lse, void* workspace, size_t workspace_bytes,
                                     void* stream);
 
+/*
+ * tilemix_paged_reserve -- pages for new tokens, on the device: from the lengths that the sequences
+ * have and those that they are to have, pages move between their page tables and a list of free
+ * ones.  With p = page_size a sequence of L tokens holds the entries first .. ceil(L / p) - 1 of its
+ * page table; first is 0, or with a window w what the calls before left it at (see first_held).
+ *   L_new > L: takes pages for the entries of L_new behind those of L.  With a window the entries in front of
+ *              floor(max(L_new - w, 0) / p) are left: pages held there are given back, none are taken (-1), and
+ *              first moves there
+ *   L_new <= L: gives back the entries that L_new does not reach (0: the sequence is done, and first is 0
+ *              again); it takes none, so a shorter sequence misses what the window has left
+ * Entries given back become -1; others stay as they are.  A sequence whose length is refused stays as
+ * it was: where L_new > max_pages * p, or where it needs pages and those that it and all sequences before
+ * it need (refused for the want of pages or not) are more than were free when the call began (what the
+ * call gives back is free from the next call on).  Sequences that need no page are never refused for the
+ * want of any.
+ *   page_table   device int32 [batch, max_pages], rows stride_table entries apart, read and written
+ *   seqlens      device int32 [batch]: lengths now; clamped to [0, max_pages * p]
+ *   wanted       device int32 [batch]: lengths to be; negative ones count as 0
+ *   window       0: none; w >= 1: only the last w tokens will be attended to (take as many more as tokens may be taken
+ *                back again)
+ *   first_held   device int32 [batch], with a window: the first entry that each sequence holds, read and
+ *                written; 0 for a sequence without tokens.  NULL without a window
+ *   free_ids     device int32 [capacity], a ring: the i-th free page is free_ids[(head + i) % capacity]; pages are
+ *                taken from its head, by sequence and entry, and given back at its end in that order.
+ *                capacity 1 .. 2^30 - 2; room for every page of the pool, or pages that find no room are lost
+ *   free_state   device int32 [4]: head, count, the sequences refused by the last call (written), and
+ *                a number that is 0 between calls
+ *   free_state_out  device int32 [4], the new state, written; may be free_state
+ *   seqlens_out  device int32 [batch], the new lengths (refused: the old), written; may be seqlens
+ *   cu_seqlens   device int32 [batch + 1] or NULL: prefix sums of the new tokens (those of refused and
+ *                shortened sequences are 0), as the other calls take them; they stop at 2^30 - 1
+ *   positions    device int32 [total] or NULL: token number of each new row, in the order of
+ *                cu_seqlens; -1 in the rows behind the last one
+ *   slots        device int64 [total] or NULL: page * p + slot of each new row; -1 where it has no page and behind the
+ *                last one
+ *   total        rows of positions and slots, 0 .. 2^28; further rows are not written
+ * One launch, no workspace; captured in a graph it works on the lengths and state of each replay.  Calls
+ * on the same list or table must not overlap.
+ */
+tilemix_status tilemix_paged_reserve(int32_t page_size, int32_t batch, int32_t max_pages, int32_t* page_table,
+                                     int64_t stride_table, const int32_t* seqlens, const int32_t* wanted,
+                                     int32_t window, int32_t* first_held, int32_t* free_ids,
+                                     int32_t capacity, int32_t* free_state, int32_t* free_state_out, int32_t* seqlens_out, int32_t* cu_seqlens,
+                                     int32_t* positions, int64_t* slots, int32_t total, void* stream);
+
+/* ------------------------------------------------------------------ rotary positions
+ * Q and K turned by their tokens' positions before they are attended to or cached.  Pair i < r / 2 of
+ * a head at position p:  (y1, y2) = g (x1 cos(p f_i) - x2 sin(p f_i), x2 cos(p f_i) + x1 sin(p f_i)); the
+ * channels from r = rotary_dim on stay as they are.
+ */
+typedef enum tilemix_rotary_layout {
+  TILEMIX_ROTARY_HALF = 0,         /* pair i: channels i and i + r / 2 */
+  TILEMIX_ROTARY_INTERLEAVED = 1   /* pair i: channels 2 i and 2 i + 1 */
+} tilemix_rotary_layout;
+
+typedef enum tilemix_scaling_kind {
+  TILEMIX_SCALING_NONE = 0,    /* f_i = base^(-2 i / r) */
+  TILEMIX_SCALING_LINEAR = 1,  /* position interpolation: f_i / s */
+  TILEMIX_SCALING_NTK = 2,     /* base s^(r / (r - 2)) in place of base */
+  TILEMIX_SCALING_YARN = 3     /* arXiv 2309.00071: between f_i and f_i / s by f_i's rotations over the original
+                                  length, n_i = original_len f_i / (2 pi): c f_i + (1 - c) f_i / s with
+                                  c = (n_i - beta_slow) / (beta_fast - beta_slow) clamped to [0, 1]; and
+                                  g = 0.1 ln s + 1 (1 for the other kinds) */
+} tilemix_scaling_kind;
+
+typedef struct tilemix_rotary_scaling {
+  int32_t kind;                 /* tilemix_scaling_kind */
+  int32_t rotary_dim;           /* r: even, 2 .. 128 */
+  double base;                  /* > 0 */
+  double factor;                /* s >= 1; ignored without scaling */
+  double beta_fast, beta_slow;  /* YaRN: rotations above which f_i is kept and below which it is divided */
+  int32_t original_len;         /* YaRN: tokens that the model was trained on, >= 1 */
+} tilemix_rotary_scaling;
+
+/* The frequencies of a scaling into HOST memory, double [r / 2], and g.  Runs on the host only. */
+tilemix_status tilemix_rotary_frequencies(const tilemix_rotary_scaling* scaling, double* inv_freq,
+                                          float* magnitude);
+
+typedef struct tilemix_rotary_params {
+  int32_t type;            /* of Q and K: TILEMIX_FP16 or TILEMIX_BF16 */
+  int32_t layout;          /* tilemix_rotary_layout */
+  int32_t head_dim;        /* d: 64 or 128 */
+  int32_t rotary_dim;      /* r: even, 2 .. d */
+  int32_t heads_q;         /* H_q >= 0; 0: no Q */
+  int32_t heads_k;         /* H_k >= 0; 0: no K */
+  int32_t inverse;         /* nonzero: turn back, by -p f_i (and stretch by g all the same): the gradient
+                              of the input, given that of the output */
+  float magnitude;         /* g, finite */
+  const double* inv_freq;  /* device double [r / 2], 8-byte aligned: f_i */
+} tilemix_rotary_params;
+
+/*
+ * tilemix_rotary -- rotary positions on Q and K in one pass.
+ *   positions    device int32 [total] or NULL: of each row; rows with a negative one are left out (their
+ *                outputs stay as they were)
+ *   seqlens_k, cu_seqlens, batch   without positions: the rows are the last ones of their sequences, as in
+ *                tilemix_paged_append: row r of the n of sequence b has position seqlens_k[b] - n + r, n =
+ *                cu_seqlens[b + 1] - cu_seqlens[b], or total / batch without cu_seqlens.  Packed rows that no sequence
+ *                owns are left out; out-of-range cu_seqlens are clamped
+ *   total        rows, 0 .. 2^28
+ *   Q, K         device, rows of H * d elements, 16-byte aligned, rows q_stride / k_stride elements apart
+ *                (>= 0, multiples of 8: a slice of a fused projection needs no copy)
+ *   Q_out, K_out written, rows q_out_stride / k_out_stride apart (>= H * d); may be Q and K with the same
+ *                strides, and may not overlap them otherwise
+ * Angles are reduced in FP64 (positions up to 2^31 keep 2^-24 of a turn), the rest is FP32, rounded once.
+ */
+tilemix_status tilemix_rotary(const tilemix_rotary_params* params, const int32_t* positions,
+                              const int32_t* seqlens_k, const int32_t* cu_seqlens, int32_t batch, int32_t total,
+                              const void* Q, int64_t q_stride, void* Q_out, int64_t q_out_stride, const void* K,
+                              int64_t k_stride, void* K_out, int64_t k_out_stride, void* stream);
+
 /* ------------------------------------------------------------------ routing templates
  * Host-side routing policies of Appendix B ("Policy Construction and Sharing", "Coverage
  * Accounting" and the layouts One, Zero, Band, Global, Row-Random, Aligned Sparse, BigBird,

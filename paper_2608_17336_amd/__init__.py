@@ -52,6 +52,11 @@ __all__ = [
     "tilemix_paged_gather",
     "tilemix_paged_decode_workspace_size",
     "tilemix_paged_decode",
+    "PageList",
+    "Reserved",
+    "tilemix_paged_reserve",
+    "tilemix_rotary_frequencies",
+    "tilemix_rotary",
     "EXPORTED_SYMBOLS",
 ]
 
@@ -84,6 +89,9 @@ EXPORTED_SYMBOLS = (
     "tilemix_paged_gather",
     "tilemix_paged_decode_workspace_size",
     "tilemix_paged_decode",
+    "tilemix_paged_reserve",
+    "tilemix_rotary_frequencies",
+    "tilemix_rotary",
     "tilemix_status_string",
     "tilemix_last_error",
 )
@@ -290,6 +298,13 @@ def load_library() -> ctypes.CDLL:
     lib.tilemix_paged_decode.argtypes = [CP, ctypes.c_int32, ctypes.c_int32, ctypes.c_float, ctypes.c_int32, vp,
                                          ctypes.c_int64, vp, vp, vp, ctypes.c_size_t, vp]
     lib.tilemix_paged_decode.restype = ctypes.c_int
+    i32, i64 = ctypes.c_int32, ctypes.c_int64
+    lib.tilemix_paged_reserve.argtypes = [i32, i32, i32, vp, i64, vp, vp, i32, vp, vp, i32, vp, vp, vp, vp, vp, vp, i32, vp]
+    lib.tilemix_paged_reserve.restype = ctypes.c_int
+    lib.tilemix_rotary_frequencies.argtypes = [CP, vp, ctypes.POINTER(ctypes.c_float)]
+    lib.tilemix_rotary_frequencies.restype = ctypes.c_int
+    lib.tilemix_rotary.argtypes = [CP, vp, vp, vp, i32, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp]
+    lib.tilemix_rotary.restype = ctypes.c_int
     lib.tilemix_route_coverage.argtypes = [P, vp, ctypes.POINTER(ctypes.c_double),
                                            ctypes.POINTER(ctypes.c_double)]
     lib.tilemix_route_coverage.restype = ctypes.c_int
@@ -1073,3 +1088,195 @@ def tilemix_paged_decode(cache: PagedCache, Q, page_table, seqlens_k, scale: flo
         c, fmt, heads, scale if scale is not None else 1.0 / math.sqrt(d), window, Q.data_ptr(), q_stride, O.data_ptr(),
         _ptr(lse), _ptr(workspace), nbytes, handle))
     return (O, lse) if return_lse else O
+
+
+class PageList(NamedTuple):
+    """The free pages of a pool for ``tilemix_paged_reserve``: ids int32 CUDA [capacity], a ring, and state int32 CUDA [4]:
+    where the first free page lies, how many there are, the sequences that the last call refused, 0."""
+    ids: object
+    state: object
+
+    @staticmethod
+    def full(pages: int, device="cuda") -> "PageList":
+        """All pages of a pool of ``pages`` are free."""
+        import torch
+        return PageList(torch.arange(pages, dtype=torch.int32, device=device),
+                        torch.tensor([0, pages, 0, 0], dtype=torch.int32, device=device))
+
+
+class Reserved(NamedTuple):
+    """What tilemix_paged_reserve returns: the new lengths int32 [B], prefix sums of the new tokens int32 [B + 1], and with
+    ``total`` the position (int32) and slot (int64) of each."""
+    seqlens: object
+    cu_seqlens: object
+    positions: object
+    slots: object
+
+
+def _require_or_empty(t, shape, dtype, like, device, stream, name):
+    """t, a dense tensor of this type and shape, or a new one."""
+    if t is None:
+        return _alloc(stream, shape, dtype=dtype, device=like.device)
+    _require_dense(t, dtype, shape, device, name)
+    return t
+
+
+def tilemix_paged_reserve(pages: PageList, page_table, seqlens, wanted, page_size: int, *, window: int = 0,
+                          first_held=None, total: int | None = None, state_out=None, seqlens_out=None, cu_seqlens=None, positions=None,
+                          slots=None, stream=None) -> Reserved:
+    """Move pages between ``page_table`` (int32 CUDA [B, max_pages]) and the free ``pages`` so that sequences of
+    ``seqlens`` tokens (int32 CUDA [B]) have room for ``wanted`` (int32 CUDA [B]; 0: done).  A sequence whose pages are
+    not there keeps its length.  ``seqlens`` and the list's state are updated in place, unless ``seqlens_out`` (int32
+    [B]) or ``state_out`` (int32 [4]) is given.  With ``total`` rows the new tokens' positions and slots
+    (page * page_size + slot) are written, -1 behind the last one; tensors for the results are allocated when not
+    given.  ``window``: a sliding window of that many tokens, whose pages go back when it has left them; ``first_held``
+    (int32 [B], 0 at the start) then keeps the first page-table entry that each sequence still holds."""
+    torch = _torch()
+    ids, state = pages
+    if not isinstance(ids, torch.Tensor) or not ids.is_cuda:
+        raise TypeError("the list's ids must be a CUDA (HIP) tensor")
+    dev, i32 = ids.get_device(), torch.int32
+    if ids.ndim != 1:
+        raise ValueError("the list's ids must be [capacity]")
+    _require_dense(ids, i32, ids.shape, dev, "the list's ids")
+    _require_dense(state, i32, (4,), dev, "the list's state")
+    if getattr(page_table, "ndim", None) != 2:
+        raise ValueError("page_table must be a tensor [B, max_pages]")
+    shape = page_table.shape
+    _require_like(page_table, i32, shape, dev, "page_table")
+    B = shape[0]
+    _require_dense(seqlens, i32, (B,), dev, "seqlens")
+    _require_dense(wanted, i32, (B,), dev, "wanted")
+    if (first_held is None) != (window == 0):
+        raise ValueError("first_held goes with a window, and with it only")
+    if first_held is not None:
+        _require_dense(first_held, i32, (B,), dev, "first_held")
+    if total is None and (positions is not None or slots is not None):
+        raise ValueError("total is needed with positions or slots")
+    _int32(page_size, "page_size"), _int32(window, "window"), _int32(total or 0, "total")
+    other = _elsewhere(dev)
+    if other is not None:
+        with other:
+            return tilemix_paged_reserve(pages, page_table, seqlens, wanted, page_size, window=window, first_held=first_held,
+                                         total=total, state_out=state_out,
+                                         seqlens_out=seqlens_out, cu_seqlens=cu_seqlens, positions=positions, slots=slots, stream=stream)
+    handle = _stream_on(stream, dev)
+    if state_out is None:
+        state_out = state
+    else:
+        _require_dense(state_out, i32, (4,), dev, "state_out")
+    if seqlens_out is None:
+        seqlens_out = seqlens
+    else:
+        _require_dense(seqlens_out, i32, (B,), dev, "seqlens_out")
+    cu_seqlens = _require_or_empty(cu_seqlens, (B + 1,), i32, ids, dev, stream, "cu_seqlens")
+    if total is not None:
+        if total < 0:
+            raise ValueError("total must be >= 0")
+        positions = _require_or_empty(positions, (total,), i32, ids, dev, stream, "positions")
+        slots = _require_or_empty(slots, (total,), torch.int64, ids, dev, stream, "slots")
+    _check(load_library().tilemix_paged_reserve(
+        page_size, B, shape[1], page_table.data_ptr(), _outer_stride(shape, page_table.stride(), 1, "page_table"), seqlens.data_ptr(),
+        wanted.data_ptr(), window, _ptr(first_held), ids.data_ptr(), ids.shape[0], state.data_ptr(), state_out.data_ptr(), seqlens_out.data_ptr(),
+        cu_seqlens.data_ptr(), _ptr(positions), _ptr(slots), total or 0, handle))
+    return Reserved(seqlens_out, cu_seqlens, positions, slots)
+
+
+# ------------------------------------------------------------------------- rotary positions
+
+_LAYOUTS = {"half": 0, "interleaved": 1}
+_SCALINGS = {None: 0, "linear": 1, "ntk": 2, "yarn": 3}
+_ROTARY = struct.Struct("<7ifQ")            # tilemix_rotary_params
+_ROTARY_SCALING = struct.Struct("<2i4di4x")  # tilemix_rotary_scaling
+
+
+def tilemix_rotary_frequencies(rotary_dim: int, base: float = 10000.0, *, scaling: str | None = None, factor: float = 1.0,
+                               original_len: int = 0, beta_fast: float = 32.0, beta_slow: float = 1.0, device="cuda"):
+    """(inv_freq float64 [rotary_dim / 2] on ``device``, magnitude) for tilemix_rotary.  ``scaling`` for contexts that are
+    ``factor`` times as long as those trained on: "linear" (positions / factor), "ntk" (a larger base) or "yarn" (arXiv
+    2309.00071, with ``original_len`` tokens trained on: frequencies of more than ``beta_fast`` rotations over them are
+    kept, those of fewer than ``beta_slow`` divided)."""
+    if scaling not in _SCALINGS:
+        raise ValueError(f"scaling must be one of {list(_SCALINGS)}, got {scaling!r}")
+    import torch
+    c = _ROTARY_SCALING.pack(_SCALINGS[scaling], _int32(rotary_dim, "rotary_dim"), base, factor, beta_fast, beta_slow,
+                             _int32(original_len, "original_len"))
+    out = (ctypes.c_double * 64)()
+    magnitude = ctypes.c_float()
+    _check(load_library().tilemix_rotary_frequencies(c, out, ctypes.byref(magnitude)))
+    return torch.tensor(out[:rotary_dim // 2], dtype=torch.float64, device=device), magnitude.value
+
+
+def tilemix_rotary(Q, K, inv_freq, positions=None, *, seqlens_k=None, cu_seqlens=None, layout: str = "half",
+                   magnitude: float = 1.0, inverse: bool = False, Q_out=None, K_out=None, stream=None):
+    """Rotary positions on Q and K, float16 or bfloat16 CUDA [total, H, d] or [B, L, H, d] (K may be None; tokens may
+    lie any multiple of 8 elements apart).  inv_freq: float64 CUDA [rotary_dim / 2], of tilemix_rotary_frequencies; channels from
+    rotary_dim on stay as they are.  Rows have the ``positions`` int32 CUDA [total] or [B, L], or are the last ones of
+    sequences of ``seqlens_k`` tokens (int32 CUDA [B]), packed by ``cu_seqlens`` (int32 CUDA [B + 1]) or L of each, as in
+    tilemix_paged_append.  Pairs are channels i and i + rotary_dim / 2 (layout "half") or 2 i and 2 i + 1
+    ("interleaved").  Returns (Q_out, K_out), allocated when not given; they may be Q and K.  Rows with a negative
+    position, or that no sequence owns, are not written.  ``inverse``: turned the other way, which makes gradients of Q and
+    K out of those of the results."""
+    torch = _torch()
+    if not isinstance(Q, torch.Tensor) or not Q.is_cuda:
+        raise TypeError("Q must be a CUDA (HIP) tensor")
+    dtype, shape, dev = Q.dtype, Q.shape, Q.get_device()
+    fmt = _format(dtype)
+    if fmt not in (0, 1):
+        raise TypeError(f"Q must be float16 or bfloat16, got {dtype}")
+    if len(shape) not in (3, 4):
+        raise ValueError("Q and K must be [total, H, d] or [B, L, H, d]")
+    if layout not in _LAYOUTS:
+        raise ValueError(f"layout must be one of {list(_LAYOUTS)}, got {layout!r}")
+    rows, (Hq, d) = shape[:-2], shape[-2:]
+    Hk, k_shape = 0, None
+    if K is not None:
+        if getattr(K, "ndim", None) != len(shape):
+            raise ValueError("K must have as many dimensions as Q")
+        Hk = K.shape[-2]
+        k_shape = (*rows, Hk, d)
+        _require_like(K, dtype, k_shape, dev, "K")
+    if getattr(inv_freq, "ndim", None) != 1:
+        raise ValueError("inv_freq must be a tensor [rotary_dim / 2]")
+    _require_dense(inv_freq, torch.float64, inv_freq.shape, dev, "inv_freq")
+    total = rows[0] if len(rows) == 1 else rows[0] * rows[1]
+    batch, pos, lens, cu = 1, None, None, None
+    if positions is not None:
+        if seqlens_k is not None or cu_seqlens is not None:
+            raise ValueError("positions and seqlens_k exclude each other")
+        _require_dense(positions, torch.int32, rows, dev, "positions")
+        pos = positions.data_ptr()
+    else:
+        if seqlens_k is None:
+            raise ValueError("positions or seqlens_k is needed")
+        batch = rows[0] if len(rows) == 2 else getattr(seqlens_k, "shape", (0,))[0]
+        _require_dense(seqlens_k, torch.int32, (batch,), dev, "seqlens_k")
+        lens = seqlens_k.data_ptr()
+        if (cu_seqlens is None) == (len(rows) == 1):
+            raise ValueError("cu_seqlens goes with [total, H, d], and with it only")
+        if cu_seqlens is not None:
+            _require_dense(cu_seqlens, torch.int32, (batch + 1,), dev, "cu_seqlens")
+            cu = cu_seqlens.data_ptr()
+    _int32(total, "total")
+    other = _elsewhere(dev)
+    if other is not None:
+        with other:
+            return tilemix_rotary(Q, K, inv_freq, positions, seqlens_k=seqlens_k, cu_seqlens=cu_seqlens, layout=layout,
+                                  magnitude=magnitude, inverse=inverse, Q_out=Q_out, K_out=K_out, stream=stream)
+    handle = _stream_on(stream, dev)
+    if Q_out is None:
+        Q_out = _alloc(stream, shape, dtype=dtype, device=Q.device)
+    else:
+        _require_like(Q_out, dtype, shape, dev, "Q_out")
+    k = ko = None
+    ks = kos = 0
+    if K is not None:
+        if K_out is None:
+            K_out = _alloc(stream, k_shape, dtype=dtype, device=K.device)
+        else:
+            _require_like(K_out, dtype, k_shape, dev, "K_out")
+        k, ks, ko, kos = K.data_ptr(), _row_stride(K, k_shape, "K"), K_out.data_ptr(), _row_stride(K_out, k_shape, "K_out")
+    c = _ROTARY.pack(fmt, _LAYOUTS[layout], d, 2 * inv_freq.shape[0], Hq, Hk, 1 if inverse else 0, magnitude, inv_freq.data_ptr())
+    _check(load_library().tilemix_rotary(c, pos, lens, cu, batch, total, Q.data_ptr(), _row_stride(Q, shape, "Q"), Q_out.data_ptr(),
+                                         _row_stride(Q_out, shape, "Q_out"), k, ks, ko, kos, handle))
+    return Q_out, K_out

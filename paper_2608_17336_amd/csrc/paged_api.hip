@@ -215,4 +215,38 @@ tilemix_status tilemix_paged_decode(const tilemix_paged_cache* cache, int32_t ty
                     "paged decode");
 }
 
+tilemix_status tilemix_paged_reserve(int32_t page_size, int32_t batch, int32_t max_pages, int32_t* page_table,
+                                     int64_t stride_table, const int32_t* seqlens, const int32_t* wanted,
+                                     int32_t window, int32_t* first_held, int32_t* free_ids,
+                                     int32_t capacity, int32_t* free_state, int32_t* free_state_out, int32_t* seqlens_out, int32_t* cu_seqlens,
+                                     int32_t* positions, int64_t* slots, int32_t total, void* stream) {
+  if (page_size < 16 || page_size > 256 || (page_size & (page_size - 1)))
+    return fail(TILEMIX_ERR_UNSUPPORTED, "page_size %d not supported (16, 32, 64, 128 or 256)", page_size);
+  if (batch < 1 || batch > 65535) return fail(TILEMIX_ERR_SHAPE, "batch must be 1 .. 65535");
+  if (max_pages < 1 || (long long)max_pages * page_size > (1LL << 30))
+    return fail(TILEMIX_ERR_SHAPE, "max_pages must be >= 1 and max_pages * page_size <= 2^30");
+  if (stride_table < max_pages || stride_table > kStrideMax) return fail(TILEMIX_ERR_SHAPE, "stride_table must be >= max_pages");
+  if (window < 0) return fail(TILEMIX_ERR_SHAPE, "window must be >= 0");
+  if (capacity < 1 || capacity > (1 << 30) - 2) return fail(TILEMIX_ERR_SHAPE, "capacity must be 1 .. 2^30 - 2");
+  if (total < 0 || total > kRowsMax) return fail(TILEMIX_ERR_SHAPE, "total must be 0 .. %d", kRowsMax);
+  if (!page_table || !seqlens || !wanted || !free_ids || !free_state || !free_state_out || !seqlens_out)
+    return fail(TILEMIX_ERR_NULL, "page_table, lengths, free_ids and free_state must be non-NULL");
+  if (window && !first_held) return fail(TILEMIX_ERR_NULL, "a window needs first_held");
+  for (const void* p : {(const void*)page_table, (const void*)seqlens, (const void*)wanted, (const void*)free_ids, (const void*)free_state,
+                        (const void*)free_state_out, (const void*)seqlens_out, (const void*)first_held, (const void*)cu_seqlens, (const void*)positions})
+    if (!aligned(p, 4)) return fail(TILEMIX_ERR_ALIGN, "page_table, lengths, free_ids, free_state and positions must be 4-byte aligned");
+  if (!aligned(slots, 8)) return fail(TILEMIX_ERR_ALIGN, "slots must be 8-byte aligned");
+  tilemix::ReserveArgs a{};
+  while ((1 << a.page_shift) < page_size) ++a.page_shift;
+  a.B = batch; a.max_pages = max_pages;
+  a.window = window; a.first_held = window ? first_held : nullptr;
+  a.table = page_table; a.stride_table = stride_table;
+  a.old_lens = seqlens; a.want = wanted;
+  a.ids = free_ids; a.capacity = capacity;
+  a.state = free_state; a.state_out = free_state_out;
+  a.lens_out = seqlens_out; a.cu = cu_seqlens;
+  a.positions = positions; a.slots = reinterpret_cast<long long*>(slots); a.total = total;
+  return hip_status(tilemix::launch_paged_reserve(a, static_cast<hipStream_t>(stream)), "paged reserve");
+}
+
 }  // extern "C"

@@ -221,4 +221,46 @@ PagedDecodePlan plan_paged_decode(const PagedPool& p, int heads_q, int d, int wi
 hipError_t launch_paged_decode(PagedDecodeArgs args, const PagedDecodePlan& plan, int d, int type, int format,
                                hipStream_t stream);
 
+// Arguments of the rotary positions kernel.
+struct RotaryArgs {
+  const int* positions;    // [total]; or nullptr: of the last rows of sequences of these lengths
+  const int* seqlens;      // [batch]
+  const int* cu;           // [batch + 1], or nullptr: total / batch rows per sequence
+  int batch, total;
+  FastDiv div_len;         // rows per sequence, without cu
+  const double* inv_freq;  // [r / 2]
+  float magnitude;
+  int inverse;
+  int d, r, Hq, Hk;
+  int in_place;            // all outputs are their inputs
+  const void* Q;
+  const void* K;
+  void* Q_out;
+  void* K_out;
+  long long q_stride, k_stride, q_out_stride, k_out_stride;   // elements between rows
+  int unit_shift, token_shift;   // filled in by the launch: log2 of the lanes of a head, of the rows of a workgroup
+  FastDiv div_pairs;             // filled in by the launch: r / 2
+};
+hipError_t launch_rotary(RotaryArgs args, int type, bool half, hipStream_t stream);
+
+// Arguments of the reservation of pages.
+struct ReserveArgs {
+  int page_shift, B, max_pages, window;
+  int* table;              // [B, max_pages], rows stride_table entries apart
+  long long stride_table;
+  const int* old_lens;     // [B]
+  const int* want;         // [B]
+  int* first_held;         // [B], with a window
+  int* ids;                // [capacity]: a ring of free pages
+  int capacity;
+  int* state;              // head, count, refused, workgroups that have arrived
+  int* state_out;          // head, count, refused, 0; may be state
+  int* lens_out;           // [B]; may be old_lens
+  int* cu;                 // [B + 1] or nullptr
+  int* positions;          // [total] or nullptr
+  long long* slots;        // [total] or nullptr
+  int total;
+};
+hipError_t launch_paged_reserve(const ReserveArgs& args, hipStream_t stream);
+
 }  // namespace tilemix
