@@ -25,13 +25,15 @@ constexpr int kCUs = 256;
 // heads of d = 128: 3 tiles 58.6, 6 53.6, 9 54.6, 14 57.5.)
 constexpr int kPartStart = 6;
 constexpr int kPagedHeads = 16;                  // query heads on the columns of a matrix-core tile
-// A tile is two slabs of 16 keys.  (Four slabs of an 8-bit cache leave two waves per SIMD instead of three: 32
+// A tile is two slabs of 16 keys, of an MXFP4 cache, whose rows are half as long as an 8-bit one's, four: as many
+// bytes, so that as many are on their way.  (Four slabs of an 8-bit cache leave two waves per SIMD instead of three: 32
 // sequences of 64 to 8192 keys 34.9 us, with two slabs 30.9; 4 x 65536 keys 102.9 and 105.1.)
-constexpr int kSlabs = 2, kTileKeys = 16 * kSlabs;
+constexpr int tile_slabs(int format) { return is_4bit(format) ? 4 : 2; }
 // Waves that a SIMD holds, by their registers (K and V rows of a tile, the output): workgroups per CU.
 constexpr int resident_per_cu(int d) { return d == 64 ? 4 : 3; }
 
 // The tokens that a sequence's query attends to: first .. len - 1, of tiles tile0 .. .
+template <int KEYS>   // of a tile
 struct Span {
   int first = 0, len = 0, tile0 = 0, tiles = 0;
   Span() = default;
@@ -39,8 +41,8 @@ struct Span {
     const PagedPool& p = a.pool;
     len = min(max(tokens, 0), p.max_pages << p.page_shift);
     first = a.window > 0 ? max(len - a.window, 0) : 0;
-    tile0 = first / kTileKeys;
-    tiles = (len + kTileKeys - 1) / kTileKeys - tile0;
+    tile0 = first / KEYS;
+    tiles = (len + KEYS - 1) / KEYS - tile0;
   }
   // Tiles as they are shared out: a sequence without tokens has one, so that it is written, too.
   __device__ __forceinline__ int share() const { return max(1, tiles); }
@@ -83,6 +85,7 @@ __device__ __forceinline__ int wave_max(int x) {
   return __builtin_amdgcn_readlane(x, kWave - 1);
 }
 
+template <int KEYS>
 struct Run {
   int b = -1, head_block, unit;   // where it begins (unit, or piece: of its sequence's); b = -1: no tile is left
   int mode, quota;
@@ -92,7 +95,7 @@ struct Run {
   }
   __device__ __forceinline__ Run(const PagedDecodeArgs& a, int w, int lane) {
     const int B = a.pool.B, per = (B + kWave - 1) / kWave, b0 = min(lane * per, B), b1 = min(b0 + per, B), W = gridDim.x;
-    auto share = [&](int s) { return Span(a, a.pool.seqlens[s]).share(); };
+    auto share = [&](int s) { return Span<KEYS>(a, a.pool.seqlens[s]).share(); };
     auto wave_total = [](int x) { return __builtin_amdgcn_readlane(wave_scan(x), kWave - 1); };
     // (Of up to 64 sequences, a lane's length is read once.)
     const int mine = b0 < b1 ? share(b0) : 0;
@@ -163,8 +166,9 @@ struct Run {
 };
 
 // A workgroup's part of one sequence and head block.  All members are the same in every lane.
+template <int KEYS>
 struct Part {
-  Span span;
+  Span<KEYS> span;
   int b = -1, head_block = 0;
   int lo = 0, hi = 0;          // its tiles, counted from the span's first: lo .. hi - 1 of span.share()
   int take = 0;                // the units that they are
@@ -173,7 +177,7 @@ struct Part {
   int hk = 0, g0 = 0;          // KV head, first query head of the block among the KV head's
   Part() = default;
   // From unit `off` of the sequence and head block on, `left` units at most.
-  __device__ __forceinline__ Part(const PagedDecodeArgs& a, int mode, int quota, int b_, int hb, int off, int left, const Span& sp)
+  __device__ __forceinline__ Part(const PagedDecodeArgs& a, int mode, int quota, int b_, int hb, int off, int left, const Span<KEYS>& sp)
       : span(sp), b(b_), head_block(hb) {
     const int n = span.share();
     hk = (int)a.div_blocks.quot(hb);
@@ -252,6 +256,12 @@ __device__ __forceinline__ float quad_rows_sum(float x) {
   return pair_sum(__builtin_bit_cast(float, (int)r[0]) + __builtin_bit_cast(float, (int)r[1]));
 }
 
+// x of lane L of the four lanes that agree in lane / 4.
+template <int L>
+__device__ __forceinline__ uint32_t quad_lane(uint32_t x) {
+  return (uint32_t)dpp<L * 0x55>((int)x, (int)x);
+}
+
 // p = 2^(s - m) is taken against the running max m, and so is the normalizer z = sum p.  The weights of the codes
 // are p dV 2^-x (p 2^-x for 16 and 4 bits): x = 0 for a BF16 cache and MXFP4, -15 for an FP16 one, and e - 15 for an 8-bit
 // one, where 2^e is above every value scale dV so far.  They stay at 2^15 at most, and are handed to the matrix cores as
@@ -293,8 +303,10 @@ struct DecodeShared {
 };
 
 template <int D, int TYPE, int FORMAT, bool STREAM>
-__device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run& run, DecodeShared<D>& shared) {
-  constexpr int kS = kSlabs, kKeys = kTileKeys;
+__device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run<16 * tile_slabs(FORMAT)>& run, DecodeShared<D>& shared) {
+  constexpr int kS = tile_slabs(FORMAT), kKeys = 16 * kS;
+  typedef Span<kKeys> Span;
+  typedef Part<kKeys> Part;
   constexpr int kBytes = kElemBytes<FORMAT>;
   constexpr bool k8 = is_8bit(FORMAT), k4 = is_4bit(FORMAT);
   constexpr int kRow = kRowBytes<D, FORMAT>, kScaleRow = kScaleBytes<D, FORMAT>;
@@ -302,7 +314,7 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run& 
   constexpr int kC = D / 16;                       // channels of a lane's value row: output products
   constexpr int kVW = k4 ? 1 : kC * kBytes / 4;    // dwords of them
   constexpr int kQ = D / 32;                       // score products per slab
-  constexpr int kQueryPieces = k4 && TYPE == TILEMIX_FP16 ? 2 : 1;   // BF16 pieces of the query
+  constexpr bool kRelative = k4 && TYPE == TILEMIX_FP16;   // keys relative to the largest exponent of their tile (see 4.)
   const PagedPool& p = a.pool;
   const int tid = threadIdx.x, lane = tid & (kWave - 1);
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
@@ -329,7 +341,7 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run& 
 
   // 1. Page ids of the wave's tiles n, n + kPagedWaves, .. of a part, 64 at a time: lane (i, j) holds the j-th of
   //    the 2^per_shift pages of tile i.
-  const int per_shift = max(0, 5 - p.page_shift);
+  const int per_shift = max(0, (kKeys == 64 ? 6 : 5) - p.page_shift);
   auto load_ids = [&](const Part& q, int n0) {
     const int n = n0 + (lane >> per_shift) * kPagedWaves;
     const int e = (n * kKeys >> p.page_shift) + (lane & ((1 << per_shift) - 1));
@@ -344,7 +356,7 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run& 
   uint4 kr[kS][kKL];
   uint32_t vr[kS][4][kVW];
   f32x4 dk[kS], dv[kS];
-  uint32_t ek[kS], ev[kS][kScaleRow ? kScaleRow : 1];              // MXFP4: exponent of the lane's channels of key l16; of all blocks of keys 4 lq ..
+  uint32_t ek[kS], ev[kS];                         // MXFP4: exponents of the lane's channels of key l16; of key 4 lq + l16 % 4
   int page[kS];                                    // per slab, of the tile that was requested last
   const char* poolK = static_cast<const char*>(p.K);
   const char* poolV = static_cast<const char*>(p.V);
@@ -395,14 +407,9 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run& 
 #pragma unroll
       for (int s = 0; s < kS; ++s) {
         const char* at = static_cast<const char*>(p.dV) + max(page[s], 0) * p.stride_dv + (long long)slab_row(hk, n, s) * kScaleRow +
-                         (some ? 4 * kScaleRow * lq : 0);
-        if constexpr (kScaleRow == 4) {
-          const u32x4 x = *reinterpret_cast<const u32x4*>(at);
-          ev[s][0] = x[0]; ev[s][1] = x[1]; ev[s][2] = x[2]; ev[s][3] = x[3];
-        } else {
-          const u32x2 x = *reinterpret_cast<const u32x2*>(at);
-          ev[s][0] = x[0]; ev[s][1] = x[1];
-        }
+                         (some ? kScaleRow * (4 * lq + l16 % 4) : 0);
+        if constexpr (kScaleRow == 4) ev[s] = *reinterpret_cast<const uint32_t*>(at);
+        else ev[s] = *reinterpret_cast<const uint16_t*>(at);
       }
     }
 #pragma unroll
@@ -425,7 +432,7 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run& 
       }
     }
   };
-  uint4 qf[kQ], ql[kQ];                            // ql: the second pieces
+  uint4 qf[kQ];
   auto load_query = [&](const Part& q) {
     const int G = a.group, heads = min(kPagedHeads, G - q.g0);
     const char* row = static_cast<const char*>(a.Q) + 2 * (q.b * a.q_stride + (long long)(q.hk * G + q.g0 + min(l16, heads - 1)) * D);
@@ -490,18 +497,6 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run& 
           qf[i] = make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
         }
       }
-      if constexpr (kQueryPieces == 2) {   // FP16's 11 bits are two BF16 numbers of 8 and 3
-  #pragma unroll
-        for (int i = 0; i < kQ; ++i) {
-          const uint32_t w[4] = {qf[i].x, qf[i].y, qf[i].z, qf[i].w};
-          uint32_t h[4], l[4];
-  #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            split2<FORMAT>(bits_to_float<TILEMIX_FP16>(w[e] & 0xffffu), bits_to_float<TILEMIX_FP16>(w[e] >> 16), h[e], l[e]);
-          qf[i] = make_uint4(h[0], h[1], h[2], h[3]);
-          ql[i] = make_uint4(l[0], l[1], l[2], l[3]);
-        }
-      }
     }
 
     // 4. The wave's tiles.  m: running max (log2 units); x: the weights' power of two; z: this lane's share of the
@@ -522,18 +517,36 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run& 
   #pragma unroll
       for (int s = 0; s < kS; ++s) has |= page[s] >= 0 ? 1u << s : 0u;
       all = all && has == (1u << kS) - 1;
-      float sc[kS][4], ve[kS][4];   // ve: MXFP4, scale of the lane's channels of key 4 lq + r
+      // FP16 queries take MXFP4 keys in FP16: code 2^(e - top), top the largest exponent of a key that counts, so that
+      // what FP16 cannot hold lies below 2^-25 of the tile's largest key.  (As two BF16 pieces, which lose nothing, they took
+      // twice the products and 16 registers more, which spilled: 8 x 65536 keys 119 us.)  A NaN among them is one in all scores.
+      float f_tile = f_head;
+      uint32_t top = 0;
+      if constexpr (kRelative) {
+        if (!all) {
+  #pragma unroll
+          for (int s = 0; s < kS; ++s) {
+            const int t = n * kKeys + 16 * s + l16;
+            ek[s] = (has >> s & 1) && t >= cur.span.first && t < cur.span.len ? ek[s] : 0u;
+          }
+        }
+        uint32_t e = ek[0];
+  #pragma unroll
+        for (int s = 1; s < kS; ++s) e = max(e, ek[s]);
+        top = (uint32_t)wave_max((int)e);
+        f_tile = top == kBlockNaN ? __builtin_nanf("") : __builtin_amdgcn_ldexpf(f_head, (int)top - 127);
+      }
+      float sc[kS][4];
   #pragma unroll
       for (int s = 0; s < kS; ++s) {
         f32x4 c = {0.0f, 0.0f, 0.0f, 0.0f};
         if constexpr (k4) {
-          const float scale = block_scale(ek[s]);
+          const float scale = kRelative ? block_scale(max(ek[s] + 127, top) - top) : block_scale(ek[s]);
           const uint32_t w[4] = {kr[s][0].x, kr[s][0].y, kr[s][0].z, kr[s][0].w};
   #pragma unroll
           for (int k = 0; k < kQ; ++k) {
-            const uint4 x = mx_values8<TILEMIX_BF16>(w[k], scale);
-            c = mfma_16<FORMAT>(x, qf[k], c);
-            if constexpr (kQueryPieces == 2) c = mfma_16<FORMAT>(x, ql[k], c);
+            constexpr int kType = kRelative ? TILEMIX_FP16 : TILEMIX_BF16;
+            c = mfma_16<kType>(mx_values8<kType>(w[k], scale), qf[k], c);
           }
         }
   #pragma unroll
@@ -547,7 +560,7 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run& 
         }
         // Scores are scaled and rounded before the max and the exponent see them.
   #pragma unroll
-        for (int r = 0; r < 4; ++r) sc[s][r] = c[r] * (k8 ? f_head * dk[s][r] : f_head);
+        for (int r = 0; r < 4; ++r) sc[s][r] = c[r] * (k8 ? f_head * dk[s][r] : f_tile);
       }
       __builtin_amdgcn_sched_barrier(0);
       const bool here = n + kPagedWaves < cur.end;
@@ -566,15 +579,6 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run& 
       }
       find_pages(ids, i);
       load_keys(hk, to, some);
-      if constexpr (k4) {
-  #pragma unroll
-        for (int s = 0; s < kS; ++s)
-  #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const uint32_t w = ev[s][r * kScaleRow / 4] >> 16 * (r * kScaleRow / 2 % 2);
-            ve[s][r] = block_scale(w >> 8 * (l16 * kC / 32) & 0xffu);
-          }
-      }
       if (!all) {
   #pragma unroll
         for (int s = 0; s < kS; ++s)
@@ -586,7 +590,7 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run& 
             if constexpr (k8) dv[s][r] = ok ? dv[s][r] : 0.0f;
             // What a slot behind the sequence holds may be a NaN, which a weight of 0 does not cancel.
             if constexpr (k4) {
-              ve[s][r] = ok ? ve[s][r] : 0.0f;
+              if (l16 % 4 == r) ev[s] = ok ? ev[s] : 0u;
             } else if constexpr (FORMAT != TILEMIX_INT8) {
   #pragma unroll
               for (int w = 0; w < kVW; ++w) vr[s][r][w] = ok ? vr[s][r][w] : 0u;
@@ -621,9 +625,13 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run& 
       }
       // No finite score so far: p = 2^(-inf - 0) = 0, not a NaN.
       const float sub = m == ninf ? 0.0f : m;
-      uint2 hi[kS], lo[kS];
+      // O^T += V^T P^T.
+#pragma unroll
+      for (int t = 0; t < kS; t += 2) {   // a pair of slabs
+      uint2 hi[2], lo[2];
   #pragma unroll
-      for (int s = 0; s < kS; ++s) {
+      for (int u = 0; u < 2; ++u) {
+        const int s = t + u;
         float w[4];
   #pragma unroll
         for (int r = 0; r < 4; ++r) {
@@ -632,19 +640,27 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run& 
           if constexpr (k8) w[r] *= __builtin_amdgcn_ldexpf(dv[s][r], -x);
           else if constexpr (FORMAT == TILEMIX_FP16) w[r] *= 0x1p15f;
         }
-        split2<FORMAT>(w[0], w[1], hi[s].x, lo[s].x);
-        split2<FORMAT>(w[2], w[3], hi[s].y, lo[s].y);
+        split2<FORMAT>(w[0], w[1], hi[u].x, lo[u].x);
+        split2<FORMAT>(w[2], w[3], hi[u].y, lo[u].y);
       }
-      // O^T += V^T P^T.
       const uint4 ph = make_uint4(hi[0].x, hi[0].y, hi[1].x, hi[1].y), pl = make_uint4(lo[0].x, lo[0].y, lo[1].x, lo[1].y);
-      auto row = [&](int j) -> const uint32_t (&)[kVW] { return vr[j / 4][j % 4]; };   // of the lane's key j < 8
+      auto row = [&](int j) -> const uint32_t (&)[kVW] { return vr[t + j / 4][j % 4]; };   // of the lane's key j < 8
       auto add = [&](int c, const uint32_t (&v)[4]) {
         const uint4 va = make_uint4(v[0], v[1], v[2], v[3]);
         acc[c] = mfma_16<FORMAT>(va, ph, acc[c]);
         acc[c] = mfma_16<FORMAT>(va, pl, acc[c]);
       };
       if constexpr (k4) {
-        // Two channels of a key in a byte: widened, with the key's scale, then paired.
+        // Two channels of a key in a byte: widened, with the key's scale of the lane's channels, then paired.
+        // (The conversion takes a scale's exponent field and leaves the other bits alone.  Byte b is brought there by a
+        // rotation to the right by 8 b + 9.)
+        float ve[8];
+  #pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const uint32_t w[4] = {quad_lane<0>(ev[t + u]), quad_lane<1>(ev[t + u]), quad_lane<2>(ev[t + u]), quad_lane<3>(ev[t + u])};
+  #pragma unroll
+          for (int r = 0; r < 4; ++r) ve[4 * u + r] = __builtin_bit_cast(float, __builtin_amdgcn_alignbit(w[r], w[r], 8 * (l16 * kC / 32) + 9));
+        }
   #pragma unroll
         for (int c = 0; c < kC; c += 2) {
           uint32_t v[2][4];
@@ -654,7 +670,7 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run& 
   #pragma unroll
             for (int u = 0; u < 2; ++u) {
               const uint32_t w = row(2 * j + u)[0];
-              const float scale = ve[(2 * j + u) / 4][(2 * j + u) % 4];
+              const float scale = ve[2 * j + u];
               x[u] = c == 0 ? mx_values<TILEMIX_BF16, 0>(w, scale) : c == 2 ? mx_values<TILEMIX_BF16, 1>(w, scale)
                    : c == 4 ? mx_values<TILEMIX_BF16, 2>(w, scale) : mx_values<TILEMIX_BF16, 3>(w, scale);
             }
@@ -696,6 +712,7 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run& 
           }
           add(c, v);
         }
+      }
       }
       __builtin_amdgcn_sched_barrier(0);   // not ahead of P V: their registers are in use
       load_values(hk, to, some);
@@ -788,9 +805,10 @@ template <int D, int TYPE, int FORMAT>
 __global__ __launch_bounds__(kPagedWaves * kWave) __attribute__((amdgpu_waves_per_eu(resident_per_cu(D))))
 void paged_decode_kernel(PagedDecodeArgs a) {
   __shared__ DecodeShared<D> shared;
-  const Run run(a, blockIdx.x, threadIdx.x & (kWave - 1));
+  constexpr int kKeys = 16 * tile_slabs(FORMAT);
+  const Run<kKeys> run(a, blockIdx.x, threadIdx.x & (kWave - 1));
   // (Two copies of the body: a branch at each request would make the waits count loads that were not issued.)
-  const long long bytes = (long long)__builtin_amdgcn_readfirstlane(run.total) * (kTileKeys * 2 * kRowBytes<D, FORMAT>);
+  const long long bytes = (long long)__builtin_amdgcn_readfirstlane(run.total) * (kKeys * 2 * kRowBytes<D, FORMAT>);
   if (bytes >= kStreamBytes && a.head_blocks == a.pool.Hk) decode_run<D, TYPE, FORMAT, true>(a, run, shared);
   else decode_run<D, TYPE, FORMAT, false>(a, run, shared);
 }
@@ -902,13 +920,13 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedDecodeArg
 
 }  // namespace
 
-PagedDecodePlan plan_paged_decode(const PagedPool& p, int heads_q, int d, int window) {
-  const int G = heads_q / p.Hk;
+PagedDecodePlan plan_paged_decode(const PagedPool& p, int heads_q, int d, int format, int window) {
+  const int G = heads_q / p.Hk, keys = 16 * tile_slabs(format);
   PagedDecodePlan pl{};
   pl.head_blocks = p.Hk * ((G + kPagedHeads - 1) / kPagedHeads);
   pl.part_heads = std::min(G, kPagedHeads);
-  long long most = (((long long)p.max_pages << p.page_shift) + kTileKeys - 1) / kTileKeys;   // tiles of a sequence
-  if (window > 0) most = std::min<long long>(most, (window + kTileKeys - 2LL) / kTileKeys + 1);
+  long long most = (((long long)p.max_pages << p.page_shift) + keys - 1) / keys;   // tiles of a sequence
+  if (window > 0) most = std::min<long long>(most, (window + keys - 2LL) / keys + 1);
   const long long segments = (long long)p.B * pl.head_blocks;
   pl.units = segments * (most + kPartStart);
   const long long resident = kCUs * resident_per_cu(d);

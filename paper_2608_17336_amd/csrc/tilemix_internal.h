@@ -217,7 +217,7 @@ struct PagedDecodePlan {
   long long units;         // the most units that the batch can have
   long long workgroups;
 };
-PagedDecodePlan plan_paged_decode(const PagedPool& p, int heads_q, int d, int window);
+PagedDecodePlan plan_paged_decode(const PagedPool& p, int heads_q, int d, int format, int window);
 hipError_t launch_paged_decode(PagedDecodeArgs args, const PagedDecodePlan& plan, int d, int type, int format,
                                hipStream_t stream);
 
