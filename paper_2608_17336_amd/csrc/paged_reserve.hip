@@ -28,17 +28,27 @@ __device__ __forceinline__ int wave_scan_most(int x) {
   return x;
 }
 
-// Sums over the threads before each one into before[], before[THREADS] the sum over all.
-template <int THREADS>
-__device__ __forceinline__ void block_scan(int x, int* before, int* waves) {
+// Sums over the threads before each one into before[i][], the sum over all into before[i][THREADS].
+template <int THREADS, int N>
+__device__ __forceinline__ void block_scan(const int (&x)[N], int (*before)[THREADS + 1], int (*waves)[THREADS / kWave]) {
   const int tid = threadIdx.x, wave = tid / kWave;
-  const int sum = wave_scan_most(x);
-  if (tid % kWave == kWave - 1) waves[wave] = sum;
+  int sum[N], base[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    sum[i] = wave_scan_most(x[i]);
+    base[i] = 0;
+    if (tid % kWave == kWave - 1) waves[i][wave] = sum[i];
+  }
   __syncthreads();
-  int base = 0;
-  for (int w = 0; w < wave; ++w) base = add(base, waves[w]);
-  before[tid + 1] = add(base, sum);
-  if (tid == 0) before[0] = 0;
+#pragma unroll
+  for (int w = 0; w < THREADS / kWave - 1; ++w)   // (all are read: the reads then do not wait for one another)
+#pragma unroll
+    for (int i = 0; i < N; ++i) base[i] = add(base[i], w < wave ? waves[i][w] : 0);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    before[i][tid + 1] = add(base[i], sum[i]);
+    if (tid == 0) before[i][0] = 0;
+  }
   __syncthreads();
 }
 
@@ -48,6 +58,7 @@ struct Ask {
   int held, keep;               // first entry that it holds, and that it will hold if it grows
   bool fits;
   int need;                     // pages
+  Ask() = default;
   __device__ __forceinline__ Ask(const ReserveArgs& a, int b) {
     const long long cap = (long long)a.max_pages << a.page_shift;
     from = (int)min((long long)max(a.old_lens[b], 0), cap);
@@ -71,6 +82,7 @@ struct Ask {
 // go back.
 struct Share {
   int len, held, rows = 0, e0 = 0, entries = 0, g0 = 0, give = 0;
+  Share() = default;
   // sum: pages wanted by it and all before it.
   __device__ __forceinline__ Share(const ReserveArgs& a, const Ask& q, int sum, int count) {
     const bool ok = q.fits && (q.need == 0 || sum <= count);
@@ -95,108 +107,105 @@ struct Share {
 
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void paged_reserve_kernel(ReserveArgs a) {
-  // Sums of the runs of the threads before each one.
-  __shared__ int needs[THREADS + 1], entries[THREADS + 1], gives[THREADS + 1], rows[THREADS + 1];
-  __shared__ int waves[4][THREADS / kWave];
+  // Sums of the runs of the threads before each one: pages needed; entries set, pages given back, new rows.
+  enum { kEntries, kGives, kRowsSum };
+  __shared__ int needed[1][THREADS + 1], sums[3][THREADS + 1], waves[3][THREADS / kWave];
   __shared__ int refused, taken, last;
+  __shared__ Ask asks[THREADS];   // where a run is one sequence: looked up again and again
   const int tid = threadIdx.x, W = gridDim.x, wg = blockIdx.x, N = a.capacity;
   const int per = (a.B + THREADS - 1) / THREADS, b0 = min(tid * per, a.B), b1 = min(b0 + per, a.B);
   const int count = min(max(a.state[1], 0), N), head = (int)((uint32_t)max(a.state[0], 0) % (uint32_t)N);
+  const int* needs = needed[0];
+  auto ask = [&](int b) { return per == 1 ? asks[b] : Ask(a, b); };
   if (tid == 0) refused = taken = 0;
-  int need = 0;
-  for (int b = b0; b < b1; ++b) need = add(need, Ask(a, b).need);
-  block_scan<THREADS>(need, needs, waves[0]);
-  int set = 0, give = 0, row = 0, no = 0, take = 0, sum = needs[tid];
+  int need[1] = {0};
   for (int b = b0; b < b1; ++b) {
     const Ask q(a, b);
+    if (per == 1) asks[b] = q;
+    need[0] = add(need[0], q.need);
+  }
+  block_scan<THREADS>(need, needed, waves);
+  int own[3] = {0, 0, 0}, no = 0, take = 0, sum = needs[tid];
+  for (int b = b0; b < b1; ++b) {
+    const Ask q = ask(b);
     sum = add(sum, q.need);
     const Share s(a, q, sum, count);
-    set = add(set, s.entries);
-    give = add(give, s.give);
-    row = add(row, s.rows);
+    own[kEntries] = add(own[kEntries], s.entries);
+    own[kGives] = add(own[kGives], s.give);
+    own[kRowsSum] = add(own[kRowsSum], s.rows);
     if (s.entries) take += q.need;   // (not more than the list has)
     no += !q.fits || (q.need > 0 && sum > count);
   }
-  block_scan<THREADS>(set, entries, waves[1]);
-  block_scan<THREADS>(give, gives, waves[2]);
-  block_scan<THREADS>(row, rows, waves[3]);
+  __syncthreads();   // `waves` is used again
   if (no) atomicAdd(&refused, no);
   if (take) atomicAdd(&taken, take);
+  block_scan<THREADS>(own, sums, waves);
+  const int entries = sums[kEntries][THREADS], gives = sums[kGives][THREADS], rows = sums[kRowsSum][THREADS];
 
-  // f(sequence, Ask, Share, item within its share, pages wanted before it) of item k, which `before` counts.
-  auto find = [&](const int* before, int k, auto&& part, auto&& f) {
-    int t = 0;   // the last thread with before[t] <= k
-#pragma unroll
-    for (int step = THREADS / 2; step; step /= 2) t += before[t + step] <= k ? step : 0;
-    int at = before[t], wanted = needs[t];
-    for (int b = t * per; b < min(t * per + per, a.B); ++b) {
-      const Ask q(a, b);
-      const int below = wanted;
-      wanted = add(wanted, q.need);
-      const Share s(a, q, wanted, count);
-      const int n = part(s);
-      if (k - at < n) {
-        f(b, q, s, k - at, below);
-        return;
-      }
-      at += n;
-    }
-  };
   auto ring = [&](int i) { return i < N ? i : i - N; };   // i < 2 N
-  const int stride = W * THREADS, at0 = wg * THREADS + tid;
-  for (int k = at0; k < entries[THREADS]; k += stride)
-    find(entries, k, [](const Share& s) { return s.entries; }, [&](int b, const Ask& q, const Share& s, int i, int below) {
-      const int e = s.e0 + i, n = e - q.first(a);
-      a.table[b * a.stride_table + e] = n >= 0 ? a.ids[ring(head + below + n)] : -1;
-    });
-  for (int k = at0; k < gives[THREADS]; k += stride)
-    find(gives, k, [](const Share& s) { return s.give; }, [&](int b, const Ask&, const Share& s, int i, int) {
-      int* entry = a.table + b * a.stride_table + s.g0 + i;
-      if (k < N - count) a.ids[ring(head + count + k)] = *entry;
-      *entry = -1;
-    });
-  if (a.positions || a.slots) {
-    for (int k = at0; k < a.total; k += stride) {
-      int pos = -1;
-      long long slot = -1;
-      if (k < rows[THREADS])
-        find(rows, k, [](const Share& s) { return s.rows; }, [&](int b, const Ask& q, const Share&, int i, int below) {
-          pos = q.from + i;
-          const int e = pos >> a.page_shift;
-          if (!a.slots || e < q.keep) return;   // (the window leaves it at once: it has no page)
-          const int page = e < Ask::have(a, q.from) ? a.table[b * a.stride_table + e]
-                                                    : a.ids[ring(head + below + (e - q.first(a)))];
-          if (page >= 0) slot = ((long long)page << a.page_shift) + (pos & ((1 << a.page_shift) - 1));
-        });
+  // All items in one line, so that a thread has few to wait for one after the other: entries, pages given back, rows.
+  // (One copy of the search for the three of them: code that is read for the first time in a launch is waited for, too.
+  // Four adjacent rows for a thread and one search took 12.8 us where this took 8.9, 410000 rows of 256 sequences.)
+  const long long items = (long long)entries + gives + a.total;
+  for (long long item = (long long)wg * THREADS + tid; item < items; item += (long long)W * THREADS) {
+    const int kind = item < entries ? kEntries : item < (long long)entries + gives ? kGives : kRowsSum;
+    const int k = kind == kEntries ? (int)item : kind == kGives ? (int)(item - entries) : (int)(item - entries - gives);
+    int pos = -1, page = -1;
+    if (kind != kRowsSum || k < rows) {
+      // Whose item k is: the last thread with sums[kind][t] <= k, then its sequences.
+      int t = 0;
+#pragma unroll
+      for (int step = THREADS / 2; step; step /= 2) t += sums[kind][t + step] <= k ? step : 0;
+      int at = sums[kind][t], wanted = needs[t], below = 0, b = t * per;
+      Ask q;
+      Share s;
+      for (;; ++b) {   // (k is less than the sum over all: its sequence comes before the run ends)
+        q = ask(b);
+        below = wanted;
+        wanted = add(wanted, q.need);
+        s = Share(a, q, wanted, count);
+        const int n = kind == kEntries ? s.entries : kind == kGives ? s.give : s.rows;
+        if (k - at < n || b + 1 >= min(t * per + per, a.B)) break;
+        at += n;
+      }
+      const int i = k - at;
+      pos = q.from + i;
+      const int e = kind == kEntries ? s.e0 + i : kind == kGives ? s.g0 + i : pos >> a.page_shift;
+      int* entry = a.table + b * a.stride_table + e;
+      if (kind == kGives) {
+        page = *entry;
+        if (k < N - count) a.ids[ring(head + count + k)] = page;
+        *entry = -1;
+      } else if (kind == kEntries || a.slots) {   // (what the window leaves at once has no page)
+        page = e < q.keep ? -1 : e < Ask::have(a, q.from) ? *entry : a.ids[ring(head + below + (e - q.first(a)))];
+        if (kind == kEntries) *entry = page;
+      }
+    }
+    if (kind == kRowsSum) {
       if (a.positions) a.positions[k] = pos;
-      if (a.slots) a.slots[k] = slot;
+      if (a.slots) a.slots[k] = page < 0 ? -1 : ((long long)page << a.page_shift) + (pos & ((1 << a.page_shift) - 1));
     }
   }
-  if (a.cu && wg == 0) {
-    int at = rows[tid], wanted = needs[tid];
-    for (int b = b0; b < b1; ++b) {
-      const Ask q(a, b);
-      wanted = add(wanted, q.need);
-      a.cu[b] = at;
-      at = add(at, Share(a, q, wanted, count).rows);
-    }
-    if (tid == 0) a.cu[a.B] = rows[THREADS];
+  if (a.in_place) {
+    __syncthreads();   // all of the workgroup's reads are done
+    if (tid == 0) last = W == 1 || atomicInc(reinterpret_cast<unsigned*>(a.state + 3), W - 1) == (unsigned)W - 1;
+    __syncthreads();
   }
-  __syncthreads();   // all of the workgroup's reads are done
-  if (tid == 0) last = W == 1 || atomicInc(reinterpret_cast<unsigned*>(a.state + 3), W - 1) == (unsigned)W - 1;
-  __syncthreads();
-  if (!last) return;
-  int wanted = needs[tid];
+  if (a.in_place ? !last : wg != 0) return;
+  int wanted = needs[tid], at = sums[kRowsSum][tid];
   for (int b = b0; b < b1; ++b) {
-    const Ask q(a, b);
+    const Ask q = ask(b);
     wanted = add(wanted, q.need);
     const Share s(a, q, wanted, count);
+    if (a.cu) a.cu[b] = at;
+    at = add(at, s.rows);
     a.lens_out[b] = s.len;
     if (a.window > 0) a.first_held[b] = s.held;
   }
   if (tid == 0) {
+    if (a.cu) a.cu[a.B] = rows;
     a.state_out[0] = ring(head + taken);
-    a.state_out[1] = min(count - taken + min(gives[THREADS], N - count), N);
+    a.state_out[1] = count - taken + min(gives, N - count);
     a.state_out[2] = refused;
     a.state_out[3] = 0;
   }
@@ -204,13 +213,16 @@ __global__ __launch_bounds__(THREADS) void paged_reserve_kernel(ReserveArgs a) {
 
 }  // namespace
 
-hipError_t launch_paged_reserve(const ReserveArgs& a, hipStream_t stream) {
-  const bool many = a.B > 256;
-  const int threads = many ? 1024 : 256;
-  const long long items = std::max<long long>(a.positions || a.slots ? a.total : 0,
-                                              std::min<long long>((long long)a.B * a.max_pages, a.capacity) / 4);
-  const unsigned grid = (unsigned)std::min<long long>(256, std::max<long long>(1, items / (4 * threads)));
-  if (many) hipLaunchKernelGGL((paged_reserve_kernel<1024>), dim3(grid), dim3(1024), 0, stream, a);
+hipError_t launch_paged_reserve(ReserveArgs a, hipStream_t stream) {
+  if (!a.positions && !a.slots) a.total = 0;
+  a.in_place = a.lens_out == a.old_lens || a.state_out == a.state || a.window > 0;
+  // (How many entries change is not known here: a part of those that could.)  Workgroups that write the state in place count
+  // themselves one after the other, some 10 ns each: fewer and larger ones.
+  const long long items = a.total + std::min<long long>((long long)a.B * a.max_pages, a.capacity) / 8;
+  const bool large = a.B > 256 || (a.in_place && items > 32768);
+  const unsigned threads = large ? 1024 : 256;
+  const unsigned grid = (unsigned)std::min<long long>(a.in_place ? 128 : 512, std::max<long long>(1, items / threads));
+  if (large) hipLaunchKernelGGL((paged_reserve_kernel<1024>), dim3(grid), dim3(1024), 0, stream, a);
   else hipLaunchKernelGGL((paged_reserve_kernel<256>), dim3(grid), dim3(256), 0, stream, a);
   return hipGetLastError();
 }

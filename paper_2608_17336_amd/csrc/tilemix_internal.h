@@ -260,7 +260,8 @@ struct ReserveArgs {
   int* positions;          // [total] or nullptr
   long long* slots;        // [total] or nullptr
   int total;
+  int in_place;            // filled in by the launch: lengths or state are written over the old ones
 };
-hipError_t launch_paged_reserve(const ReserveArgs& args, hipStream_t stream);
+hipError_t launch_paged_reserve(ReserveArgs args, hipStream_t stream);
 
 }  // namespace tilemix
