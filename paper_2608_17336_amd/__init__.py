@@ -350,11 +350,21 @@ def _alloc(stream, *args, **kw):
     """torch.empty for a buffer the library uses on ``stream``: allocated while that stream is
     current, so that the caching allocator hands the block to no other stream's allocation
     before the work enqueued on ``stream`` is done with it."""
-    import torch
+    torch = _torch()
     if stream is None:
         return torch.empty(*args, **kw)
     with torch.cuda.stream(stream):
         return torch.empty(*args, **kw)
+
+
+def _alloc_like(stream, t, shape, dtype=None):
+    """_alloc of a dense tensor on t's device, of t's type unless another is given.  (A call is a few microseconds, and
+    these are the cheapest ways to a tensor.)"""
+    if stream is None:
+        if dtype is not None:
+            return t.new_empty(shape, dtype=dtype)
+        return _torch().empty_like(t) if t.shape == shape and t.is_contiguous() else t.new_empty(shape)
+    return _alloc(stream, shape, dtype=t.dtype if dtype is None else dtype, device=t.device)
 
 
 def tilemix_route_words_per_row(params: Params) -> int:
@@ -887,30 +897,35 @@ def _paged(cache: PagedCache, page_table, seqlens_k):
     if len(shape) != 4:
         raise ValueError(f"the pool's K must be [pages, Hk, page, d], got {tuple(shape)}")
     _require_like(V, dtype, shape, dev, "the pool's V")
-    sk, sv = _outer_stride(shape, K.stride(), 3, "the pool's K"), _outer_stride(shape, V.stride(), 3, "the pool's V")
-    sdk = sdv = pdk = pdv = 0
     P, Hk, page, d = shape
+    per = Hk * page
+    # (What is contiguous, as it mostly is, needs no look at its strides.)
+    sk = per * d if K.is_contiguous() else _outer_stride(shape, K.stride(), 3, "the pool's K")
+    sv = per * d if V.is_contiguous() else _outer_stride(shape, V.stride(), 3, "the pool's V")
+    sdk = sdv = pdk = pdv = 0
     if fmt >= 2:
         if fmt == 5:
             if d % 16:   # (where this is refused, the message speaks of d)
                 raise ValueError(f"head_dim {2 * d} not supported (64 or 128)")
             rows, of, inner = (P, Hk, page, d // 16), torch.float8_e8m0fnu, 3
+            per *= d // 16
             d *= 2
         else:
             rows, of, inner = shape[:3], torch.float32, 2
         _require_like(dK, of, rows, dev, "the pool's dK")
         _require_like(dV, of, rows, dev, "the pool's dV")
-        sdk, sdv = _outer_stride(rows, dK.stride(), inner, "the pool's dK"), _outer_stride(rows, dV.stride(), inner, "the pool's dV")
+        sdk = per if dK.is_contiguous() else _outer_stride(rows, dK.stride(), inner, "the pool's dK")
+        sdv = per if dV.is_contiguous() else _outer_stride(rows, dV.stride(), inner, "the pool's dV")
         pdk, pdv = dK.data_ptr(), dV.data_ptr()
     if getattr(page_table, "ndim", None) != 2:
         raise ValueError("page_table must be a tensor [B, max_pages]")
     t_shape = page_table.shape
     _require_like(page_table, torch.int32, t_shape, dev, "page_table")
-    B, per = t_shape
+    B, entries = t_shape
     _require_dense(seqlens_k, torch.int32, (B,), dev, "seqlens_k")
-    return _PAGED.pack(fmt, P, page, Hk, d, B, per, sk, sv, sdk, sdv,
-                       _outer_stride(t_shape, page_table.stride(), 1, "page_table"), K.data_ptr(), V.data_ptr(), pdk, pdv,
-                       page_table.data_ptr(), seqlens_k.data_ptr()), fmt, dev, B, Hk, d
+    return _PAGED.pack(fmt, P, page, Hk, d, B, entries, sk, sv, sdk, sdv,
+                       entries if page_table.is_contiguous() else _outer_stride(t_shape, page_table.stride(), 1, "page_table"),
+                       K.data_ptr(), V.data_ptr(), pdk, pdv, page_table.data_ptr(), seqlens_k.data_ptr()), fmt, dev, B, Hk, d
 
 
 def _int32(n: int, name: str) -> int:
@@ -932,6 +947,8 @@ def _paged_rows(cu_seqlens, max_len, total, device, B, Hk, d):
 
 def _row_stride(t, shape, name: str) -> int:
     """Elements between the token rows of t, [total, Hk, d] or [B, len, Hk, d]."""
+    if t.is_contiguous():
+        return shape[-2] * shape[-1]
     stride = t.stride()
     if len(shape) == 3:
         return _outer_stride(shape, stride, 2, name)
@@ -1022,11 +1039,11 @@ def tilemix_paged_gather(cache: PagedCache, page_table, seqlens_k, max_len: int,
                                         stream=stream)
     handle = _stream_on(stream, dev)
     if K is None:
-        K = _alloc(stream, shape, dtype=dtype, device=cache.K.device)
+        K = _alloc_like(stream, cache.K, shape, dtype)
     else:
         _require_dense(K, dtype, shape, dev, "K")
     if V is None:
-        V = _alloc(stream, shape, dtype=dtype, device=cache.K.device)
+        V = _alloc_like(stream, K, shape)
     else:
         _require_dense(V, dtype, shape, dev, "V")
     _check(load_library().tilemix_paged_gather(c, fmt, rows, max_len, total, K.data_ptr(), V.data_ptr(), handle))
@@ -1067,19 +1084,19 @@ def tilemix_paged_decode(cache: PagedCache, Q, page_table, seqlens_k, scale: flo
                                         return_lse=return_lse, workspace=workspace, stream=stream)
     handle, lib = _stream_on(stream, dev), load_library()
     if O is None:
-        O = _alloc(stream, shape, dtype=dtype, device=Q.device)
+        O = _alloc_like(stream, Q, shape)
     else:
         _require_dense(O, dtype, shape, dev, "O")
     if lse is not None:
         _require_dense(lse, torch.float32, (B, heads), dev, "lse")
     elif return_lse:
-        lse = _alloc(stream, (B, heads), dtype=torch.float32, device=Q.device)
+        lse = _alloc_like(stream, Q, (B, heads), torch.float32)
     if workspace is None:
         n = ctypes.c_size_t(0)
         _check(lib.tilemix_paged_decode_workspace_size(c, heads, ctypes.byref(n)))
         nbytes = n.value
         if nbytes:
-            workspace = _alloc(stream, nbytes, dtype=torch.uint8, device=Q.device)
+            workspace = _alloc_like(stream, Q, (nbytes,), torch.uint8)
     else:
         if not isinstance(workspace, torch.Tensor) or workspace.get_device() != dev or not workspace.is_contiguous():
             raise ValueError("workspace must be a contiguous tensor on the pool's device")
@@ -1111,14 +1128,6 @@ class Reserved(NamedTuple):
     cu_seqlens: object
     positions: object
     slots: object
-
-
-def _require_or_empty(t, shape, dtype, like, device, stream, name):
-    """t, a dense tensor of this type and shape, or a new one."""
-    if t is None:
-        return _alloc(stream, shape, dtype=dtype, device=like.device)
-    _require_dense(t, dtype, shape, device, name)
-    return t
 
 
 def tilemix_paged_reserve(pages: PageList, page_table, seqlens, wanted, page_size: int, *, window: int = 0,
@@ -1169,14 +1178,24 @@ def tilemix_paged_reserve(pages: PageList, page_table, seqlens, wanted, page_siz
         seqlens_out = seqlens
     else:
         _require_dense(seqlens_out, i32, (B,), dev, "seqlens_out")
-    cu_seqlens = _require_or_empty(cu_seqlens, (B + 1,), i32, ids, dev, stream, "cu_seqlens")
+    if cu_seqlens is None:
+        cu_seqlens = _alloc_like(stream, ids, (B + 1,))
+    else:
+        _require_dense(cu_seqlens, i32, (B + 1,), dev, "cu_seqlens")
     if total is not None:
         if total < 0:
             raise ValueError("total must be >= 0")
-        positions = _require_or_empty(positions, (total,), i32, ids, dev, stream, "positions")
-        slots = _require_or_empty(slots, (total,), torch.int64, ids, dev, stream, "slots")
+        if positions is None:
+            positions = _alloc_like(stream, ids, (total,))
+        else:
+            _require_dense(positions, i32, (total,), dev, "positions")
+        if slots is None:
+            slots = _alloc_like(stream, ids, (total,), torch.int64)
+        else:
+            _require_dense(slots, torch.int64, (total,), dev, "slots")
     _check(load_library().tilemix_paged_reserve(
-        page_size, B, shape[1], page_table.data_ptr(), _outer_stride(shape, page_table.stride(), 1, "page_table"), seqlens.data_ptr(),
+        page_size, B, shape[1], page_table.data_ptr(),
+        shape[1] if page_table.is_contiguous() else _outer_stride(shape, page_table.stride(), 1, "page_table"), seqlens.data_ptr(),
         wanted.data_ptr(), window, _ptr(first_held), ids.data_ptr(), ids.shape[0], state.data_ptr(), state_out.data_ptr(), seqlens_out.data_ptr(),
         cu_seqlens.data_ptr(), _ptr(positions), _ptr(slots), total or 0, handle))
     return Reserved(seqlens_out, cu_seqlens, positions, slots)
@@ -1265,14 +1284,14 @@ def tilemix_rotary(Q, K, inv_freq, positions=None, *, seqlens_k=None, cu_seqlens
                                   magnitude=magnitude, inverse=inverse, Q_out=Q_out, K_out=K_out, stream=stream)
     handle = _stream_on(stream, dev)
     if Q_out is None:
-        Q_out = _alloc(stream, shape, dtype=dtype, device=Q.device)
+        Q_out = _alloc_like(stream, Q, shape)
     else:
         _require_like(Q_out, dtype, shape, dev, "Q_out")
     k = ko = None
     ks = kos = 0
     if K is not None:
         if K_out is None:
-            K_out = _alloc(stream, k_shape, dtype=dtype, device=K.device)
+            K_out = _alloc_like(stream, K, k_shape)
         else:
             _require_like(K_out, dtype, k_shape, dev, "K_out")
         k, ks, ko, kos = K.data_ptr(), _row_stride(K, k_shape, "K"), K_out.data_ptr(), _row_stride(K_out, k_shape, "K_out")
