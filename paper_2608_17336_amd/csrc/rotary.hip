@@ -17,7 +17,12 @@ namespace tilemix {
 namespace {
 
 constexpr int kRotaryThreads = 256;
-constexpr int kRowsAhead = 4;        // heads that a lane requests at a time
+// Heads that a lane requests at a time.  (us at 1, 2, 4 and 8: 196 million BF16 elements, half of each head turned, 146, 146,
+// 153 and 163; 4 x 8192 tokens of 64/8 heads, d = 128, 212, 207, 222 and 241.)
+constexpr int kRowsAhead = 2;
+// Results of this many bytes and more, and their inputs, pass the caches by, which cannot hold them for their reader: the
+// same two 146 and 129, 207 and 189.  (Not fewer: 60000 tokens of 8/8 heads, d = 64, 123 MB, 42.7 and 50.7.)
+constexpr long long kStreamBytes = 128 << 20;
 constexpr int kMaxTokens = 8;        // of a workgroup
 
 // cos and sin of `turns` whole turns.  |a| <= pi / 4: the first terms left out are below 2^-32.
@@ -69,11 +74,11 @@ template <int V>
 struct Vec;
 template <>
 struct Vec<8> {
-  typedef uint4 t;
+  typedef uint32_t t __attribute__((ext_vector_type(4)));
 };
 template <>
 struct Vec<4> {
-  typedef uint2 t;
+  typedef uint32_t t __attribute__((ext_vector_type(2)));
 };
 template <>
 struct Vec<2> {
@@ -105,7 +110,18 @@ __device__ __forceinline__ typename Vec<V>::t pack(const float (&x)[V]) {
 // A head of d channels is d / (2 V) units of two vectors of V channels: where pairs are r / 2 apart, the two halves of V
 // pairs, then two adjacent vectors behind r; else two vectors d / 2 apart, each of V / 2 pairs or behind r.  A lane
 // takes one unit of every step-th head of one token.
-template <int TYPE, bool HALF, int V>
+template <bool STREAM, typename T>
+__device__ __forceinline__ T load(const uint16_t* p) {
+  if constexpr (STREAM) return __builtin_nontemporal_load(reinterpret_cast<const T*>(p));
+  return *reinterpret_cast<const T*>(p);
+}
+template <bool STREAM, typename T>
+__device__ __forceinline__ void store(uint16_t* p, T x) {
+  if constexpr (STREAM) __builtin_nontemporal_store(x, reinterpret_cast<T*>(p));
+  else *reinterpret_cast<T*>(p) = x;
+}
+
+template <int TYPE, bool HALF, int V, bool STREAM>
 __global__ __launch_bounds__(kRotaryThreads) void rotary_kernel(RotaryArgs a) {
   typedef typename Vec<V>::t Vt;
   __shared__ float2 turn[kMaxTokens * 64];
@@ -171,7 +187,7 @@ __global__ __launch_bounds__(kRotaryThreads) void rotary_kernel(RotaryArgs a) {
         const uint16_t* p = from(h + k * step);
 #pragma unroll
         for (int j = 0; j < 2; ++j)
-          if (moves[j]) v[k][j] = *reinterpret_cast<const Vt*>(p + c[j]);
+          if (moves[j]) v[k][j] = load<STREAM, Vt>(p + c[j]);
       }
 #pragma unroll
     for (int k = 0; k < kRowsAhead; ++k) {
@@ -198,7 +214,7 @@ __global__ __launch_bounds__(kRotaryThreads) void rotary_kernel(RotaryArgs a) {
       }
 #pragma unroll
       for (int j = 0; j < 2; ++j)   // (what does not turn is moved as it is, whatever it holds)
-        if (moves[j]) *reinterpret_cast<Vt*>(p + c[j]) = turns[j] ? pack<TYPE, V>(y[j]) : v[k][j];
+        if (moves[j]) store<STREAM, Vt>(p + c[j], turns[j] ? pack<TYPE, V>(y[j]) : v[k][j]);
     }
   }
 }
@@ -220,7 +236,10 @@ hipError_t launch_rotary(RotaryArgs a, int type, bool half, hipStream_t stream) 
   a.div_pairs = FastDiv((uint32_t)(a.r / 2));
   const dim3 grid((unsigned)(((long long)a.total + (1 << a.token_shift) - 1) >> a.token_shift));
   auto go = [&](auto T, auto H, auto V) {
-    hipLaunchKernelGGL((rotary_kernel<T(), H(), V()>), grid, dim3(kRotaryThreads), 0, stream, a);
+    if (V() == 8 && 2LL * a.total * heads * a.d >= kStreamBytes)
+      hipLaunchKernelGGL((rotary_kernel<T(), H(), V(), V() == 8>), grid, dim3(kRotaryThreads), 0, stream, a);
+    else
+      hipLaunchKernelGGL((rotary_kernel<T(), H(), V(), false>), grid, dim3(kRotaryThreads), 0, stream, a);
     return hipGetLastError();
   };
   using std::integral_constant;
