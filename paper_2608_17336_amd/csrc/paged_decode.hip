@@ -939,7 +939,14 @@ PagedDecodePlan plan_paged_decode(const PagedPool& p, int heads_q, int d, int fo
   // The same limits for the others: FP16 8 of 1000 14.7 and 13.8, 24 of 1000 19.5 and 23.5, 16 of 1500 23.4 and 23.2, 32 of
   // 2000 42.8 and 47.8, 24 of 4000 69.5 and 66.7 (but 128 of 1 to 1000 68.0 and 58.3); INT8, d = 64 24 of 1000 12.8 and
   // 13.8, 16 of 1500 16.4 and 14.0, 32 of 2000 20.0 and 20.6, 24 of 4000 35.2 and 27.0.
-  const long long limit = segments < kCUs / 2 ? 16 : segments < kCUs * 3 / 4 || segments > resident ? 32 : 64;
+  // MXFP4's tiles, of 64 keys, us on the GPU (what a call takes is at the host's 11 us without the second launch and 15
+  // with it): 1 sequence of 500 keys 9.5 and 10.6, of 1000 13.0 and 10.6; 16 of 1000 13.4 and 12.6, of 1900 21.7 and 17.2;
+  // 24 of 1000 13.5 and 14.4, of 1900 22.0 and 20.4; 32 of 1900 22.5 and 23.6, of 4000 37.3 and 33.8; 64 of 1900 30.7 and
+  // 33.1, of 4000 55.3 and 59.5; 128 of 2000 62.0 and 64.1.
+  const bool mx = is_4bit(format);
+  const long long limit = segments < kCUs / 2 ? 16
+                        : segments < kCUs * 3 / 4 ? (mx ? 16 : 32)
+                        : segments > resident || (mx && segments < kCUs * 3 / 2) ? 32 : 64;
   pl.whole = most <= limit ? (int)most : 0;
   pl.workgroups = std::min<long long>(resident,
                                       pl.whole ? segments : (segments * most + kPagedWaves - 1) / kPagedWaves);
