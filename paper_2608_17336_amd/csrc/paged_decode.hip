@@ -256,10 +256,27 @@ __device__ __forceinline__ float quad_rows_sum(float x) {
   return pair_sum(__builtin_bit_cast(float, (int)r[0]) + __builtin_bit_cast(float, (int)r[1]));
 }
 
+// The scale operand of the conversions of byte b of w.  They take its exponent field and leave the other bits alone, so
+// a rotation by 8 b + 9 to the right is enough.
+__device__ __forceinline__ float exponent_scale(uint32_t w, int b) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_alignbit(w, w, 8 * b + 9));
+}
+
+// The lanes' x as CTRL moves them; every lane has a source.
+template <int CTRL>
+__device__ __forceinline__ int dpp_all(int x) {
+  return __builtin_amdgcn_update_dpp(0, x, CTRL, 0xf, 0xf, true);
+}
+
+// x of the lane that holds the other piece of the same head (PAIRED): lane ^ 8.
+__device__ __forceinline__ float other_piece(float x) {
+  return __builtin_bit_cast(float, dpp_all<0x128>(__builtin_bit_cast(int, x)));
+}
+
 // x of lane L of the four lanes that agree in lane / 4.
 template <int L>
 __device__ __forceinline__ uint32_t quad_lane(uint32_t x) {
-  return (uint32_t)dpp<L * 0x55>((int)x, (int)x);
+  return (uint32_t)dpp_all<L * 0x55>((int)x);
 }
 
 // p = 2^(s - m) is taken against the running max m, and so is the normalizer z = sum p.  The weights of the codes
@@ -288,6 +305,13 @@ __device__ __forceinline__ void split2(float w0, float w1, uint32_t& hi, uint32_
   lo = __builtin_bit_cast(uint32_t, l);
 }
 
+// One BF16 piece of two weights (see split2): the first, or else the second.
+__device__ __forceinline__ uint32_t own_piece(float w0, float w1, bool first) {
+  const uint32_t h = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{w0, w1}), bf16x2)) & (first ? 0u : ~0u);
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{w0 - __builtin_bit_cast(float, h << 16),
+                                                                     w1 - __builtin_bit_cast(float, h & 0xffff0000u)}), bf16x2));
+}
+
 // Scores are computed transposed, S^T = K Q^T: a slab's 16 keys on the rows, the query heads on the columns
 // of a 16x16 product, so that lane (l16, lq) = (lane % 16, lane / 16) receives keys 4 lq + r (r < 4) of
 // head l16.  For the pair of slabs 2 t, 2 t + 1 these are the eight keys that the B operand of
@@ -302,7 +326,14 @@ struct DecodeShared {
   __align__(16) float o[kPagedWaves][kPagedHeads][D + 4];   // padded rows
 };
 
-template <int D, int TYPE, int FORMAT, bool STREAM>
+// Two variants of MXFP4 (an MXFP4 tile has as many bytes as the others' and twice the work, and what bounds it beside the
+// memory is how many instructions a wave issues: one in some 8 cycles, scalar ones too):
+// PAIRED: KV heads of up to 8 query heads.  Half of the 16 columns would be padding: columns h and h + 8 both belong to head
+// h and carry the two pieces of its weights, and of an FP16 query, which add up to the scores of both.  Half of the
+// products of O^T += V^T P^T are spared.
+// ONE_PAGE: pages hold whole tiles, so that a tile's rows lie one behind the other.  The addresses of four slabs are 200 of 780
+// instructions of a tile: 8 x 65536 keys (FP16, BF16 queries) 111 and 109 us without, 106 and 103 with it.
+template <int D, int TYPE, int FORMAT, bool STREAM, bool PAIRED, bool ONE_PAGE>
 __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run<16 * tile_slabs(FORMAT)>& run, DecodeShared<D>& shared) {
   constexpr int kS = tile_slabs(FORMAT), kKeys = 16 * kS;
   typedef Span<kKeys> Span;
@@ -314,11 +345,11 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run<1
   constexpr int kC = D / 16;                       // channels of a lane's value row: output products
   constexpr int kVW = k4 ? 1 : kC * kBytes / 4;    // dwords of them
   constexpr int kQ = D / 32;                       // score products per slab
-  constexpr bool kRelative = k4 && TYPE == TILEMIX_FP16;   // keys relative to the largest exponent of their tile (see 4.)
+  constexpr bool kRelative = k4 && TYPE == TILEMIX_FP16 && !PAIRED;   // keys relative to the largest exponent of their tile (see 4.)
   const PagedPool& p = a.pool;
   const int tid = threadIdx.x, lane = tid & (kWave - 1);
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-  const int l16 = lane & 15, lq = lane >> 4;
+  const int l16 = lane & 15, lq = lane >> 4, column = PAIRED ? l16 & 7 : l16;   // column: query head of the block
   const float ninf = -__builtin_huge_valf();
   auto& red_m = shared.m;
   auto& red_z = shared.z;
@@ -356,26 +387,35 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run<1
   uint4 kr[kS][kKL];
   uint32_t vr[kS][4][kVW];
   f32x4 dk[kS], dv[kS];
-  uint32_t ek[kS], ev[kS];                         // MXFP4: exponents of the lane's channels of key l16; of key 4 lq + l16 % 4
-  int page[kS];                                    // per slab, of the tile that was requested last
+  // MXFP4: words with the exponents of key l16 and of key 4 lq + l16 % 4 (d = 64: of two keys).  All rows and exponents are loaded as
+  // whole words: of a narrower one the compiler clears the upper bits as soon as it is loaded, and waits for it there.
+  uint32_t ek[kS], ev[kS];
+  const int key_byte = kScaleRow == 4 ? lq : 2 * (l16 & 1) + (lq >> 1);   // of the lane's channels in ek
+  constexpr int kPages = ONE_PAGE ? 1 : kS;
+  int page[kPages];                                // per slab, of the tile that was requested last
   const char* poolK = static_cast<const char*>(p.K);
   const char* poolV = static_cast<const char*>(p.V);
-  const uint32_t k_lane = l16 * kRow + (k4 ? kRow / 4 : 16) * lq, v_lane = 4 * lq * kRow + l16 * (kRow / 16);
+  const uint32_t k_lane = l16 * kRow + (k4 ? kRow / 4 : 16) * lq, v_lane = 4 * lq * kRow + (k4 ? l16 * (kRow / 16) & ~3 : l16 * (kRow / 16));
   auto find_pages = [&](int ids, int i) {
     const int at = (i & (id_tiles - 1)) << per_shift;
 #pragma unroll
-    for (int s = 0; s < kS; ++s) {
+    for (int s = 0; s < kPages; ++s) {
       const int id = __builtin_amdgcn_readlane(ids, at + (16 * s >> p.page_shift));
       page[s] = id < p.pages ? id : -1;
     }
   };
-  // Row of slab s of tile n in its page, or in page 0 where there is none: it is masked.
+  // Row of slab s of tile n in its page, or in page 0 where there is none: it is masked.  slab_at: bytes from the pool's start,
+  // of rows of row_bytes and pages `stride` elements of `elem` bytes apart.
   auto slab_row = [&](int hk, int n, int s) { return (hk << p.page_shift) + ((n * kKeys + 16 * s) & ((1 << p.page_shift) - 1)); };
+  auto slab_at = [&](int hk, int n, int s, long long stride, int elem, int row_bytes) {
+    const int from = ONE_PAGE ? 0 : s;
+    return elem * (max(page[from], 0) * stride) + (long long)slab_row(hk, n, from) * row_bytes + (s - from) * 16 * row_bytes;
+  };
   auto load_keys = [&](int hk, int n, bool some) {
     const uint32_t k_off = some ? k_lane : 0u, s_off = some ? 16u * lq : 0u;
 #pragma unroll
     for (int s = 0; s < kS; ++s) {
-      const char* base = poolK + kBytes * (max(page[s], 0) * p.stride_k + (long long)slab_row(hk, n, s) * (kRow / kBytes));
+      const char* base = poolK + slab_at(hk, n, s, p.stride_k, kBytes, kRow);
       if constexpr (k4 && D == 64) {
         const u32x2 x = load_row<STREAM, u32x2>(base + k_off);
         kr[s][0] = make_uint4(x[0], x[1], 0, 0);
@@ -387,13 +427,13 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run<1
     if constexpr (k8) {
 #pragma unroll
       for (int s = 0; s < kS; ++s)
-        dk[s] = *reinterpret_cast<const f32x4*>(static_cast<const char*>(p.dK) + 4 * (max(page[s], 0) * p.stride_dk + slab_row(hk, n, s)) + s_off);
+        dk[s] = *reinterpret_cast<const f32x4*>(static_cast<const char*>(p.dK) + slab_at(hk, n, s, p.stride_dk, 4, 4) + s_off);
     }
     if constexpr (k4) {
 #pragma unroll
       for (int s = 0; s < kS; ++s)
-        ek[s] = *reinterpret_cast<const uint8_t*>(static_cast<const char*>(p.dK) + max(page[s], 0) * p.stride_dk +
-                                                  (long long)slab_row(hk, n, s) * kScaleRow + (some ? l16 * kScaleRow + lq * kScaleRow / 4 : 0));
+        ek[s] = *reinterpret_cast<const uint32_t*>(static_cast<const char*>(p.dK) + slab_at(hk, n, s, p.stride_dk, 1, kScaleRow) +
+                                                   (some ? l16 * kScaleRow & ~3u : 0u));
     }
   };
   auto load_values = [&](int hk, int n, bool some) {
@@ -401,26 +441,22 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run<1
     if constexpr (k8) {
 #pragma unroll
       for (int s = 0; s < kS; ++s)
-        dv[s] = *reinterpret_cast<const f32x4*>(static_cast<const char*>(p.dV) + 4 * (max(page[s], 0) * p.stride_dv + slab_row(hk, n, s)) + s_off);
+        dv[s] = *reinterpret_cast<const f32x4*>(static_cast<const char*>(p.dV) + slab_at(hk, n, s, p.stride_dv, 4, 4) + s_off);
     }
     if constexpr (k4) {
 #pragma unroll
       for (int s = 0; s < kS; ++s) {
-        const char* at = static_cast<const char*>(p.dV) + max(page[s], 0) * p.stride_dv + (long long)slab_row(hk, n, s) * kScaleRow +
-                         (some ? kScaleRow * (4 * lq + l16 % 4) : 0);
-        if constexpr (kScaleRow == 4) ev[s] = *reinterpret_cast<const uint32_t*>(at);
-        else ev[s] = *reinterpret_cast<const uint16_t*>(at);
+        ev[s] = *reinterpret_cast<const uint32_t*>(static_cast<const char*>(p.dV) + slab_at(hk, n, s, p.stride_dv, 1, kScaleRow) +
+                                                   (some ? kScaleRow * (4 * lq + l16 % 4) & ~3u : 0u));
       }
     }
 #pragma unroll
     for (int s = 0; s < kS; ++s) {
-      const char* base = poolV + kBytes * (max(page[s], 0) * p.stride_v + (long long)slab_row(hk, n, s) * (kRow / kBytes));
+      const char* base = poolV + slab_at(hk, n, s, p.stride_v, kBytes, kRow);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const char* at = base + r * kRow + v_off;
-        if constexpr (k4 && D == 64) {
-          vr[s][r][0] = load_row<STREAM, uint16_t>(at);
-        } else if constexpr (kVW == 4) {
+        if constexpr (kVW == 4) {
           const u32x4 x = load_row<STREAM, u32x4>(at);
           vr[s][r][0] = x[0]; vr[s][r][1] = x[1]; vr[s][r][2] = x[2]; vr[s][r][3] = x[3];
         } else if constexpr (kVW == 2) {
@@ -435,7 +471,7 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run<1
   uint4 qf[kQ];
   auto load_query = [&](const Part& q) {
     const int G = a.group, heads = min(kPagedHeads, G - q.g0);
-    const char* row = static_cast<const char*>(a.Q) + 2 * (q.b * a.q_stride + (long long)(q.hk * G + q.g0 + min(l16, heads - 1)) * D);
+    const char* row = static_cast<const char*>(a.Q) + 2 * (q.b * a.q_stride + (long long)(q.hk * G + q.g0 + min(column, heads - 1)) * D);
 #pragma unroll
     for (int i = 0; i < kQ; ++i) qf[i] = ld_global_16(row + 2 * (k4 ? D / 4 * lq + 8 * i : k8 ? 64 * (i / 2) + 16 * lq + 8 * (i % 2) : 32 * i + 8 * lq));
   };
@@ -473,7 +509,7 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run<1
     //    f_head is then no subnormal number (for scales of 2^-17 and more).
     float f_head = a.scale_log2e;   // score of a product, in log2 units, before the key's scale
     {
-      const uint32_t some = l16 < heads ? ~0u : 0u;
+      const uint32_t some = column < heads ? ~0u : 0u;
   #pragma unroll
       for (int i = 0; i < kQ; ++i) qf[i] = make_uint4(qf[i].x & some, qf[i].y & some, qf[i].z & some, qf[i].w & some);
       if constexpr (k8 && TYPE == TILEMIX_BF16) {
@@ -497,6 +533,18 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run<1
           qf[i] = make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
         }
       }
+      if constexpr (PAIRED && TYPE == TILEMIX_FP16) {   // FP16's 11 bits are two BF16 numbers of 8 and 3
+  #pragma unroll
+        for (int i = 0; i < kQ; ++i) {
+          const uint32_t w[4] = {qf[i].x, qf[i].y, qf[i].z, qf[i].w};
+          uint32_t h[4];
+  #pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            h[e] = own_piece(bits_to_float<TILEMIX_FP16>(w[e] & 0xffffu), bits_to_float<TILEMIX_FP16>(w[e] >> 16), l16 < 8);
+          }
+          qf[i] = make_uint4(h[0], h[1], h[2], h[3]);
+        }
+      }
     }
 
     // 4. The wave's tiles.  m: running max (log2 units); x: the weights' power of two; z: this lane's share of the
@@ -513,9 +561,9 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run<1
     while (n < cur.end) {
       // Which of the tile's keys count, where it is not all of them.
       bool all = n * kKeys >= cur.span.first && (n + 1) * kKeys <= cur.span.len;
-      uint32_t has = 0;
+      uint32_t has = ONE_PAGE && page[0] >= 0 ? (1u << kS) - 1 : 0u;
   #pragma unroll
-      for (int s = 0; s < kS; ++s) has |= page[s] >= 0 ? 1u << s : 0u;
+      for (int s = 0; s < (ONE_PAGE ? 0 : kS); ++s) has |= page[s] >= 0 ? 1u << s : 0u;
       all = all && has == (1u << kS) - 1;
       // FP16 queries take MXFP4 keys in FP16: code 2^(e - top), top the largest exponent of a key that counts, so that
       // what FP16 cannot hold lies below 2^-25 of the tile's largest key.  (As two BF16 pieces, which lose nothing, they took
@@ -530,6 +578,8 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run<1
             ek[s] = (has >> s & 1) && t >= cur.span.first && t < cur.span.len ? ek[s] : 0u;
           }
         }
+  #pragma unroll
+        for (int s = 0; s < kS; ++s) ek[s] = ek[s] >> 8 * key_byte & 0xffu;
         uint32_t e = ek[0];
   #pragma unroll
         for (int s = 1; s < kS; ++s) e = max(e, ek[s]);
@@ -541,7 +591,7 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run<1
       for (int s = 0; s < kS; ++s) {
         f32x4 c = {0.0f, 0.0f, 0.0f, 0.0f};
         if constexpr (k4) {
-          const float scale = kRelative ? block_scale(max(ek[s] + 127, top) - top) : block_scale(ek[s]);
+          const float scale = kRelative ? block_scale(max(ek[s] + 127, top) - top) : exponent_scale(ek[s], key_byte);
           const uint32_t w[4] = {kr[s][0].x, kr[s][0].y, kr[s][0].z, kr[s][0].w};
   #pragma unroll
           for (int k = 0; k < kQ; ++k) {
@@ -557,6 +607,10 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run<1
           } else {
             c = mfma_16<FORMAT>(kr[s][k], qf[k], c);
           }
+        }
+        if constexpr (PAIRED && TYPE == TILEMIX_FP16) {
+  #pragma unroll
+          for (int r = 0; r < 4; ++r) c[r] += other_piece(c[r]);
         }
         // Scores are scaled and rounded before the max and the exponent see them.
   #pragma unroll
@@ -589,7 +643,7 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run<1
             sc[s][r] = ok ? sc[s][r] : ninf;
             if constexpr (k8) dv[s][r] = ok ? dv[s][r] : 0.0f;
             // What a slot behind the sequence holds may be a NaN, which a weight of 0 does not cancel.
-            if constexpr (k4) {
+            if constexpr (k4) {   // (d = 64: the other key of the word has its own lane)
               if (l16 % 4 == r) ev[s] = ok ? ev[s] : 0u;
             } else if constexpr (FORMAT != TILEMIX_INT8) {
   #pragma unroll
@@ -640,26 +694,39 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run<1
           if constexpr (k8) w[r] *= __builtin_amdgcn_ldexpf(dv[s][r], -x);
           else if constexpr (FORMAT == TILEMIX_FP16) w[r] *= 0x1p15f;
         }
-        split2<FORMAT>(w[0], w[1], hi[u].x, lo[u].x);
-        split2<FORMAT>(w[2], w[3], hi[u].y, lo[u].y);
+        if constexpr (PAIRED) {
+          hi[u].x = own_piece(w[0], w[1], l16 < 8);
+          hi[u].y = own_piece(w[2], w[3], l16 < 8);
+        } else {
+          split2<FORMAT>(w[0], w[1], hi[u].x, lo[u].x);
+          split2<FORMAT>(w[2], w[3], hi[u].y, lo[u].y);
+        }
       }
       const uint4 ph = make_uint4(hi[0].x, hi[0].y, hi[1].x, hi[1].y), pl = make_uint4(lo[0].x, lo[0].y, lo[1].x, lo[1].y);
       auto row = [&](int j) -> const uint32_t (&)[kVW] { return vr[t + j / 4][j % 4]; };   // of the lane's key j < 8
       auto add = [&](int c, const uint32_t (&v)[4]) {
         const uint4 va = make_uint4(v[0], v[1], v[2], v[3]);
         acc[c] = mfma_16<FORMAT>(va, ph, acc[c]);
-        acc[c] = mfma_16<FORMAT>(va, pl, acc[c]);
+        if constexpr (!PAIRED) acc[c] = mfma_16<FORMAT>(va, pl, acc[c]);
       };
       if constexpr (k4) {
         // Two channels of a key in a byte: widened, with the key's scale of the lane's channels, then paired.
-        // (The conversion takes a scale's exponent field and leaves the other bits alone.  Byte b is brought there by a
-        // rotation to the right by 8 b + 9.)
         float ve[8];
   #pragma unroll
         for (int u = 0; u < 2; ++u) {
           const uint32_t w[4] = {quad_lane<0>(ev[t + u]), quad_lane<1>(ev[t + u]), quad_lane<2>(ev[t + u]), quad_lane<3>(ev[t + u])};
   #pragma unroll
-          for (int r = 0; r < 4; ++r) ve[4 * u + r] = __builtin_bit_cast(float, __builtin_amdgcn_alignbit(w[r], w[r], 8 * (l16 * kC / 32) + 9));
+          for (int r = 0; r < 4; ++r) ve[4 * u + r] = exponent_scale(w[r], l16 * kC / 32 + (kScaleRow == 2 ? 2 * (r & 1) : 0));
+        }
+        // d = 64: a lane's two bytes are one half of its word, and those of two keys are brought into one.
+        uint32_t codes[8];
+        if constexpr (D == 64) {
+          const uint32_t pick = l16 & 1 ? 0x07060302u : 0x05040100u;
+  #pragma unroll
+          for (int j = 0; j < 4; ++j) codes[j] = __builtin_amdgcn_perm(row(2 * j + 1)[0], row(2 * j)[0], pick);
+        } else {
+  #pragma unroll
+          for (int j = 0; j < 8; ++j) codes[j] = row(j)[0];
         }
   #pragma unroll
         for (int c = 0; c < kC; c += 2) {
@@ -669,10 +736,11 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run<1
             uint32_t x[2];
   #pragma unroll
             for (int u = 0; u < 2; ++u) {
-              const uint32_t w = row(2 * j + u)[0];
+              const uint32_t w = D == 64 ? codes[j] : codes[2 * j + u];
+              const int byte = D == 64 ? c / 2 + 2 * u : c / 2;
               const float scale = ve[2 * j + u];
-              x[u] = c == 0 ? mx_values<TILEMIX_BF16, 0>(w, scale) : c == 2 ? mx_values<TILEMIX_BF16, 1>(w, scale)
-                   : c == 4 ? mx_values<TILEMIX_BF16, 2>(w, scale) : mx_values<TILEMIX_BF16, 3>(w, scale);
+              x[u] = byte == 0 ? mx_values<TILEMIX_BF16, 0>(w, scale) : byte == 1 ? mx_values<TILEMIX_BF16, 1>(w, scale)
+                   : byte == 2 ? mx_values<TILEMIX_BF16, 2>(w, scale) : mx_values<TILEMIX_BF16, 3>(w, scale);
             }
             v[0][j] = __builtin_amdgcn_perm(x[1], x[0], 0x05040100u);
             v[1][j] = __builtin_amdgcn_perm(x[1], x[0], 0x07060302u);
@@ -759,6 +827,7 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run<1
   #pragma unroll
       for (int w = 0; w < kPagedWaves; ++w) {
         sum += *reinterpret_cast<const f32x4*>(&osum[w][g][c]);
+        if constexpr (PAIRED) sum += *reinterpret_cast<const f32x4*>(&osum[w][g + 8][c]);
         zz += red_z[w][g];
       }
       if (whole) {
@@ -801,7 +870,7 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run<1
   }
 }
 
-template <int D, int TYPE, int FORMAT>
+template <int D, int TYPE, int FORMAT, bool PAIRED, bool ONE_PAGE>
 __global__ __launch_bounds__(kPagedWaves * kWave) __attribute__((amdgpu_waves_per_eu(resident_per_cu(D))))
 void paged_decode_kernel(PagedDecodeArgs a) {
   __shared__ DecodeShared<D> shared;
@@ -809,8 +878,8 @@ void paged_decode_kernel(PagedDecodeArgs a) {
   const Run<kKeys> run(a, blockIdx.x, threadIdx.x & (kWave - 1));
   // (Two copies of the body: a branch at each request would make the waits count loads that were not issued.)
   const long long bytes = (long long)__builtin_amdgcn_readfirstlane(run.total) * (kKeys * 2 * kRowBytes<D, FORMAT>);
-  if (bytes >= kStreamBytes && a.head_blocks == a.pool.Hk) decode_run<D, TYPE, FORMAT, true>(a, run, shared);
-  else decode_run<D, TYPE, FORMAT, false>(a, run, shared);
+  if (bytes >= kStreamBytes && a.head_blocks == a.pool.Hk) decode_run<D, TYPE, FORMAT, true, PAIRED, ONE_PAGE>(a, run, shared);
+  else decode_run<D, TYPE, FORMAT, false, PAIRED, ONE_PAGE>(a, run, shared);
 }
 
 // op over the lanes that agree in lane % LANES (8, 16 or 32).
@@ -959,7 +1028,19 @@ hipError_t launch_paged_decode(PagedDecodeArgs a, const PagedDecodePlan& pl, int
   a.div_blocks = FastDiv(pl.head_blocks / a.pool.Hk);
   a.div_workgroups = FastDiv((uint32_t)pl.workgroups);
   return for_paged_types(d, type, format, [&](auto D, auto T, auto F) {
-    hipLaunchKernelGGL((paged_decode_kernel<D(), T(), F()>), dim3((unsigned)pl.workgroups), dim3(kPagedWaves * kWave), 0, stream, a);
+    const dim3 workgroups((unsigned)pl.workgroups), threads(kPagedWaves * kWave);
+    auto go = [&](auto PAIRED, auto ONE_PAGE) {
+      hipLaunchKernelGGL((paged_decode_kernel<D(), T(), F(), PAIRED(), ONE_PAGE()>), workgroups, threads, 0, stream, a);
+    };
+    if constexpr (is_4bit(F())) {
+      const bool paired = a.group <= 8, one_page = 1 << a.pool.page_shift >= 16 * tile_slabs(F());
+      if (paired && one_page) go(std::true_type{}, std::true_type{});
+      else if (paired) go(std::true_type{}, std::false_type{});
+      else if (one_page) go(std::false_type{}, std::true_type{});
+      else go(std::false_type{}, std::false_type{});
+    } else {
+      go(std::false_type{}, std::false_type{});
+    }
     if (pl.whole) return hipGetLastError();
     // All channels in a workgroup where there are many, most of them with nothing to join; 32 of them, and so more parts
     // at a time, where there are few or a sequence may have many rows (one has at most as many as there are
