@@ -512,7 +512,7 @@ tilemix_status tilemix_paged_decode(const tilemix_paged_cache* cache, int32_t ty
  *   free_state   device int32 [4]: head, count, the sequences refused by the last call (written), and
  *                a number that is 0 between calls
  *   free_state_out  device int32 [4], the new state, written; may be free_state
- *   seqlens_out  device int32 [batch], the new lengths (refused: the old), written; may be seqlens
+ *   seqlens_out  device int32 [batch], the new lengths (refused: the old), written; may be seqlens or wanted
  *   cu_seqlens   device int32 [batch + 1] or NULL: prefix sums of the new tokens (those of refused and
  *                shortened sequences are 0), as the other calls take them; they stop at 2^30 - 1
  *   positions    device int32 [total] or NULL: token number of each new row, in the order of

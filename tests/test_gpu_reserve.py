@@ -209,6 +209,28 @@ def test_captured_in_a_graph(window):
         s.check(got, new, total)
 
 
+@pytest.mark.parametrize("B,rows", [(3, 40), (200, 2000), (1500, 300)])
+def test_lengths_written_over_the_wanted_ones(B, rows):
+    """seqlens_out may be `wanted`, which all workgroups read, and seqlens itself may be what is wanted."""
+    tm = _tm()
+    rng = random.Random(B)
+    for _ in range(3):
+        old, want = [rng.randrange(rows) for _ in range(B)], [rng.randrange(2 * rows) for _ in range(B)]
+        per, P = -(-2 * rows // 16), B * (2 * rows // 16 + 2)
+        s = Server(B, per, 16, P, seed=1)
+        s.step(old)
+        w = _gpu(want)
+        state = torch.empty(4, dtype=I32, device="cuda")
+        total = sum(max(0, n - o) for o, n in zip(old, want))
+        got = tm.tilemix_paged_reserve(s.list, s.t, s.l, w, 16, total=total, state_out=state, seqlens_out=w)
+        torch.cuda.synchronize()
+        assert got.seqlens is w and s.l.tolist() == old
+        s.list, s.l = tm.PageList(s.list.ids, state), w
+        s.check(got, want, total)
+        got = tm.tilemix_paged_reserve(s.list, s.t, s.l, s.l, 16, total=5)
+        s.check(got, want, 5)
+
+
 def test_binding_refusals():
     tm = _tm()
     s = Server(2, 3, 16, 4)
