@@ -62,7 +62,7 @@ def _read(pool, op, page, slot, dtype):
 def _same(a, b):
     """Bit for bit; a NaN has any payload."""
     nan = torch.isnan(a) & torch.isnan(b)
-    return bool(((_bits(a) == _bits(b)) | nan).all())
+    return bool(((_bits(a) == _bits(b)) | nan.cpu()).all())
 
 
 # ------------------------------------------------------------------------- append and gather
@@ -338,6 +338,55 @@ def test_decode_many_sequences(dtype, Hq, Hk, d, long):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("Hq,Hk,d,page,long", [(6, 2, 128, 64, 1500), (128, 16, 64, 64, 1500), (96, 2, 128, 128, 1100), (40, 2, 64, 256, 2600)])
+def test_decode_many_sequences_in_large_pages(dtype, Hq, Hk, d, page, long):
+    """The same where a page holds whole tiles, with up to 8 query heads for a KV head and more."""
+    lens = [(0, 3, 37, 150, 1, 64, 65, 200)[b * b % 8] for b in range(150)]
+    lens[7] = lens[130] = long
+    lens[149] = 0
+    _decode_case(dtype, Hq, Hk, d, page, lens, seed=1550)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("Hq,Hk", [(8, 1), (9, 1)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_decode_of_slices(dtype, Hq, Hk, d):
+    """Pages of K and V that are slices of one tensor, and strided queries."""
+    tm = _tm()
+    for page in (16, 64):
+        pool = _cached_pool((12, Hk, page, d), 1560)
+        want = tm.tilemix_paged_decode(_on_gpu(pool), *(_args := (torch.randn(3, 1, Hq, d, generator=_gen(1561)).to(TYPES[dtype]).cuda(),
+                                       _table(3, 4, 12, 1562).cuda(), torch.tensor([4 * page, 17, 2 * page + 5], dtype=torch.int32).cuda())))
+        K, V, dK, dV = (t.cuda() for t in pool)
+        both, scales = torch.stack([K, V, K], 1), torch.stack([dK, dV], 1)
+        cache = tm.PagedCache(both[:, 0].view(E2M1), both[:, 1].view(E2M1), scales[:, 0].view(E8M0), scales[:, 1].view(E8M0))
+        fused = torch.cat([_args[0], _args[0]], 2)
+        got = tm.tilemix_paged_decode(cache, fused[:, :, Hq:], *_args[1:])
+        assert torch.equal(_bits(got), _bits(want))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("G", [8, 9])
+def test_decode_keys_of_many_magnitudes(dtype, G):
+    """Keys around 2^30, 1 and 2^-30 side by side in a tile, and tiles of small ones only: scores are off by FP32's share
+    of the largest, and a sequence of small keys keeps their bits."""
+    for exps in ((30, 0, -30), (-30, -30, -30), (-60, -30, 30)):
+        tm = _tm()
+        d, page, L = 128, 64, 300
+        K = torch.randn(1, L, 1, d, generator=_gen(61)) * torch.exp2(torch.tensor(exps, dtype=torch.float32)[torch.arange(L) % 3])[None, :, None, None]
+        V = torch.randn(1, L, 1, d, generator=_gen(62))
+        Q = torch.randn(1, 1, G, d, generator=_gen(63)).to(TYPES[dtype])
+        cache = tm.PagedCache(*(t.view(torch.uint8).zero_().view(t.dtype) for t in tm.PagedCache.empty(5, page, 1, d, E2M1)))
+        table, lens = torch.arange(5, dtype=torch.int32).view(1, 5).cuda(), torch.tensor([L], dtype=torch.int32).cuda()
+        tm.tilemix_paged_append(cache, K.bfloat16().cuda(), V.bfloat16().cuda(), table, lens)
+        scale = 2.0 ** -max(exps) / d ** 0.5
+        O, lse = tm.tilemix_paged_decode(cache, Q.cuda(), table, lens, scale, return_lse=True)
+        pool = _host(cache)
+        want = paged_decode(Q.double().numpy()[:, 0], _values(pool, 0), _values(pool, 1), [L], table.cpu().numpy(), scale)
+        _check_decode(f"magnitudes {exps} {dtype} G{G}", O, lse, want, dtype, L, V.numpy())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("Hq,B,slots", [(4, 3, 480), (4, 3, 512), (4, 3, 544), (64, 64, 992), (64, 64, 1024), (64, 64, 1056),
                                         (128, 140, 256)])
 def test_decode_capacities(dtype, Hq, B, slots):
@@ -463,7 +512,8 @@ def test_decode_bf16_range(gains):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("d", [64, 128])
-def test_decode_nan_stays_in_its_sequence(dtype, d):
+@pytest.mark.parametrize("G", [2, 10])
+def test_decode_nan_stays_in_its_sequence(dtype, d, G):
     """A NaN block in one sequence's keys reaches that sequence's heads and nobody else; one in its values those
     channels of its heads."""
     tm = _tm()
@@ -471,7 +521,7 @@ def test_decode_nan_stays_in_its_sequence(dtype, d):
     pool = _cached_pool((12, 2, page, d), 800)
     table = _table(3, 4, 12, 801)
     lens = torch.tensor([60, 60, 60], dtype=torch.int32).cuda()
-    Q = torch.randn(3, 1, 4, d, generator=_gen(802)).to(TYPES[dtype]).cuda()
+    Q = torch.randn(3, 1, 2 * G, d, generator=_gen(802)).to(TYPES[dtype]).cuda()
     before = tm.tilemix_paged_decode(_on_gpu(pool), Q, table.cuda(), lens)
     at = (int(table[1, 2]), 1, 5)                                    # token 37 of sequence 1, KV head 1
     for op in (0, 1):
@@ -480,7 +530,7 @@ def test_decode_nan_stays_in_its_sequence(dtype, d):
         bad[op + 2][at][1] = 255
         after = tm.tilemix_paged_decode(_on_gpu(bad), Q, table.cuda(), lens)
         hit = torch.zeros_like(before, dtype=torch.bool)
-        hit[1, 0, 2:, slice(None) if op == 0 else slice(32, 64)] = True
+        hit[1, 0, G:, slice(None) if op == 0 else slice(32, 64)] = True
         assert torch.isnan(after[hit]).all() and not torch.isnan(after[~hit]).any()
         if op == 0:
             assert torch.equal(_bits(after[~hit]), _bits(before[~hit]))
@@ -508,6 +558,30 @@ def test_offsets_past_32_bits():
         got.append((*tm.tilemix_paged_gather(c, t, lens, 600, cu, 1113, dtype=torch.bfloat16), tm.tilemix_paged_decode(c, Q, t, lens)))
     for a, b in zip(*got):
         assert torch.equal(_bits(a), _bits(b))
+
+
+@pytest.mark.parametrize("fmt", ["mxfp4", "int8", "bf16"])
+def test_gather_of_many_rows(fmt):
+    """More than 2^27 bytes of rows at once are those of several calls."""
+    tm = _tm()
+    Hk, d, page, L = 8, 128, 64, 33000
+    P = -(-L // page)
+    if fmt == "mxfp4":
+        cache = _on_gpu(_cached_pool((16, Hk, page, d), 1900))
+    else:
+        cache = tm.PagedCache.empty(16, page, Hk, d, {"int8": torch.int8, "bf16": torch.bfloat16}[fmt])
+        x = torch.randn(1, 16 * page, Hk, d, generator=_gen(1901)).bfloat16().cuda()
+        tm.tilemix_paged_append(cache, x, x * 2, torch.arange(16, dtype=torch.int32).view(1, 16).cuda(),
+                                torch.tensor([16 * page], dtype=torch.int32).cuda())
+    table = torch.randint(0, 16, (1, P), generator=_gen(1902)).to(torch.int32)
+    table[0, 5] = -1
+    lens = torch.tensor([L], dtype=torch.int32).cuda()
+    assert 4 * L * Hk * d > 2 ** 27
+    K, V = tm.tilemix_paged_gather(cache, table.cuda(), lens, L, dtype=torch.bfloat16)
+    for lo in range(0, L, 11000):
+        k, v = tm.tilemix_paged_gather(cache, table.cuda(), lens - (L - lo - 11000), 11000, dtype=torch.bfloat16)
+        assert _same(K[:, lo:lo + 11000], k) and _same(V[:, lo:lo + 11000], v)
+    assert not K[0, 5 * page:6 * page].any()
 
 
 # ------------------------------------------------------------------------------- as they are used

@@ -272,6 +272,27 @@ def test_streams_and_graph():
         _check("replay", qo[:, 0], q[:, 0].cpu(), lens.cpu().numpy() - 1, f.cpu().numpy(), "half", "bf16")
 
 
+@pytest.mark.parametrize("layout", LAYOUTS)
+def test_more_rows_than_the_caches_hold(layout):
+    """More than 2^27 bytes of results at once, also in place, are those of several calls."""
+    tm = _tm()
+    n, Hq, Hk, d = 17001, 28, 4, 128
+    assert n * (Hq + Hk) * d * 2 > 2 ** 27
+    g = torch.Generator(device="cuda").manual_seed(97)
+    q, k = (torch.randn(n, H, d, generator=g, device="cuda").half() for H in (Hq, Hk))
+    pos = torch.arange(n, dtype=torch.int32, device="cuda") * 7
+    for r in (128, 64, 8):
+        f, _ = tm.tilemix_rotary_frequencies(r)
+        a, b = tm.tilemix_rotary(q, k, f, pos, layout=layout)
+        for lo in range(0, n, 4000):
+            s = slice(lo, lo + 4000)
+            x, y = tm.tilemix_rotary(q[s], k[s], f, pos[s], layout=layout)
+            assert torch.equal(a[s], x) and torch.equal(b[s], y)
+        qi, ki = q.clone(), k.clone()
+        tm.tilemix_rotary(qi, ki, f, pos, layout=layout, Q_out=qi, K_out=ki)
+        assert torch.equal(qi, a) and torch.equal(ki, b)
+
+
 def test_offsets_past_32_bits():
     """Rows 2^31 elements in, and rows that lie far apart."""
     tm = _tm()
