@@ -473,10 +473,11 @@ tilemix_status tilemix_paged_decode_workspace_size(const tilemix_paged_cache* ca
  * to [0, max_pages * page_size]; a sequence without any such token gets O = 0 and lse = -inf.
  * Scores, softmax and sums are FP32; the query is not quantised.  Weights are multiplied as two
  * 16-bit pieces: 22 significant bits down to 2^-40 of the largest possible contribution (a
- * BF16 or MXFP4 cache: 16 bits, whatever their size).  FP16 queries meet the keys of an MXFP4 cache in
- * FP16, which holds them to 2^-25 of the largest magnitude among the (up to 64) tokens of their tile.  An infinity in a value that is attended to makes its
- * channel of O infinite or NaN; so do values of a BF16 or MXFP4 cache of 2^128 / n and more, n the tokens
- * attended to, whose FP32 sum has no room.
+ * BF16 or MXFP4 cache: 16 bits, whatever their size).  With G > 8, FP16 queries meet the
+ * keys of an MXFP4 cache in FP16, which holds them to 2^-25 of the largest magnitude among the (up to 64) tokens
+ * of their tile; otherwise products of an MXFP4 cache are exact.  An infinity in a value that is attended to
+ * makes its channel of O infinite or NaN; so do values of a BF16 or MXFP4 cache of 2^128 / n and more, n the
+ * tokens attended to, whose FP32 sum has no room.
  * Limit: B * H_k * ceil(G / 16) * (max_pages * page_size / 32 + 6) <= 2^30, G = H_q / H_k.
  */
 tilemix_status tilemix_paged_decode(const tilemix_paged_cache* cache, int32_t type, int32_t heads_q,
@@ -520,6 +521,8 @@ tilemix_status tilemix_paged_decode(const tilemix_paged_cache* cache, int32_t ty
  *   slots        device int64 [total] or NULL: page * p + slot of each new row; -1 where it has no page and behind the
  *                last one
  *   total        rows of positions and slots, 0 .. 2^28; further rows are not written
+ * Readers of a page are not counted: one that several tables name would be given back by each of them, so tables
+ * that share pages are not for this call, and the entries that a sequence holds must name pages of its own.
  * One launch, no workspace; captured in a graph it works on the lengths and state of each replay.  Calls
  * on the same list or table must not overlap.
  */

@@ -1139,7 +1139,8 @@ def tilemix_paged_reserve(pages: PageList, page_table, seqlens, wanted, page_siz
     [B]) or ``state_out`` (int32 [4]) is given.  With ``total`` rows the new tokens' positions and slots
     (page * page_size + slot) are written, -1 behind the last one; tensors for the results are allocated when not
     given.  ``window``: a sliding window of that many tokens, whose pages go back when it has left them; ``first_held``
-    (int32 [B], 0 at the start) then keeps the first page-table entry that each sequence still holds."""
+    (int32 [B], 0 at the start) then keeps the first page-table entry that each sequence still holds.  Readers of a page
+    are not counted: tables whose sequences share pages are not for this call."""
     torch = _torch()
     ids, state = pages
     if not isinstance(ids, torch.Tensor) or not ids.is_cuda:
@@ -1249,7 +1250,10 @@ def tilemix_rotary(Q, K, inv_freq, positions=None, *, seqlens_k=None, cu_seqlens
         raise ValueError(f"layout must be one of {list(_LAYOUTS)}, got {layout!r}")
     rows, (Hq, d) = shape[:-2], shape[-2:]
     Hk, k_shape = 0, None
-    if K is not None:
+    if K is None:
+        if K_out is not None:
+            raise ValueError("K_out is given without K")
+    else:
         if getattr(K, "ndim", None) != len(shape):
             raise ValueError("K must have as many dimensions as Q")
         Hk = K.shape[-2]

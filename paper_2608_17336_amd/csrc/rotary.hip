@@ -24,6 +24,7 @@ constexpr int kRowsAhead = 2;
 // same two 146 and 129, 207 and 189.  (Not fewer: 60000 tokens of 8/8 heads, d = 64, 123 MB, 42.7 and 50.7.)
 constexpr long long kStreamBytes = 128 << 20;
 constexpr int kMaxTokens = 8;        // of a workgroup
+constexpr int kGridShift = 23;       // a launch has less than 2^32 threads in x: 2^23 workgroups, and the others in y
 
 // cos and sin of `turns` whole turns.  |a| <= pi / 4: the first terms left out are below 2^-32.
 __device__ __forceinline__ float2 cos_sin(double turns) {
@@ -127,7 +128,7 @@ __global__ __launch_bounds__(kRotaryThreads) void rotary_kernel(RotaryArgs a) {
   __shared__ float2 turn[kMaxTokens * 64];
   __shared__ int where[kMaxTokens];
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
-  const int d = a.d, r = a.r, pairs = r / 2, tokens = 1 << a.token_shift, first = blockIdx.x << a.token_shift;
+  const int d = a.d, r = a.r, pairs = r / 2, tokens = 1 << a.token_shift, first = (blockIdx.x + (blockIdx.y << kGridShift)) << a.token_shift;
   for (int t = wave; t < tokens; t += kRotaryThreads / kWave) {
     const int p = row_position(a, first + t, lane);
     if (lane == 0) where[t] = p;
@@ -234,7 +235,8 @@ hipError_t launch_rotary(RotaryArgs a, int type, bool half, hipStream_t stream) 
          a.total >> a.token_shift > 1024)
     ++a.token_shift;
   a.div_pairs = FastDiv((uint32_t)(a.r / 2));
-  const dim3 grid((unsigned)(((long long)a.total + (1 << a.token_shift) - 1) >> a.token_shift));
+  const unsigned workgroups = (unsigned)(((long long)a.total + (1 << a.token_shift) - 1) >> a.token_shift);
+  const dim3 grid(std::min(workgroups, 1u << kGridShift), (workgroups + (1u << kGridShift) - 1) >> kGridShift);
   auto go = [&](auto T, auto H, auto V) {
     if (V() == 8 && 2LL * a.total * heads * a.d >= kStreamBytes)
       hipLaunchKernelGGL((rotary_kernel<T(), H(), V(), V() == 8>), grid, dim3(kRotaryThreads), 0, stream, a);

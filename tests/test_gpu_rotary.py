@@ -326,3 +326,26 @@ def test_binding_refusals():
                dict(Q_out=torch.zeros(1, 2, 64, dtype=torch.float16, device="cuda").expand(4, 2, 64))):
         with pytest.raises((ValueError, TypeError, tm.TilemixError)):
             tm.tilemix_rotary(**{**ok, **kw})
+
+
+def test_more_workgroups_than_a_launch_has_in_x():
+    """2^27 rows of one head, 8 of them in a workgroup: 2^32 threads and more."""
+    tm = _tm()
+    n, d = 2 ** 27 + 5, 64
+    f, _ = tm.tilemix_rotary_frequencies(d)
+    at = torch.cat([torch.arange(a, b, device="cuda") for a, b in ((0, 20), (2 ** 26 - 11, 2 ** 26 + 13), (n - 25, n))])
+    x, own = torch.empty((n, 1, d), dtype=torch.float16, device="cuda"), _x((len(at), 1, d), "fp16", 97).cuda()
+    x[at] = own
+    pos, some = torch.full((n,), -1, dtype=torch.int32, device="cuda"), _positions(len(at), 98).cuda()
+    pos[at] = some
+    want, _ = tm.tilemix_rotary(own, None, f, some)
+    tm.tilemix_rotary(x, None, f, pos, Q_out=x)
+    assert torch.equal(x[at], want)
+
+
+def test_k_out_goes_with_k():
+    tm = _tm()
+    f, _ = tm.tilemix_rotary_frequencies(64)
+    q, pos = torch.zeros(4, 2, 64, dtype=torch.float16, device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError):
+        tm.tilemix_rotary(q, None, f, pos, K_out=torch.empty_like(q))
