@@ -29,8 +29,11 @@ constexpr int kPagedHeads = 16;                  // query heads on the columns o
 // bytes, so that as many are on their way.  (Four slabs of an 8-bit cache leave two waves per SIMD instead of three: 32
 // sequences of 64 to 8192 keys 34.9 us, with two slabs 30.9; 4 x 65536 keys 102.9 and 105.1.)
 constexpr int tile_slabs(int format) { return is_4bit(format) ? 4 : 2; }
-// Waves that a SIMD holds, by their registers (K and V rows of a tile, the output): workgroups per CU.
-constexpr int resident_per_cu(int d) { return d == 64 ? 4 : 3; }
+// Waves that a SIMD holds, by their registers (K and V rows of a tile, the output): workgroups per CU.  (MXFP4 with four at
+// d = 64, some of whose variants spill then, us with four and with three: 32 sequences of 64 to 8192 keys, 32 / 8 heads, 19.4
+// and 18.2; 16 of 700 to 20001, 16 / 4 heads, 17.2 and 15.7; 131072 keys, 28 / 4 heads, 21.8 and 20.2; 64 x 65536 keys,
+// 16 / 4 heads, 240 and 240, in pages of 16 tokens 269 and 260; with two 19.1, 15.4, 18.3, 244 and 277.)
+constexpr int resident_per_cu(int d, int format) { return d == 64 && !is_4bit(format) ? 4 : 3; }
 
 // The tokens that a sequence's query attends to: first .. len - 1, of tiles tile0 .. .
 template <int KEYS>   // of a tile
@@ -871,7 +874,7 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run<1
 }
 
 template <int D, int TYPE, int FORMAT, bool PAIRED, bool ONE_PAGE>
-__global__ __launch_bounds__(kPagedWaves * kWave) __attribute__((amdgpu_waves_per_eu(resident_per_cu(D))))
+__global__ __launch_bounds__(kPagedWaves * kWave) __attribute__((amdgpu_waves_per_eu(resident_per_cu(D, FORMAT))))
 void paged_decode_kernel(PagedDecodeArgs a) {
   __shared__ DecodeShared<D> shared;
   constexpr int kKeys = 16 * tile_slabs(FORMAT);
@@ -998,7 +1001,7 @@ PagedDecodePlan plan_paged_decode(const PagedPool& p, int heads_q, int d, int fo
   if (window > 0) most = std::min<long long>(most, (window + keys - 2LL) / keys + 1);
   const long long segments = (long long)p.B * pl.head_blocks;
   pl.units = segments * (most + kPartStart);
-  const long long resident = kCUs * resident_per_cu(d);
+  const long long resident = kCUs * resident_per_cu(d, format);
   // Where sequences cannot be long none is split whatever their lengths, and no second launch joins them.  How long,
   // depends on how many workgroups that leaves; us without and with a split, INT8, 8 KV heads, d = 128:
   //   16 tiles     1 sequence of 250 keys 7.7 and 9.5; 8 of 1000 keys 15.2 and 12.7
