@@ -1001,7 +1001,12 @@ PagedDecodePlan plan_paged_decode(const PagedPool& p, int heads_q, int d, int fo
   if (window > 0) most = std::min<long long>(most, (window + keys - 2LL) / keys + 1);
   const long long segments = (long long)p.B * pl.head_blocks;
   pl.units = segments * (most + kPartStart);
-  const long long resident = kCUs * resident_per_cu(d, format);
+  const bool mx = is_4bit(format);
+  // A tile of MXFP4 has twice the keys: two workgroups per CU keep the memory as busy as three where few sequences and
+  // heads are cut, and leave fewer partial results.  us with three and with two, d = 128: 131072 keys, 28 / 4 heads, 27.6 and
+  // 25.5; 32 sequences of 64 to 8192 keys, 32 / 8 heads, 25.3 and 24.6; 8 x 65536 keys, 64 / 8 heads, 98.2 and 96.5; but 64 of 1000
+  // to 30000 keys 107 and 109, 128 of 1 to 4000 34.7 and 36.9; d = 64 32 of 64 to 8192 18.3 and 19.2.
+  const long long resident = kCUs * (mx && d == 128 && segments <= kCUs ? 2 : resident_per_cu(d, format));
   // Where sequences cannot be long none is split whatever their lengths, and no second launch joins them.  How long,
   // depends on how many workgroups that leaves; us without and with a split, INT8, 8 KV heads, d = 128:
   //   16 tiles     1 sequence of 250 keys 7.7 and 9.5; 8 of 1000 keys 15.2 and 12.7
@@ -1015,7 +1020,6 @@ PagedDecodePlan plan_paged_decode(const PagedPool& p, int heads_q, int d, int fo
   // with it): 1 sequence of 500 keys 9.5 and 10.6, of 1000 13.0 and 10.6; 16 of 1000 13.4 and 12.6, of 1900 21.7 and 17.2;
   // 24 of 1000 13.5 and 14.4, of 1900 22.0 and 20.4; 32 of 1900 22.5 and 23.6, of 4000 37.3 and 33.8; 64 of 1900 30.7 and
   // 33.1, of 4000 55.3 and 59.5; 128 of 2000 62.0 and 64.1.
-  const bool mx = is_4bit(format);
   const long long limit = segments < kCUs / 2 ? 16
                         : segments < kCUs * 3 / 4 ? (mx ? 16 : 32)
                         : segments > resident || (mx && segments < kCUs * 3 / 2) ? 32 : 64;
