@@ -26,8 +26,7 @@ constexpr int kRowsThreads = 256;
 constexpr int kRowsAhead = 2;
 // Rows that a lane group takes in all, at most.  us, of the same and of reading 12 prefixes of up to 32768
 // tokens (INT8): 4 rows 129.2 and 115.4, 8 131.1 and 112.0; 16 139.8 and 113.3 (4 at a time).
-// Read back out of MXFP4 (402 MB of rows, cold): 4 rows 100.4, 8 94.6, 16 91.7, 32 91.6.
-constexpr int kAppendRows = 4, kGatherRows = 8, kGatherRows4 = 16;
+constexpr int kAppendRows = 4, kGatherRows = 8;
 
 // The tokens of a workgroup.  Those of a packed batch are numbered in tiles, sequence after sequence, which
 // every wave looks up for itself (a lane takes a run of sequences): a grid over the longest sequence would be
@@ -183,9 +182,8 @@ __global__ __launch_bounds__(kRowsThreads) void paged_append_kernel(PagedRowsArg
 }
 
 // Rows of this many bytes and more are written past the caches, which cannot hold them for their reader and keep
-// the pool instead: 12 prefixes of up to 32768 tokens (402 MB) out of an MXFP4 pool 102.5 us, so 94.6, and 70.7 where the
-// pool is in the caches still; out of an INT8 pool, which is, 111 and 84; 24 prompts of up to 16000 tokens, appended
-// to MXFP4 and read back (193 MB), 124.7 and 97.5.
+// the pool instead: 12 prefixes of up to 32768 tokens (402 MB) out of an MXFP4 pool 101.8 us, so 70.7; 24 of up to 17500
+// (193 MB), after they were appended, 55 and 27.
 constexpr long long kStreamBytes = 128 << 20;
 
 template <int D, int TYPE, int FORMAT, bool STREAM>
@@ -270,7 +268,7 @@ hipError_t launch_paged_append(PagedRowsArgs a, int d, int type, int format, hip
 }
 
 hipError_t launch_paged_gather(PagedRowsArgs a, int d, int type, int format, hipStream_t stream) {
-  const dim3 grid = rows_grid(a, d, is_4bit(format) ? kGatherRows4 : kGatherRows);
+  const dim3 grid = rows_grid(a, d, kGatherRows);
   return for_paged_types(d, type, format, [&](auto D, auto T, auto F) {
     if (4LL * a.total * a.pool.Hk * d >= kStreamBytes)
       hipLaunchKernelGGL((paged_gather_kernel<D(), T(), F(), true>), grid, dim3(kRowsThreads), 0, stream, a);
