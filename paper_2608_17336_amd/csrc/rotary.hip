@@ -20,9 +20,10 @@ constexpr int kRotaryThreads = 256;
 // Heads that a lane requests at a time.  (us at 1, 2, 4 and 8: 196 million BF16 elements, half of each head turned, 146, 146,
 // 153 and 163; 4 x 8192 tokens of 64/8 heads, d = 128, 212, 207, 222 and 241.)
 constexpr int kRowsAhead = 2;
-// Results of this many bytes and more, and their inputs, pass the caches by, which cannot hold them for their reader: the
-// same two 146 and 129, 207 and 189.  (Not fewer: 60000 tokens of 8/8 heads, d = 64, 123 MB, 42.7 and 50.7.)
-constexpr long long kStreamBytes = 128 << 20;
+// Results of this many bytes and more, and their inputs, pass the caches by: the same two 146 and 129, 207 and 189.  But a reader
+// finds less in the caches: sequences of 512 tokens, 32 / 8 heads, d = 128, 126 MB 51.3 and 47.9, with their prefill 184 and 190;
+// 147 MB 58.7 and 55.3, 211 and 214; 189 MB 73.5 and 70.0, 272 and 272; 336 MB 127 and 122, 463 and 459.
+constexpr long long kStreamBytes = 160 << 20;
 constexpr int kMaxTokens = 8;        // of a workgroup
 constexpr int kGridShift = 23;       // a launch has less than 2^32 threads in x: 2^23 workgroups, and the others in y
 

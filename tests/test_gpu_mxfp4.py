@@ -584,6 +584,33 @@ def test_gather_of_many_rows(fmt):
     assert not K[0, 5 * page:6 * page].any()
 
 
+@pytest.mark.parametrize("fmt", ["mxfp4", "int8", "e4m3", "fp16"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_gather_past_the_caches(fmt, d):
+    """More than 2^28 bytes of rows at once, of two sequences in pages that lie in any order, are those of several calls."""
+    tm = _tm()
+    page, Hk, L, short = 32, 1024 // d, 67001, 777
+    P, n = -(-L // page), 67001 + 777
+    if fmt == "mxfp4":
+        cache = _on_gpu(_cached_pool((16, Hk, page, d), 1910))
+    else:
+        dtype = {"int8": torch.int8, "e4m3": torch.float8_e4m3fn, "fp16": torch.float16}[fmt]
+        cache = tm.PagedCache.empty(16, page, Hk, d, dtype)
+        x = torch.randn(1, 16 * page, Hk, d, generator=_gen(1911)).half().cuda()
+        tm.tilemix_paged_append(cache, x, x * 2, torch.arange(16, dtype=torch.int32).view(1, 16).cuda(),
+                                torch.tensor([16 * page], dtype=torch.int32).cuda())
+    table = torch.randint(0, 16, (2, P), generator=_gen(1912)).to(torch.int32).cuda()
+    lens = torch.tensor([L, short], dtype=torch.int32).cuda()
+    cu = torch.tensor([0, L, n], dtype=torch.int32).cuda()
+    assert 4 * n * Hk * d > 2 ** 28
+    K, V = tm.tilemix_paged_gather(cache, table, lens, L, cu, n, dtype=torch.float16)
+    for lo, hi in ((0, 20000), (20000, 40000), (40000, L)):
+        k, v = tm.tilemix_paged_gather(cache, table[:1], lens[:1] - (L - hi), hi - lo, dtype=torch.float16)
+        assert _same(K[lo:hi], k[0]) and _same(V[lo:hi], v[0])
+    k, v = tm.tilemix_paged_gather(cache, table[1:], lens[1:], short, dtype=torch.float16)
+    assert _same(K[L:], k[0]) and _same(V[L:], v[0])
+
+
 # ------------------------------------------------------------------------------- as they are used
 
 def test_prefill_append_decode_and_chunked_prefill():

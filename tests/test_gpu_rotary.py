@@ -293,6 +293,34 @@ def test_more_rows_than_the_caches_hold(layout):
         assert torch.equal(qi, a) and torch.equal(ki, b)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("layout", LAYOUTS)
+def test_results_past_the_caches(layout, dtype):
+    """More than 2^28 bytes of results at once, also in place and of rows without a position, are those of several calls."""
+    tm = _tm()
+    n, Hq, Hk, d = 33001, 28, 4, 128
+    assert n * (Hq + Hk) * d * 2 > 2 ** 28
+    g = torch.Generator(device="cuda").manual_seed(99)
+    q, k = (torch.randn(n, H, d, generator=g, device="cuda").to(TYPES[dtype]) for H in (Hq, Hk))
+    pos = torch.arange(n, dtype=torch.int32, device="cuda") * 7
+    pos[::11] = -1
+    for r in (128, 48):
+        f, _ = tm.tilemix_rotary_frequencies(r)
+        out = [torch.full_like(t, 7) for t in (q, k)]
+        tm.tilemix_rotary(q, k, f, pos, layout=layout, Q_out=out[0], K_out=out[1])
+        assert all((t[::11] == 7).all() for t in out)
+        for lo in range(0, n, 9000):
+            s = slice(lo, lo + 9000)
+            x, y = (torch.full_like(t[s], 7) for t in (q, k))
+            tm.tilemix_rotary(q[s], k[s], f, pos[s], layout=layout, Q_out=x, K_out=y)
+            assert torch.equal(out[0][s], x) and torch.equal(out[1][s], y)
+        qi, ki = q.clone(), k.clone()
+        tm.tilemix_rotary(qi, ki, f, pos, layout=layout, Q_out=qi, K_out=ki)
+        moved = pos >= 0
+        assert torch.equal(qi[moved], out[0][moved]) and torch.equal(ki[moved], out[1][moved])
+        assert torch.equal(qi[~moved], q[~moved]) and torch.equal(ki[~moved], k[~moved])
+
+
 def test_offsets_past_32_bits():
     """Rows 2^31 elements in, and rows that lie far apart."""
     tm = _tm()
