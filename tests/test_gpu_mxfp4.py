@@ -652,6 +652,28 @@ def test_prefill_append_decode_and_chunked_prefill():
         assert np.abs(err).max() <= 2e-3 and np.linalg.norm(err) <= 1e-3 * np.linalg.norm(want)
 
 
+def test_calls_on_two_streams():
+    """Concurrent decodes and gathers on two streams, each with results and workspace of its own, and `stream` given while
+    another is current."""
+    tm = _tm()
+    B, Hq, Hk, d, page = 3, 8, 2, 128, 64
+    cache, table = _on_gpu(_cached_pool((90, Hk, page, d), 1300)), _table(B, 30, 90, 1301).cuda()
+    lens = torch.tensor([1900, 1, 1640], dtype=torch.int32).cuda()
+    Qs = [torch.randn(B, 1, Hq, d, generator=_gen(1302 + i)).half().cuda() for i in range(2)]
+    want = [tm.tilemix_paged_decode(cache, Q, table, lens) for Q in Qs]
+    rows = tm.tilemix_paged_gather(cache, table, lens, 700)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = []
+    for r in range(5):
+        got += [(i, tm.tilemix_paged_decode(cache, Qs[i], table, lens, stream=streams[i]),
+                 tm.tilemix_paged_gather(cache, table, lens, 700, stream=streams[1 - i])) for i in range(2)]
+    torch.cuda.synchronize()
+    for i, O, kv in got:
+        assert torch.equal(_bits(O), _bits(want[i]))
+        assert all(_same(x, y) for x, y in zip(kv, rows))
+
+
 def test_step_captured_in_a_graph():
     """A step of append, decode and gather, captured in two graphs that share a workspace: every replay takes the
     tokens and lengths of its time and gives the eager result."""
