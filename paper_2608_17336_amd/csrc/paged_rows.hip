@@ -25,8 +25,13 @@ constexpr int kRowsThreads = 256;
 // all: 8 at a time 140.1, 4 133.5, 2 131.1.
 constexpr int kRowsAhead = 2;
 // Rows that a lane group takes in all, at most.  us, of the same and of reading 12 prefixes of up to 32768
-// tokens (INT8): 4 rows 129.2 and 115.4, 8 131.1 and 112.0; 16 139.8 and 113.3 (4 at a time).
-constexpr int kAppendRows = 4, kGatherRows = 8;
+// tokens (INT8): appended 2 rows and read 4 116.2 and 94.2, 4 and 4 111.0 and 94.2, 4 and 8 111.2 and 99.1, 8 and 4 112.7 and
+// 93.9, 4 and 2 119.3 and 111.8.
+constexpr int kRows = 4;
+// Adjacent tiles for one XCD: workgroups are dealt to the 8 XCDs in turn, and a tile's scales and exponents are parts of
+// cache lines, which are moved once where one L2 has all parts.  us, as before, in MXFP4: 1 tile 98.5 and 97.6, 4 96.8 and 97.5, 8 96.0
+// and 97.0, 32 95.1 and 96.8, 128 95.3 and 97.5, 512 97.9 and 100.4; in E4M3 and INT8 1 112.5 and 99.2, 32 111.2 and 99.1.
+constexpr int kXcdTiles = 32;
 
 // The tokens of a workgroup.  Those of a packed batch are numbered in tiles, sequence after sequence, which
 // every wave looks up for itself (a lane takes a run of sequences): a grid over the longest sequence would be
@@ -35,7 +40,9 @@ struct RowsTile {
   int b = 0, first = 0, count = 0;   // sequence, packed row of the first token, tokens
   long long token = 0;               // its token number
   __device__ __forceinline__ RowsTile(const PagedRowsArgs& a, int lane) {
-    const int id = blockIdx.x, size = 1 << a.tile_shift;
+    const int size = 1 << a.tile_shift, i = blockIdx.x % (8 * kXcdTiles), first_of = blockIdx.x - i;   // i-th of 8 kXcdTiles
+    // (Behind the last 8 kXcdTiles they stay in order.)
+    const int id = first_of + (first_of + 8 * kXcdTiles <= (int)gridDim.x ? i % 8 * kXcdTiles + i / 8 : i);
     int start, n, t0;
     if (a.cu) {
       const int B = a.pool.B, per = (B + kWave - 1) / kWave, b0 = min(lane * per, B), b1 = min(b0 + per, B);
@@ -245,12 +252,12 @@ __global__ __launch_bounds__(kRowsThreads) void paged_gather_kernel(PagedRowsArg
 }
 
 // Tokens of a workgroup: the most, no more than lane groups and than a sequence can bring, with which a lane group has
-// at most `most` rows.
-dim3 rows_grid(PagedRowsArgs& a, int d, int most) {
+// at most kRows rows.
+dim3 rows_grid(PagedRowsArgs& a, int d) {
   const int groups = kRowsThreads / (d / 8);
   a.tile_shift = 0;
   while ((2 << a.tile_shift) <= groups && (1 << a.tile_shift) < a.len &&
-         (2LL * a.pool.Hk << (a.tile_shift + 1)) <= (long long)groups * most)
+         (2LL * a.pool.Hk << (a.tile_shift + 1)) <= (long long)groups * kRows)
     ++a.tile_shift;
   const long long per = ((long long)a.len + (1 << a.tile_shift) - 1) >> a.tile_shift;   // tiles of the longest sequence
   a.div_tiles = FastDiv((uint32_t)per);
@@ -262,7 +269,7 @@ dim3 rows_grid(PagedRowsArgs& a, int d, int most) {
 }  // namespace
 
 hipError_t launch_paged_append(PagedRowsArgs a, int d, int type, int format, hipStream_t stream) {
-  const dim3 grid = rows_grid(a, d, kAppendRows);
+  const dim3 grid = rows_grid(a, d);
   return for_paged_types(d, type, format, [&](auto D, auto T, auto F) {
     hipLaunchKernelGGL((paged_append_kernel<D(), T(), F()>), grid, dim3(kRowsThreads), 0, stream, a);
     return hipGetLastError();
@@ -270,7 +277,7 @@ hipError_t launch_paged_append(PagedRowsArgs a, int d, int type, int format, hip
 }
 
 hipError_t launch_paged_gather(PagedRowsArgs a, int d, int type, int format, hipStream_t stream) {
-  const dim3 grid = rows_grid(a, d, kGatherRows);
+  const dim3 grid = rows_grid(a, d);
   return for_paged_types(d, type, format, [&](auto D, auto T, auto F) {
     if (4LL * a.total * a.pool.Hk * d >= kStreamBytes)
       hipLaunchKernelGGL((paged_gather_kernel<D(), T(), F(), true>), grid, dim3(kRowsThreads), 0, stream, a);

@@ -560,6 +560,47 @@ def test_offsets_past_32_bits():
         assert torch.equal(_bits(a), _bits(b))
 
 
+@pytest.mark.parametrize("fmt", ["mxfp4", "int8", "fp16"])
+@pytest.mark.parametrize("d,Hk", [(64, 3), (128, 8)])
+def test_append_of_many_tiles(fmt, d, Hk):
+    """A packed batch of thousands of tokens fills the pool as its sequences do one by one in pieces, and nothing else; the
+    rows behind the last sequence are read by nobody and written by nobody."""
+    tm = _tm()
+    page, new = 16, [1, 4999, 0, 333, 2048, 7, 1201]
+    old = [5, 0, 9, 15, 100, 16, 3]
+    B, n, behind = len(new), sum(new), 41
+    per = max(-(-(o + x) // page) for o, x in zip(old, new))
+    P = B * per
+    table = _table(B, per, P, 1920).cuda()
+    lens = torch.tensor([o + x for o, x in zip(old, new)], dtype=torch.int32).cuda()
+    cu = torch.tensor(np.concatenate([[0], np.cumsum(new)]), dtype=torch.int32).cuda()
+    k, v = (torch.randn(n + behind, Hk, d, generator=_gen(1921 + i)).half().cuda() for i in range(2))
+    dtype = {"mxfp4": E2M1, "int8": torch.int8, "fp16": torch.float16}[fmt]
+    bits = lambda c: [t.view(torch.uint8) for t in c if t is not None]
+    one, ref = (tm.PagedCache.empty(P, page, Hk, d, dtype) for _ in range(2))
+    for c in (one, ref):
+        for t in bits(c):
+            t.fill_(77)
+    tm.tilemix_paged_append(one, k, v, table, lens, cu, max(new))
+    for b in range(B):
+        for lo in range(0, new[b], 64):
+            m = min(64, new[b] - lo)
+            at = slice(int(cu[b]) + lo, int(cu[b]) + lo + m)
+            tm.tilemix_paged_append(ref, k[None, at], v[None, at], table[b:b + 1], torch.tensor([old[b] + lo + m], dtype=torch.int32).cuda())
+    for x, y in zip(bits(one), bits(ref)):
+        assert torch.equal(x, y)
+    gk, gv = (torch.full((n + behind, Hk, d), 3.0, dtype=torch.float16, device="cuda") for _ in range(2))
+    tm.tilemix_paged_gather(one, table, lens, max(new), cu, n + behind, K=gk, V=gv, dtype=torch.float16)
+    assert (gk[n:] == 3).all() and (gv[n:] == 3).all()
+    for b in range(B):
+        if new[b]:
+            for lo in range(0, new[b], 64):
+                m = min(64, new[b] - lo)
+                x, y = tm.tilemix_paged_gather(one, table[b:b + 1], torch.tensor([old[b] + lo + m], dtype=torch.int32).cuda(), m)
+                at = slice(int(cu[b]) + lo, int(cu[b]) + lo + m)
+                assert _same(gk[at], x[0]) and _same(gv[at], y[0])
+
+
 @pytest.mark.parametrize("fmt", ["mxfp4", "int8", "bf16"])
 def test_gather_of_many_rows(fmt):
     """More than 2^27 bytes of rows at once are those of several calls."""
