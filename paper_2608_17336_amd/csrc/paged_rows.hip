@@ -189,10 +189,9 @@ __global__ __launch_bounds__(kRowsThreads) void paged_append_kernel(PagedRowsArg
 }
 
 // Rows of this many bytes and more are written past the caches, which then keep the pool.  us, 12 prefixes out of an MXFP4
-// pool: 73 MB of rows 19.5, so 18.2; 120 MB 33.7 and 25.8; 204 MB 61.3 and 43.3; 361 MB 101.8 and 97.7 (out of INT8 108.8 and
-// 99.2); 24 prompts appended to MXFP4 and read back, 201 MB, 125.0 and 98.5.  But their reader finds less in the caches:
-// with a prefill of 16 tokens a sequence over them 113 MB 123 and 127, 148 MB 158 and 162, 183 MB 205 and 203, 226 MB 254 and 254,
-// 355 MB 448 and 431.
+// pool: 73 MB of rows 19.0, so 16.2; 204 MB 64.9 and 40.9; 361 MB 110.5 and 96.8 (out of INT8 102.1 and 94.1); 24 prompts
+// appended to MXFP4 and read back, 201 MB, 126.4 and 94.7.  But their reader finds less in the caches: with a prefill of 16
+// tokens a sequence over them 113 MB 124 and 129, 148 MB 160 and 165, 183 MB 210 and 207, 226 MB 260 and 258, 355 MB 458 and 438.
 constexpr long long kStreamBytes = 160 << 20;
 
 template <int D, int TYPE, int FORMAT, bool STREAM>
