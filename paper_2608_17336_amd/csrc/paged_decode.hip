@@ -1017,9 +1017,10 @@ PagedDecodePlan plan_paged_decode(const PagedPool& p, int heads_q, int d, int fo
   // 2000 42.8 and 47.8, 24 of 4000 69.5 and 66.7 (but 128 of 1 to 1000 68.0 and 58.3); INT8, d = 64 24 of 1000 12.8 and
   // 13.8, 16 of 1500 16.4 and 14.0, 32 of 2000 20.0 and 20.6, 24 of 4000 35.2 and 27.0.
   // MXFP4's tiles, of 64 keys, us on the GPU (what a call takes is at the host's 11 us without the second launch and 15
-  // with it): 1 sequence of 500 keys 9.5 and 10.6, of 1000 13.0 and 10.6; 16 of 1000 13.4 and 12.6, of 1900 21.7 and 17.2;
-  // 24 of 1000 13.5 and 14.4, of 1900 22.0 and 20.4; 32 of 1900 22.5 and 23.6, of 4000 37.3 and 33.8; 64 of 1900 30.7 and
-  // 33.1, of 4000 55.3 and 59.5; 128 of 2000 62.0 and 64.1.
+  // with it): 1 sequence of 500 keys 9.5 and 10.6, of 1000 13.0 and 10.6; 16 of 1000 11.7 and 13.6, of 1900 17.0 and 16.3;
+  // 24 of 1000 11.9 and 15.5, of 1900 18.8 and 21.2, of 500 to 4000 26.7 and 20.1; 32 of 1900 20.3 and 23.7, of 100 to 1900 16.9
+  // and 16.0, of 4000 34.3 and 37.7, of 500 to 4000 27.9 and 24.6; 64 of 1900 30.7 and 33.1, of 4000 55.3 and 59.5; 128 of 2000
+  // 62.0 and 64.1.
   const long long limit = segments < kCUs / 2 ? 16
                         : segments < kCUs * 3 / 4 ? (mx ? 16 : 32)
                         : segments > resident || (mx && segments < kCUs * 3 / 2) ? 32 : 64;
