@@ -26,8 +26,10 @@ constexpr int kRowsThreads = 256;
 constexpr int kRowsAhead = 2;
 // Rows that a lane group takes in all, at most.  us, of the same and of reading 12 prefixes of up to 32768
 // tokens (INT8): appended 2 rows and read 4 116.2 and 94.2, 4 and 4 111.0 and 94.2, 4 and 8 111.2 and 99.1, 8 and 4 112.7 and
-// 93.9, 4 and 2 119.3 and 111.8.
+// 93.9, 4 and 2 119.3 and 111.8.  Read out of MXFP4 at d = 128, whose rows are 64 bytes, with 4 and with 8: 8 heads 96.8 and 96.8,
+// 16 55.8 and 52.2, 32 136 and 131 (d = 64: 8 heads 35.8 and 37.1, 32 110 and 112).
 constexpr int kRows = 4;
+constexpr int gather_rows(int d, int format) { return is_4bit(format) && d == 128 ? 2 * kRows : kRows; }
 // Adjacent tiles for one XCD: workgroups are dealt to the 8 XCDs in turn, and a tile's scales and exponents are parts of
 // cache lines, which are moved once where one L2 has all parts.  us, as before, in MXFP4: 1 tile 98.5 and 97.6, 4 96.8 and 97.5, 8 96.0
 // and 97.0, 32 95.1 and 96.8, 128 95.3 and 97.5, 512 97.9 and 100.4; in E4M3 and INT8 1 112.5 and 99.2, 32 111.2 and 99.1.
@@ -251,12 +253,12 @@ __global__ __launch_bounds__(kRowsThreads) void paged_gather_kernel(PagedRowsArg
 }
 
 // Tokens of a workgroup: the most, no more than lane groups and than a sequence can bring, with which a lane group has
-// at most kRows rows.
-dim3 rows_grid(PagedRowsArgs& a, int d) {
+// at most `most` rows.
+dim3 rows_grid(PagedRowsArgs& a, int d, int most) {
   const int groups = kRowsThreads / (d / 8);
   a.tile_shift = 0;
   while ((2 << a.tile_shift) <= groups && (1 << a.tile_shift) < a.len &&
-         (2LL * a.pool.Hk << (a.tile_shift + 1)) <= (long long)groups * kRows)
+         (2LL * a.pool.Hk << (a.tile_shift + 1)) <= (long long)groups * most)
     ++a.tile_shift;
   const long long per = ((long long)a.len + (1 << a.tile_shift) - 1) >> a.tile_shift;   // tiles of the longest sequence
   a.div_tiles = FastDiv((uint32_t)per);
@@ -268,7 +270,7 @@ dim3 rows_grid(PagedRowsArgs& a, int d) {
 }  // namespace
 
 hipError_t launch_paged_append(PagedRowsArgs a, int d, int type, int format, hipStream_t stream) {
-  const dim3 grid = rows_grid(a, d);
+  const dim3 grid = rows_grid(a, d, kRows);
   return for_paged_types(d, type, format, [&](auto D, auto T, auto F) {
     hipLaunchKernelGGL((paged_append_kernel<D(), T(), F()>), grid, dim3(kRowsThreads), 0, stream, a);
     return hipGetLastError();
@@ -276,7 +278,7 @@ hipError_t launch_paged_append(PagedRowsArgs a, int d, int type, int format, hip
 }
 
 hipError_t launch_paged_gather(PagedRowsArgs a, int d, int type, int format, hipStream_t stream) {
-  const dim3 grid = rows_grid(a, d);
+  const dim3 grid = rows_grid(a, d, gather_rows(d, format));
   return for_paged_types(d, type, format, [&](auto D, auto T, auto F) {
     if (4LL * a.total * a.pool.Hk * d >= kStreamBytes)
       hipLaunchKernelGGL((paged_gather_kernel<D(), T(), F(), true>), grid, dim3(kRowsThreads), 0, stream, a);
