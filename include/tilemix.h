@@ -521,6 +521,7 @@ tilemix_status tilemix_paged_decode(const tilemix_paged_cache* cache, int32_t ty
  *   slots        device int64 [total] or NULL: page * p + slot of each new row; -1 where it has no page and behind the
  *                last one
  *   total        rows of positions and slots, 0 .. 2^28; further rows are not written
+ * Nothing that is written may overlap anything else of the call, but for seqlens_out and free_state_out as said above.
  * Readers of a page are not counted: one that several tables name would be given back by each of them, so tables
  * that share pages are not for this call, and the entries that a sequence holds must name pages of its own.
  * One launch, no workspace; captured in a graph it works on the lengths and state of each replay.  Calls

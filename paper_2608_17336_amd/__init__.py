@@ -1140,7 +1140,8 @@ def tilemix_paged_reserve(pages: PageList, page_table, seqlens, wanted, page_siz
     (page * page_size + slot) are written, -1 behind the last one; tensors for the results are allocated when not
     given.  ``window``: a sliding window of that many tokens, whose pages go back when it has left them; ``first_held``
     (int32 [B], 0 at the start) then keeps the first page-table entry that each sequence still holds.  Readers of a page
-    are not counted: tables whose sequences share pages are not for this call."""
+    are not counted: tables whose sequences share pages are not for this call.  Results may overlap no other tensor of the call,
+    but seqlens_out may be ``seqlens`` or ``wanted`` and state_out the list's state."""
     torch = _torch()
     ids, state = pages
     if not isinstance(ids, torch.Tensor) or not ids.is_cuda:

@@ -126,6 +126,22 @@ tilemix_status check_decode(const tilemix_paged_cache* c, int32_t heads_q) {
   return TILEMIX_OK;
 }
 
+// Bytes of a tensor that a reservation reads or writes, of `rows` rows that lie `step` bytes apart.
+struct Region {
+  const void* at;
+  bool written;
+  long long bytes, rows = 1, step = 0;
+  bool some() const { return at && bytes > 0; }
+  // Whether a row of this one and y, which is in one piece, have a byte in common.
+  bool meets(const Region& y) const {
+    const long long from = (long long)((intptr_t)y.at - (intptr_t)at), to = from + y.bytes;
+    if (from < 0) return to > 0;
+    if (rows == 1) return from < bytes;
+    const long long row = from / step, in = from - row * step;
+    return row < rows && (in < bytes || (row + 1 < rows && in + y.bytes > step));
+  }
+};
+
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // Workspace: [segments][part_mzx][part_o], each 256-byte aligned.
@@ -236,6 +252,23 @@ tilemix_status tilemix_paged_reserve(int32_t page_size, int32_t batch, int32_t m
                         (const void*)free_state_out, (const void*)seqlens_out, (const void*)first_held, (const void*)cu_seqlens, (const void*)positions})
     if (!aligned(p, 4)) return fail(TILEMIX_ERR_ALIGN, "page_table, lengths, free_ids, free_state and positions must be 4-byte aligned");
   if (!aligned(slots, 8)) return fail(TILEMIX_ERR_ALIGN, "slots must be 8-byte aligned");
+  // Workgroups and their threads read and write in no order: what is written may lie over nothing else, but for the lengths
+  // and the state over their old values, which are replaced when all have been read.
+  enum { kTable, kIds, kState, kStateOut, kOld, kWanted, kNew, kFirst, kCu, kPositions, kSlots, kRegions };
+  const long long lengths = 4LL * batch;
+  const Region regions[kRegions] = {
+      {page_table, true, 4LL * max_pages, batch, 4LL * stride_table}, {free_ids, true, 4LL * capacity}, {free_state, true, 16},
+      {free_state_out, true, 16}, {seqlens, false, lengths}, {wanted, false, lengths}, {seqlens_out, true, lengths},
+      {window ? first_held : nullptr, true, lengths}, {cu_seqlens, true, lengths + 4}, {positions, true, 4LL * total},
+      {slots, true, 8LL * total}};
+  for (int i = 0; i < kRegions; ++i)
+    for (int j = i + 1; j < kRegions; ++j) {
+      const Region &x = regions[i], &y = regions[j];
+      const bool may_be = (i == kState && j == kStateOut) || ((i == kOld || i == kWanted) && j == kNew);
+      if ((x.written || y.written) && x.some() && y.some() && !(may_be && x.at == y.at) && x.meets(y))
+        return fail(TILEMIX_ERR_SHAPE, "what is written may overlap nothing else, but seqlens_out may be seqlens or wanted and "
+                                       "free_state_out may be free_state");
+    }
   tilemix::ReserveArgs a{};
   while ((1 << a.page_shift) < page_size) ++a.page_shift;
   a.B = batch; a.max_pages = max_pages;

@@ -215,14 +215,8 @@ __global__ __launch_bounds__(THREADS) void paged_reserve_kernel(ReserveArgs a) {
 
 hipError_t launch_paged_reserve(ReserveArgs a, hipStream_t stream) {
   if (!a.positions && !a.slots) a.total = 0;
-  // (first_held always is.)
-  auto overlap = [](const int* x, long long n, const int* y, long long m) { return x < y + m && y < x + n; };
-  a.in_place = a.window > 0;
-  for (const int* in : {a.old_lens, a.want}) {
-    a.in_place |= overlap(a.lens_out, a.B, in, a.B) || overlap(a.state_out, 4, in, a.B);
-    if (a.cu) a.in_place |= overlap(a.cu, a.B + 1, in, a.B);
-  }
-  a.in_place |= overlap(a.state_out, 4, a.state, 4) || overlap(a.lens_out, a.B, a.state, 4);
+  // (first_held always is; other overlaps are refused.)
+  a.in_place = a.window > 0 || a.lens_out == a.old_lens || a.lens_out == a.want || a.state_out == a.state;
   // (How many entries change is not known here: a part of those that could.)  Workgroups that write the state in place count
   // themselves one after the other, some 10 ns each: fewer and larger ones.
   const long long items = a.total + std::min<long long>((long long)a.B * a.max_pages, a.capacity) / 8;
