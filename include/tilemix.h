@@ -504,7 +504,7 @@ tilemix_status tilemix_paged_decode(const tilemix_paged_cache* cache, int32_t ty
  *   seqlens      device int32 [batch]: lengths now; clamped to [0, max_pages * p]
  *   wanted       device int32 [batch]: lengths to be; negative ones count as 0
  *   window       0: none; w >= 1: only the last w tokens will be attended to (take as many more as tokens may be taken
- *                back again)
+ *                back again); batch * max_pages < 2^30 then
  *   first_held   device int32 [batch], with a window: the first entry that each sequence holds, read and
  *                written; 0 for a sequence without tokens.  NULL without a window
  *   free_ids     device int32 [capacity], a ring: the i-th free page is free_ids[(head + i) % capacity]; pages are

@@ -243,6 +243,9 @@ tilemix_status tilemix_paged_reserve(int32_t page_size, int32_t batch, int32_t m
     return fail(TILEMIX_ERR_SHAPE, "max_pages must be >= 1 and max_pages * page_size <= 2^30");
   if (stride_table < max_pages || stride_table > kStrideMax) return fail(TILEMIX_ERR_SHAPE, "stride_table must be >= max_pages");
   if (window < 0) return fail(TILEMIX_ERR_SHAPE, "window must be >= 0");
+  // (Without one, no more entries change than pages are free; the kernel counts them up to 2^30 - 1.)
+  if (window && (long long)batch * max_pages >= 1 << 30)
+    return fail(TILEMIX_ERR_SHAPE, "batch * max_pages must be < 2^30 with a window");
   if (capacity < 1 || capacity > (1 << 30) - 2) return fail(TILEMIX_ERR_SHAPE, "capacity must be 1 .. 2^30 - 2");
   if (total < 0 || total > kRowsMax) return fail(TILEMIX_ERR_SHAPE, "total must be 0 .. %d", kRowsMax);
   if (!page_table || !seqlens || !wanted || !free_ids || !free_state || !free_state_out || !seqlens_out)

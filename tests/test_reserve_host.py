@@ -61,3 +61,12 @@ def test_overlaps_through_a_shifted_alias():
     assert _reserve(cu=lens - 4) == SHAPE and _reserve(cu=3 * STEP - 4) == SHAPE
     assert _reserve(lens_out=lens, wanted=lens, first=lens, window=3) == SHAPE
     assert _reserve(state_out=6 * STEP, state=6 * STEP, cu=6 * STEP + 8) == SHAPE
+
+
+def test_entries_that_the_window_leaves_are_counted_in_32_bits():
+    """With a window a call may set every entry of the table: up to 2^30 - 1 of them.  (NULL: passed the checks of sizes.)"""
+    many = dict(B=64, per=1 << 24, stride=1 << 24, page=64)
+    assert _reserve(window=1, **many) == SHAPE and b"window" in tm.load_library().tilemix_last_error()
+    assert _reserve(window=1, **{**many, "B": 65, "per": (1 << 24) - 1}) == SHAPE
+    assert _reserve(window=1, table=None, **{**many, "per": (1 << 24) - 1}) == NULL
+    assert _reserve(window=0, table=None, **many) == NULL
