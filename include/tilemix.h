@@ -592,7 +592,8 @@ typedef struct tilemix_rotary_params {
  *                (>= 0, multiples of 8: a slice of a fused projection needs no copy)
  *   Q_out, K_out written, rows q_out_stride / k_out_stride apart (>= H * d); may be Q and K with the same
  *                strides, and may not overlap them otherwise
- * Angles are reduced in FP64 (positions up to 2^31 keep 2^-24 of a turn), the rest is FP32, rounded once.
+ * Angles are those of the given f_i, reduced in two FP64 numbers: a cosine or sine of a position up to 2^31 (|f_i| <= 1) is off by
+ * 2^-21 of itself and 2^-48; the rest is FP32, rounded once.
  */
 tilemix_status tilemix_rotary(const tilemix_rotary_params* params, const int32_t* positions,
                               const int32_t* seqlens_k, const int32_t* cu_seqlens, int32_t batch, int32_t total,

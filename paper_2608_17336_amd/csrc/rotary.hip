@@ -5,8 +5,8 @@
 // (x1, x2) being channels (i, i + r / 2) or (2 i, 2 i + 1); channels from r on stay as they are.  `inverse` turns by
 // -p f_i: the transposed map, which is the gradient of the other.
 //
-// An angle of a far position has more bits than FP32: it is reduced to a quarter turn in FP64, and the sine and
-// cosine of what is left, at most an eighth of a turn, are Taylor sums in FP32.  That is some 40 instructions, so a
+// An angle of a far position has more bits than FP32: it is reduced to a quarter turn in two FP64 numbers, and the sine and
+// cosine of what is left, at most an eighth of a turn, are Taylor sums in FP32.  That is some 45 instructions, so a
 // workgroup does it once for each (token, pair) and leaves both in LDS for all heads.
 #include "paged_device.h"
 
@@ -27,9 +27,15 @@ constexpr long long kStreamBytes = 160 << 20;
 constexpr int kMaxTokens = 8;        // of a workgroup
 constexpr int kGridShift = 23;       // a launch has less than 2^32 threads in x: 2^23 workgroups, and the others in y
 
-// cos and sin of `turns` whole turns.  |a| <= pi / 4: the first terms left out are below 2^-32.
-__device__ __forceinline__ float2 cos_sin(double turns) {
-  const double quarters = (turns - rint(turns)) * 4.0, n = rint(quarters);
+// cos and sin of p f, p a whole number.  The product and its turns are each a sum of two FP64 numbers, and so is 1 / (2 pi):
+// rounded to one, the turns of position 2^31 were off by up to 2^-24, where a result near 0 has no such room.  What is
+// left of whole turns is then off by 2^-52.  |a| <= pi / 4: the first terms left out are below 2^-32.
+__device__ __forceinline__ float2 cos_sin(int p, double f) {
+#pragma clang fp contract(off)   // (a product whose rounding `low` takes up again must be rounded)
+  constexpr double kTurn = 0.15915494309189535, kTurnLow = -9.839338337591243e-18;
+  const double t = p * f, turns = t * kTurn;
+  const double low = fma(t, kTurn, -turns) + fma(t, kTurnLow, fma((double)p, f, -t) * kTurn);
+  const double quarters = (turns - rint(turns) + low) * 4.0, n = rint(quarters);
   const float a = (float)(quarters - n) * 1.57079632679489662f, b = a * a;
   float s = fmaf(b, -1.0f / 39916800, 1.0f / 362880);
   s = fmaf(b, s, -1.0f / 5040);
@@ -137,7 +143,7 @@ __global__ __launch_bounds__(kRotaryThreads) void rotary_kernel(RotaryArgs a) {
   __syncthreads();
   for (int k = tid; k < tokens * pairs; k += kRotaryThreads) {
     const int t = (int)a.div_pairs.quot(k), i = k - t * pairs;
-    const float2 cs = cos_sin((double)where[t] * a.inv_freq[i] * 0.15915494309189533577);
+    const float2 cs = cos_sin(where[t], a.inv_freq[i]);
     turn[k] = make_float2(cs.x * a.magnitude, a.inverse ? -cs.y * a.magnitude : cs.y * a.magnitude);
   }
   __syncthreads();

@@ -1,5 +1,7 @@
 """GPU: rotary positions against float64."""
 
+from fractions import Fraction
+
 import numpy as np
 import pytest
 import torch
@@ -101,6 +103,60 @@ def test_far_positions(layout):
         f, g = tm.tilemix_rotary_frequencies(64, **kw)
         q, _ = tm.tilemix_rotary(Q.cuda(), None, f, pos.cuda(), layout=layout, magnitude=g)
         _check(f"far {kw}", q, Q, pos.numpy(), f.cpu().numpy(), layout, "fp16", g)
+
+
+def _pi(bits=400):
+    """pi 2^bits as a whole number: 16 arctan(1/5) - 4 arctan(1/239)."""
+    def arctan(x):
+        t = (1 << (bits + 32)) // x
+        total, n = t, 1
+        while t:
+            t //= -x * x
+            n += 2
+            total += t // n
+        return total
+    return (16 * arctan(5) - 4 * arctan(239)) >> 32
+
+
+def _exact_cos_sin(p, f):
+    """cos(p f) and sin(p f), from the angle's remainder by a quarter turn in whole numbers."""
+    num, den = float(f).as_integer_ratio()           # den: a power of two
+    quarter = _pi() * den >> 1                       # 2^400 den pi / 2
+    k, rest = divmod((p * num << 400) + quarter // 2, quarter)
+    a = float(Fraction(rest - quarter // 2, den << 400))
+    c, s = np.cos(a), np.sin(a)
+    return ((c, s), (-s, c), (-c, -s), (s, -c))[k % 4]
+
+
+@pytest.mark.parametrize("layout", LAYOUTS)
+def test_far_angles_next_to_quarter_turns(layout):
+    """(1, 0) turned by angles of positions up to 2^31 whose cosine is next to 0: the BF16 result has its own size's bits, and
+    shows what the angle has lost.  A cosine or sine is off by 8 2^-24 of itself (the argument's 2^-24 and its factor's 2^-25, the
+    last sums' roundings) and the FP64 angle's 2^-52 of a turn, below 2^-48; the result rounds by half a step."""
+    tm = _tm()
+    f, _ = tm.tilemix_rotary_frequencies(128)
+    host = f.cpu().numpy()
+    pos = []
+    for i in (0, 1, 2, 7, 20, 40):
+        k = np.arange(1 << 21) + int((2 ** 31 - 10) * host[i] / np.pi) - (1 << 21)
+        k = k[k >= 0]
+        p = np.rint((k + 0.5) * np.pi / host[i])
+        near = np.abs(p * host[i] - (k + 0.5) * np.pi) < 1e-5
+        pos += p[near & (p < 2 ** 31)].astype(int).tolist()[-40:]
+    assert len(pos) > 100
+    x = torch.zeros(len(pos), 1, 128)
+    x[..., :64] = 1.0
+    if layout == "interleaved":
+        x = x.view(-1, 1, 2, 64).transpose(2, 3).reshape(-1, 1, 128)
+    q, _ = tm.tilemix_rotary(x.bfloat16().cuda(), None, f, torch.tensor(pos, dtype=torch.int32).cuda(), layout=layout)
+    got = q.double().cpu().numpy()[:, 0]
+    got = (got[:, :64], got[:, 64:]) if layout == "half" else (got[:, 0::2], got[:, 1::2])
+    want = np.array([[_exact_cos_sin(p, v) for v in host] for p in pos])
+    assert (np.abs(want[..., 0]) < 1e-5).sum() > 100
+    for j in range(2):
+        err, tol = np.abs(got[j] - want[..., j]), np.abs(want[..., j]) * (2.0 ** -8 + 2.0 ** -21) + 2.0 ** -48
+        log(f"rotary next to quarter turns {layout} {j}: error/tolerance {(err / tol).max():.3f}")
+        assert (err <= tol).all(), (err / tol).max()
 
 
 def test_every_angle_of_a_turn():
