@@ -474,8 +474,8 @@ tilemix_status tilemix_paged_decode_workspace_size(const tilemix_paged_cache* ca
  * Scores, softmax and sums are FP32; the query is not quantised.  Weights are multiplied as two
  * 16-bit pieces: 22 significant bits down to 2^-40 of the largest possible contribution (a
  * BF16 or MXFP4 cache: 16 bits, whatever their size).  With G > 8, FP16 queries meet the
- * keys of an MXFP4 cache in FP16, which holds them to 2^-25 of the largest magnitude among the (up to 64) tokens
- * of their tile; otherwise products of an MXFP4 cache are exact.  An infinity in a value that is attended to
+ * keys of an MXFP4 cache in FP16, which holds them to 2^-38 of the largest power of two of a block among the (up to
+ * 64) tokens of their tile; otherwise products of an MXFP4 cache are exact.  An infinity in a value that is attended to
  * makes its channel of O infinite or NaN; so do values of a BF16 or MXFP4 cache of 2^128 / n and more, n the
  * tokens attended to, whose FP32 sum has no room.
  * Limit: B * H_k * ceil(G / 16) * (max_pages * page_size / 32 + 6) <= 2^30, G = H_q / H_k.

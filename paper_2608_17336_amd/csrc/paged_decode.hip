@@ -292,6 +292,7 @@ __device__ __forceinline__ uint32_t quad_lane(uint32_t x) {
 // number any more; and z, which knows nothing of x, loses nothing to a value's size.  e starts at kExpMin, that of the
 // smallest subnormal scale, 2^-149: values near BF16's smallest are weighted like any others.
 constexpr int kExpMin = -148;
+constexpr int kKeyTop = 13;   // the largest exponent of MXFP4 keys in FP16: 6 2^13 is the largest of them
 template <int FORMAT>
 constexpr int kHeadroom = operand_type(FORMAT) == TILEMIX_BF16 ? 0 : 15;
 
@@ -568,9 +569,11 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run<1
   #pragma unroll
       for (int s = 0; s < (ONE_PAGE ? 0 : kS); ++s) has |= page[s] >= 0 ? 1u << s : 0u;
       all = all && has == (1u << kS) - 1;
-      // FP16 queries take MXFP4 keys in FP16: code 2^(e - top), top the largest exponent of a key that counts, so that
-      // what FP16 cannot hold lies below 2^-25 of the tile's largest key.  (As two BF16 pieces, which lose nothing, they took
-      // twice the products and 16 registers more, which spilled: 8 x 65536 keys 119 us.)  A NaN among them is one in all scores.
+      // FP16 queries take MXFP4 keys in FP16: code 2^(e - top + kKeyTop), top the largest exponent of a key that counts, so that
+      // what FP16 cannot hold lies below 2^-38 of 2^top.  (As two BF16 pieces, which lose nothing, they took twice the products
+      // and 16 registers more, which spilled: 8 x 65536 keys 119 us.)  A NaN among them is one in all scores.  What takes a
+      // score back to its size is a factor up to 1 and, for keys beyond 2^13, a power of two for the score itself: as
+      // one factor it is infinite for scales of 6 and more beside BF16's largest numbers.
       float f_tile = f_head;
       uint32_t top = 0;
       if constexpr (kRelative) {
@@ -587,14 +590,14 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run<1
   #pragma unroll
         for (int s = 1; s < kS; ++s) e = max(e, ek[s]);
         top = (uint32_t)wave_max((int)e);
-        f_tile = top == kBlockNaN ? __builtin_nanf("") : __builtin_amdgcn_ldexpf(f_head, (int)top - 127);
+        f_tile = top == kBlockNaN ? __builtin_nanf("") : __builtin_amdgcn_ldexpf(f_head, min((int)top - 127 - kKeyTop, 0));
       }
       float sc[kS][4];
   #pragma unroll
       for (int s = 0; s < kS; ++s) {
         f32x4 c = {0.0f, 0.0f, 0.0f, 0.0f};
         if constexpr (k4) {
-          const float scale = kRelative ? block_scale(max(ek[s] + 127, top) - top) : exponent_scale(ek[s], key_byte);
+          const float scale = kRelative ? block_scale(max(ek[s] + 127 + kKeyTop, top) - top) : exponent_scale(ek[s], key_byte);
           const uint32_t w[4] = {kr[s][0].x, kr[s][0].y, kr[s][0].z, kr[s][0].w};
   #pragma unroll
           for (int k = 0; k < kQ; ++k) {
@@ -618,6 +621,14 @@ __device__ __forceinline__ void decode_run(const PagedDecodeArgs& a, const Run<1
         // Scores are scaled and rounded before the max and the exponent see them.
   #pragma unroll
         for (int r = 0; r < 4; ++r) sc[s][r] = c[r] * (k8 ? f_head * dk[s][r] : f_tile);
+      }
+      if constexpr (kRelative) {
+        if (top > 127 + kKeyTop) {
+  #pragma unroll
+          for (int s = 0; s < kS; ++s)
+  #pragma unroll
+            for (int r = 0; r < 4; ++r) sc[s][r] = __builtin_amdgcn_ldexpf(sc[s][r], (int)top - 127 - kKeyTop);
+        }
       }
       __builtin_amdgcn_sched_barrier(0);
       const bool here = n + kPagedWaves < cur.end;

@@ -387,6 +387,61 @@ def test_decode_keys_of_many_magnitudes(dtype, G):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("G,d,page", [(8, 128, 64), (9, 128, 64), (16, 128, 16), (16, 64, 64), (12, 64, 32)])
+@pytest.mark.parametrize("byte,code", [(252, 6.0), (253, 3.0), (254, 1.5)])
+@pytest.mark.parametrize("scale", [1.0, 8.0, 4096.0])
+def test_decode_largest_keys(dtype, G, d, page, byte, code, scale):
+    """Keys of 1.5 2^127, of either sign, and queries that are 0 or have one small channel: finite scores.  Those of a head are
+    equal but for their sign, so that its weights are equal, or 0: off by their pieces' 2^-15, and a sum of n terms by n 2^-24.
+    (Scores are FP32 in units of ln 2: with the largest scale 2^(h - 25) 1.5 2^127 4096 / ln 2 = 2.16 2^(h + 114) of heads from 13
+    on is none.)"""
+    tm = _tm()
+    L, pages = 90, 90 // page + 1
+    pool = _cached_pool((pages, 1, page, d), 1800)
+    sign = torch.randint(0, 2, (pages, 1, page, d), generator=_gen(1801)).numpy() * 2.0 - 1
+    pool[0] = torch.from_numpy(pack_e2m1(code * sign))
+    pool[2] = torch.full((pages, 1, page, d // 32), byte, dtype=torch.uint8)
+    Q = torch.zeros(1, 1, G, d)
+    for h in range(1, G):
+        Q[0, 0, h, (11 * h) % d] = 2.0 ** (h - 25)
+    Q = Q.to(TYPES[dtype])
+    table, lens = torch.arange(pages, dtype=torch.int32).view(1, -1), torch.tensor([L], dtype=torch.int32)
+    O, lse = tm.tilemix_paged_decode(_on_gpu(pool), Q.cuda(), table.cuda(), lens.cuda(), scale, return_lse=True)
+    V = _values(pool, 1)
+    wO, wl, mass, reach = paged_decode(Q.double().numpy()[:, 0], _values(pool, 0), V, [L], table.numpy(), scale)
+    room = reach / np.log(2.0) < 2.0 ** 128
+    assert room.sum() == (min(G, 13) if scale == 4096.0 else G)
+    wO, wl, mass = wO[room], wl[room], mass[room]
+    O, lse, f = O.double().cpu().numpy()[:, 0][room], lse.double().cpu().numpy()[room], torch.finfo(TYPES[dtype])
+    assert np.isfinite(O).all() and (np.abs(O - wO) <= f.eps / 2 * np.abs(wO) + (2.0 ** -15 + L * 2.0 ** -24) * mass * (1 + f.eps) + f.smallest_normal * f.eps).all()
+    assert (np.abs(lse - wl) <= 2.0 ** -21 * np.abs(wl)).all()      # four roundings, log2 e's and ln 2's among them
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("G,d,page", [(8, 128, 64), (9, 128, 64), (16, 128, 16), (16, 64, 64)])
+def test_decode_small_keys_beside_a_large_one(dtype, G, d, page):
+    """A tile with one key 2^32 times as large as the others, in channels that the query does not read: the others keep
+    their bits."""
+    tm = _tm()
+    L, pages = 64, 64 // page
+    K = torch.randn(1, L, 1, d, generator=_gen(1810)) * 2.0 ** -12
+    K[..., :32] = 0.0
+    K[0, 5, 0, :32] = 2.0 ** 20
+    V = torch.randn(1, L, 1, d, generator=_gen(1811))
+    Q = torch.randn(1, 1, G, d, generator=_gen(1812))
+    Q[..., :32] = 0.0
+    Q = Q.to(TYPES[dtype])
+    cache = tm.PagedCache.empty(pages, page, 1, d, E2M1)
+    table, lens = torch.arange(pages, dtype=torch.int32).view(1, -1).cuda(), torch.tensor([L], dtype=torch.int32).cuda()
+    tm.tilemix_paged_append(cache, K.bfloat16().cuda(), V.bfloat16().cuda(), table, lens)
+    scale = 2.0 ** 12 / d ** 0.5
+    O, lse = tm.tilemix_paged_decode(cache, Q.cuda(), table, lens, scale, return_lse=True)
+    pool = _host(cache)
+    want = paged_decode(Q.double().numpy()[:, 0], _values(pool, 0), _values(pool, 1), [L], table.cpu().numpy(), scale)
+    _check_decode(f"beside a large key {dtype} G{G} d{d}", O, lse, want, dtype, L, _values(pool, 1))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("Hq,B,slots", [(4, 3, 480), (4, 3, 512), (4, 3, 544), (64, 64, 992), (64, 64, 1024), (64, 64, 1056),
                                         (128, 140, 256)])
 def test_decode_capacities(dtype, Hq, B, slots):
