@@ -815,10 +815,10 @@ class PagedCache(NamedTuple):
     @staticmethod
     def empty(pages: int, page_size: int, heads_kv: int, head_dim: int, dtype=None, device="cuda") -> "PagedCache":
         """An uninitialised pool (int8 when no dtype is given)."""
-        import torch
+        torch = _torch()
         dtype = torch.int8 if dtype is None else dtype
         shape = (pages, heads_kv, page_size, head_dim)
-        if dtype == torch.float4_e2m1fn_x2:
+        if _format(dtype) == 5:
             return PagedCache(*(torch.empty((*shape[:3], head_dim // n), dtype=t, device=device)
                                 for n, t in ((2, dtype), (2, dtype), (32, torch.float8_e8m0fnu), (32, torch.float8_e8m0fnu))))
         K, V = (torch.empty(shape, dtype=dtype, device=device) for _ in range(2))
@@ -840,7 +840,9 @@ def _torch():
     global _TORCH
     if _TORCH is None:
         import torch
-        _FORMATS.update({torch.float16: 0, torch.bfloat16: 1, torch.int8: 2, torch.float8_e4m3fn: 3, torch.float4_e2m1fn_x2: 5})
+        _FORMATS.update({torch.float16: 0, torch.bfloat16: 1, torch.int8: 2, torch.float8_e4m3fn: 3})
+        if hasattr(torch, "float4_e2m1fn_x2"):   # (without the type there are no pools of it, and all else works)
+            _FORMATS[torch.float4_e2m1fn_x2] = 5
         _TORCH = torch
     return _TORCH
 

@@ -55,3 +55,16 @@ def test_binding_refusals():
                  lambda: tm.tilemix_paged_decode(pool, x, table, lens)):
         with pytest.raises(TypeError, match="CUDA"):
             call()
+
+
+def test_a_torch_without_the_4_bit_type(monkeypatch):
+    """Everything but MXFP4 pools works with a torch that has no such type."""
+    monkeypatch.delattr(torch, "float4_e2m1fn_x2")
+    monkeypatch.delattr(torch, "float8_e8m0fnu")
+    monkeypatch.setattr(tm, "_TORCH", None)
+    monkeypatch.setattr(tm, "_FORMATS", {})
+    pool = tm.PagedCache.empty(4, 16, 2, 64, device="cpu")
+    assert pool.K.dtype == torch.int8 and pool.dK.dtype == torch.float32
+    assert tm.PagedCache.empty(4, 16, 2, 64, torch.bfloat16, device="cpu").dK is None
+    assert [tm._format(t) for t in (torch.float16, torch.bfloat16, torch.int8, torch.float8_e4m3fn, torch.float64)] == [0, 1, 2, 3, -1]
+    assert tm._alloc(None, (3,), dtype=torch.int32).shape == (3,)
