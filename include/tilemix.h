@@ -407,8 +407,8 @@ typedef struct tilemix_paged_cache {
   int64_t stride_table;       /* entries between rows of page_table, >= max_pages */
   void* K;                    /* device, 16-byte aligned */
   void* V;
-  void* dK;                   /* device, 16-byte aligned; ignored for FP16 and BF16 */
-  void* dV;
+  float* dK;                  /* device, 16-byte aligned; ignored for FP16 and BF16.  MXFP4: the exponents' bytes, cast */
+  float* dV;
   const int32_t* page_table;  /* device int32 [B, max_pages], 4-byte aligned */
   const int32_t* seqlens_k;   /* device int32 [B], 4-byte aligned: tokens of each sequence */
 } tilemix_paged_cache;

@@ -1,6 +1,7 @@
 """Host-side checks of the paged cache calls over an MXFP4 pool (no kernel is launched, the pointers are fake)."""
 
 import os
+import subprocess
 
 import pytest
 import torch
@@ -68,3 +69,23 @@ def test_a_torch_without_the_4_bit_type(monkeypatch):
     assert tm.PagedCache.empty(4, 16, 2, 64, torch.bfloat16, device="cpu").dK is None
     assert [tm._format(t) for t in (torch.float16, torch.bfloat16, torch.int8, torch.float8_e4m3fn, torch.float64)] == [0, 1, 2, 3, -1]
     assert tm._alloc(None, (3,), dtype=torch.int32).shape == (3,)
+
+
+@pytest.mark.parametrize("compiler,name", [("gcc", "use.c"), ("g++", "use.cpp")])
+def test_scales_keep_their_type_in_c(tmp_path, compiler, name):
+    """FP32 scales are written and read back as such, by name and by position; exponents are bytes behind the same pointers."""
+    src = tmp_path / name
+    src.write_text('''
+#include "tilemix.h"
+float first(const tilemix_paged_cache* c) { const float* s = c->dK; float* v = c->dV; return s[0] + v[0]; }
+void bytes(tilemix_paged_cache* c, uint8_t* e) { c->dK = (float*)e; c->dV = (float*)(e + 16); }
+tilemix_paged_cache make(void* x, float* s, const int32_t* t) {
+  tilemix_paged_cache c = {TILEMIX_INT8, 4, 16, 2, 64, 1, 4, 2048, 2048, 32, 32, 4, x, x, s, s + 32, t, t};
+  float* back = c.dK;
+  c.dV = back;
+  return c;
+}
+''')
+    include = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include")
+    r = subprocess.run([compiler, "-fsyntax-only", "-Wall", "-Werror", "-I", include, str(src)], capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
