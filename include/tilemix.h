@@ -475,7 +475,8 @@ tilemix_status tilemix_paged_decode_workspace_size(const tilemix_paged_cache* ca
  * 16-bit pieces: 22 significant bits down to 2^-40 of the largest possible contribution (a
  * BF16 or MXFP4 cache: 16 bits, whatever their size).  With G > 8, FP16 queries meet the
  * keys of an MXFP4 cache in FP16, which holds them to 2^-38 of the largest power of two of a block among the (up to
- * 64) tokens of their tile; otherwise products of an MXFP4 cache are exact.  An infinity in a value that is attended to
+ * 64) tokens of their tile (a code that reads as an infinity counts as code * 2^e); otherwise products of an MXFP4 cache are
+ * exact.  An infinity in a value that is attended to
  * makes its channel of O infinite or NaN; so do values of a BF16 or MXFP4 cache of 2^128 / n and more, n the
  * tokens attended to, whose FP32 sum has no room.
  * Limit: B * H_k * ceil(G / 16) * (max_pages * page_size / 32 + 6) <= 2^30, G = H_q / H_k.
@@ -550,7 +551,9 @@ typedef enum tilemix_scaling_kind {
   TILEMIX_SCALING_YARN = 3     /* arXiv 2309.00071: between f_i and f_i / s by f_i's rotations over the original
                                   length, n_i = original_len f_i / (2 pi): c f_i + (1 - c) f_i / s with
                                   c = (n_i - beta_slow) / (beta_fast - beta_slow) clamped to [0, 1]; and
-                                  g = 0.1 ln s + 1 (1 for the other kinds) */
+                                  g = 0.1 ln s + 1 (1 for the other kinds).  Programs that ramp c over the pair's
+                                  number i instead, between those of beta_fast and beta_slow, have other
+                                  frequencies in between: models trained so need theirs as inv_freq */
 } tilemix_scaling_kind;
 
 typedef struct tilemix_rotary_scaling {

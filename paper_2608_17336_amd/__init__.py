@@ -1218,7 +1218,8 @@ def tilemix_rotary_frequencies(rotary_dim: int, base: float = 10000.0, *, scalin
     """(inv_freq float64 [rotary_dim / 2] on ``device``, magnitude) for tilemix_rotary.  ``scaling`` for contexts that are
     ``factor`` times as long as those trained on: "linear" (positions / factor), "ntk" (a larger base) or "yarn" (arXiv
     2309.00071, with ``original_len`` tokens trained on: frequencies of more than ``beta_fast`` rotations over them are
-    kept, those of fewer than ``beta_slow`` divided)."""
+    kept, those of fewer than ``beta_slow`` divided, and those in between mixed by their rotations, as in the paper; a model
+    whose training mixed them by the pair's number needs its own inv_freq)."""
     if scaling not in _SCALINGS:
         raise ValueError(f"scaling must be one of {list(_SCALINGS)}, got {scaling!r}")
     import torch
@@ -1239,7 +1240,7 @@ def tilemix_rotary(Q, K, inv_freq, positions=None, *, seqlens_k=None, cu_seqlens
     tilemix_paged_append.  Pairs are channels i and i + rotary_dim / 2 (layout "half") or 2 i and 2 i + 1
     ("interleaved").  Returns (Q_out, K_out), allocated when not given; they may be Q and K.  Rows with a negative
     position, or that no sequence owns, are not written.  ``inverse``: turned the other way, which makes gradients of Q and
-    K out of those of the results."""
+    K out of those of the results (which carry none themselves: nothing here is recorded for autograd)."""
     torch = _torch()
     if not isinstance(Q, torch.Tensor) or not Q.is_cuda:
         raise TypeError("Q must be a CUDA (HIP) tensor")
